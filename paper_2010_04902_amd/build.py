@@ -14,7 +14,8 @@ KERNELS = os.path.join(CSRC, "kernels.hip")
 # build in parallel this way
 # the slowest parts first: the pool starts them in this order
 KERNEL_PARTS = (2, 1, 18, 7, 4, 22, 25, 14, 24, 15, 17, 6, 5, 23, 20, 21, 8, 10, 16, 9, 11, 19, 3, 13, 12, 0)
-OTHER_SOURCES = [os.path.join(CSRC, "krum.hip"), os.path.join(CSRC, "host.cpp")]
+OTHER_SOURCES = [os.path.join(CSRC, name) for name in
+                 ("group_norm.hip", "gated_ffn.hip", "distill.hip", "krum.hip", "host.cpp")]
 
 
 def build(verbose=False):

@@ -1,0 +1,96 @@
+// Shared by the operators of a worker's step (not part of the C-ABI): element types, vector loads and
+// stores, activations, reductions in a fixed order.
+#ifndef BYZ_WORKER_INTERNAL_H
+#define BYZ_WORKER_INTERNAL_H
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "byz_internal.h"
+#include "byzshield_worker.h"
+
+#define BYZ_HIP(call)                              \
+    do {                                           \
+        hipError_t e_ = (call);                    \
+        if (e_ != hipSuccess) {                    \
+            byz_internal_set_hip_error((int)e_);   \
+            return BYZ_EDEVICE;                    \
+        }                                          \
+    } while (0)
+
+namespace byz_worker {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+inline size_t dtype_size(int dtype) { return dtype == BYZ_F32 ? 4 : 2; }
+inline bool dtype_known(int dtype) { return dtype == BYZ_F32 || dtype == BYZ_BF16 || dtype == BYZ_F16; }
+inline bool act_known(int act) { return act >= BYZ_ACT_NONE && act <= BYZ_ACT_SIGMOID; }
+
+// V neighbouring values of type T as they lie in memory, loaded and stored in one piece.
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Pack {
+    T v[V];
+};
+
+// fp32 -> T, to the nearest, ties to even
+template <typename T>
+__device__ __forceinline__ T round_to(float x) {
+    return (T)x;
+}
+
+__device__ __forceinline__ float sigmoidf(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == BYZ_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == BYZ_ACT_SILU) return z * sigmoidf(z);
+    if constexpr (ACT == BYZ_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == BYZ_ACT_SIGMOID) return sigmoidf(z);
+    return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == BYZ_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == BYZ_ACT_SILU) {
+        const float s = sigmoidf(z);
+        return s * (1.0f + z * (1.0f - s));
+    }
+    if constexpr (ACT == BYZ_ACT_GELU)
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if constexpr (ACT == BYZ_ACT_SIGMOID) {
+        const float s = sigmoidf(z);
+        return s * (1.0f - s);
+    }
+    return 1.0f;
+}
+
+// Calls fn with the activation as a compile-time constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F fn) {
+    switch (act) {
+        case BYZ_ACT_RELU: fn(std::integral_constant<int, BYZ_ACT_RELU>{}); break;
+        case BYZ_ACT_SILU: fn(std::integral_constant<int, BYZ_ACT_SILU>{}); break;
+        case BYZ_ACT_GELU: fn(std::integral_constant<int, BYZ_ACT_GELU>{}); break;
+        case BYZ_ACT_SIGMOID: fn(std::integral_constant<int, BYZ_ACT_SIGMOID>{}); break;
+        default: fn(std::integral_constant<int, BYZ_ACT_NONE>{});
+    }
+}
+
+inline bool aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// first + (rows - 1) * pitch + width elements can be counted, and addressed with 64 bits
+inline bool extent_ok(int64_t count, int64_t stride, int64_t more) {
+    int64_t span;
+    return stride >= 0 && more >= 0 && !__builtin_mul_overflow(count > 0 ? count - 1 : 0, stride, &span) &&
+           !__builtin_add_overflow(span, more, &span) && span <= (INT64_MAX >> 4);
+}
+
+}  // namespace byz_worker
+
+#endif
