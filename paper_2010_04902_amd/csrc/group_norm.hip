@@ -2,20 +2,23 @@
 //
 // A sample is a p x c matrix, a group a strip of c / groups of its columns.  A block takes a slice:
 // some whole groups (or a part of one wide group), all positions or a chunk of them.  Thread t holds the
-// same V channels at positions t / tx, t / tx + ty, ...: its values stay in registers as they were loaded.
+// same V channels at positions t / tx, t / tx + ty, ...
 //
-//   forward    mean of the tile, then the sum of squared distances from it (both from registers, so no
-//              difference of large sums), then act(xhat gamma + beta).
-//   backward   with xhat and the activation's slope recomputed, dz = dy act'(z): per channel the
-//              sums A of dz and B of dz xhat are all that is needed,
+//   forward    a thread's own mean and squared distances from it, joined pairwise (count, mean, distances) over
+//              threads, waves and chunks in a fixed order, so there is no difference of large sums.  Means are
+//              counted from the group's first value: the pairwise differences of means then lose nothing where
+//              a group's mean is many times its deviation.  Then act((x - mean) rstd gamma + beta).
+//   backward   with the activation's slope recomputed, dz = dy act'(z): per channel the sums A of dz and
+//              B of dz xhat are all that is needed,
 //                  dbeta = sum A,  dgamma = sum B  (over the samples, in order),
 //                  S1 = sum gamma A / m,  S2 = sum gamma B / m  (over a group's channels),
 //                  dx = rstd (gamma dz - S1 - xhat S2).
 //
 // Bound by memory: 2 values moved per value forward, 3 backward, a dozen operations each.  Where a slice
 // of a sample fits the registers of one block ("whole") everything is read once.  Larger samples are cut into
-// chunks: their statistics are written by a first kernel, joined by the second in chunk order (pairwise
-// update of mean and squared distances), which reads the chunk again.  No atomics.
+// chunks: a first kernel writes their statistics, a second joins them in chunk order, a third reads the chunks again.
+// No atomics.
+#include <algorithm>
 #include <type_traits>
 
 #include "worker_internal.h"
@@ -24,15 +27,23 @@ using namespace byz_worker;
 
 namespace {
 
-constexpr int kMaxThreads = 1024;
+constexpr int kForwardThreads = 1024;  // most threads of a whole slice and most 16-byte vectors that a thread holds of a
+constexpr int kForwardR = 8;           // tensor: 128 registers a thread of 1024, 256 a thread of 512, which the two
+constexpr int kBackwardThreads = 512;  // tensors of the backward pass need
+constexpr int kBackwardR = 8;
 constexpr int kMaxLanes = 256;         // most vectors of a slice's row
+constexpr int kDepth = 32;             // positions of a thread in a chunk at most: what its sums about its first
+                                       // value can lose is 2^-24 times this
 constexpr int64_t kMaxGrid = 1 << 20;  // blocks of a launch; more tiles are taken in turn
 
 struct Plan {
-    int64_t n, p, c, groups, gc;  // gc: channels of a group
-    int vec, cs, tx, ty, threads, r;
-    int parts;                    // blocks that share a group's channels (1: a slice has whole groups)
-    int64_t slices, chunk, chunks, tiles;
+    int64_t n, p, c;
+    uint32_t groups, gc;          // groups of gc channels
+    uint32_t slices, chunks, tiles;
+    int vec, cs, tx, ty, threads, r, unit;  // unit: neighbouring channels of a vector that are in one group
+    int head;                     // groups of a slice
+    uint32_t parts;               // blocks that share a group's channels (1: a slice has whole groups)
+    int64_t chunk;
 };
 
 struct View {
@@ -54,53 +65,81 @@ int widest_vec(int elem, int64_t c, std::initializer_list<View> views) {
     return 1;
 }
 
-// `regs`: 16-byte vectors that a thread holds of each tensor at most.
-Plan make_plan(int64_t n, int64_t p, int64_t c, int64_t groups, int elem, int vec, int max_r) {
-    Plan q{};
-    q.n = n, q.p = p, q.c = c, q.groups = groups, q.gc = c / groups;
+// False: more tiles than can be counted.
+bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int elem, int vec, bool forward) {
+    const int max_r = forward ? kForwardR : kBackwardR;
+    int max_threads;
+    q = Plan{};
+    const int64_t gc = c / groups;
+    int64_t slices, step;
+    q.n = n, q.p = p, q.c = c, q.groups = (uint32_t)groups, q.gc = (uint32_t)gc;
     // a slice of whole groups whose rows start at multiples of vec, or a part of one group; narrower
     // vectors where neither is possible
     for (;; vec = vec > 4 / elem ? (4 / elem > 1 ? 4 / elem : 1) : 1) {
-        const int64_t step = q.gc / gcd(q.gc, vec) * vec;
+        step = gc / gcd(gc, vec) * vec;
+        // eight units a thread: with 1024 threads their statistics would not fit 64 KB of LDS
+        max_threads = !forward ? kBackwardThreads : vec / gcd(gc, vec) >= 8 ? kForwardThreads / 2 : kForwardThreads;
         if (step / vec <= kMaxLanes) {
+            // 128 bytes of a row, a cache line, where the channels reach
             int64_t cs = step;
             while (cs * elem < 128 && cs + step <= c) cs += step;
+            // narrower, down to 64 bytes, for a slice that fits a block, or to 32 for a block on every compute unit
+            auto narrow = [&](int64_t w) { return (w / 2 + step - 1) / step * step; };
+            while (cs > step && narrow(cs) < cs &&
+                   ((narrow(cs) * elem >= 64 && p * (cs / vec) > (int64_t)max_threads * max_r) ||
+                    (narrow(cs) * elem >= 32 && n * ((c + cs - 1) / cs) < 256)))
+                cs = narrow(cs);
+            if (p * (cs / vec) > (int64_t)max_threads * max_r)  // chunks after all: back to whole lines
+                while (cs * elem < 128 && cs + step <= c) cs += step;
             q.cs = (int)cs, q.parts = 1;
-            q.slices = (c + cs - 1) / cs;
+            slices = (c + cs - 1) / cs;
             break;
         }
-        if (q.gc % vec == 0) {
-            const int64_t lanes = q.gc / vec, parts = (lanes + kMaxLanes - 1) / kMaxLanes;
+        if (gc % vec == 0) {
+            const int64_t lanes = gc / vec, parts = (lanes + kMaxLanes - 1) / kMaxLanes;
             q.cs = (int)((lanes + parts - 1) / parts) * vec;
-            q.parts = (int)((q.gc + q.cs - 1) / q.cs);
-            q.slices = groups * q.parts;
+            q.parts = (uint32_t)((gc + q.cs - 1) / q.cs);
+            slices = groups * q.parts;
             break;
         }
     }
     q.vec = vec;
+    q.unit = (int)gcd(gc, vec);
+    q.head = q.parts > 1 ? 1 : (int)(q.cs / gc);
     q.tx = q.cs / vec;
-    // four vectors a thread where that gives enough threads, max_r of them at most
     const int64_t vectors = p * q.tx;
-    int64_t threads = (vectors + 3) / 4;
-    threads = threads < 64 ? 64 : threads > kMaxThreads ? kMaxThreads : (threads + 63) / 64 * 64;
-    if (threads < q.tx) threads = (q.tx + 63) / 64 * 64;
-    q.threads = (int)threads;
-    q.ty = q.threads / q.tx;
-    int64_t r = (p + q.ty - 1) / q.ty;
-    if (r > max_r || q.parts > 1) {
-        q.threads = q.tx > 128 ? 512 : 256;
+    int64_t chunks = 1;
+    if (q.parts == 1 && vectors <= (int64_t)max_threads * max_r) {
+        // four vectors a thread where that gives enough threads
+        int64_t threads = (vectors + 3) / 4;
+        threads = threads < 64 ? 64 : threads > max_threads ? max_threads : (threads + 63) / 64 * 64;
+        if (threads < q.tx) threads = (q.tx + 63) / 64 * 64;
+        q.threads = (int)threads;
         q.ty = q.threads / q.tx;
-        r = max_r < 8 ? max_r : 8;
-        if (r > (p + q.ty - 1) / q.ty) r = (p + q.ty - 1) / q.ty;
+        const int64_t r = (p + q.ty - 1) / q.ty;
+        if (r <= max_r) {
+            q.r = r <= 1 ? 1 : r <= 2 ? 2 : r <= 4 ? 4 : 8;
+            q.chunk = p;
+        }
     }
-    q.r = r <= 1 ? 1 : r <= 2 ? 2 : r <= 4 ? 4 : r <= 8 ? 8 : 16;
-    q.chunk = (int64_t)q.ty * q.r;
-    q.chunks = (p + q.chunk - 1) / q.chunk;
-    q.tiles = n * q.chunks * q.slices;
-    return q;
+    if (!q.r) {
+        q.threads = 256;
+        q.ty = q.threads / q.tx;
+        // long chunks, as long as every compute unit gets eight
+        int depth = kDepth;
+        while (depth > 8 && n * slices * ((p + (int64_t)q.ty * depth - 1) / ((int64_t)q.ty * depth)) < 2048) depth /= 2;
+        q.chunk = (int64_t)q.ty * depth;
+        chunks = (p + q.chunk - 1) / q.chunk;
+    }
+    int64_t tiles;
+    if (__builtin_mul_overflow(n, slices, &tiles) || __builtin_mul_overflow(tiles, chunks, &tiles) || tiles > INT32_MAX ||
+        n * groups > INT32_MAX)
+        return false;
+    q.slices = (uint32_t)slices, q.chunks = (uint32_t)chunks, q.tiles = (uint32_t)tiles;
+    return true;
 }
 
-bool whole(const Plan &q) { return q.chunks == 1 && q.parts == 1; }
+bool whole(const Plan &q) { return q.r > 0; }
 
 struct Args {
     Plan q;
@@ -112,6 +151,7 @@ struct Args {
     float eps;
     int act;
     float2 *part;   // forward: (mean, squared distances) of [sample][group][chunk][part]; backward: (A, B) of [sample][chunk][channel]
+    float *first;   // forward: the groups' first values, which the third kernel may overwrite (y over x)
     float2 *total;  // backward: (A, B) of [sample][channel]
     float2 *sums;   // backward: (S1, S2) of [sample][group]
     float *dgamma, *dbeta;
@@ -119,37 +159,166 @@ struct Args {
 
 // What a block works on.
 struct Tile {
-    int64_t i, chunk, slice, p0, c0;  // sample, chunk, slice, first position, first channel
-    int np, nc;                       // positions, channels
-    int part;
-    int tx, ty;                       // this thread's vector and first position; nc / V <= tx: idle
-    __device__ Tile(const Plan &q, int64_t t, int V) {
-        slice = t % q.slices;
-        chunk = t / q.slices % q.chunks;
-        i = t / q.slices / q.chunks;
+    int64_t i, p0, c0;          // sample, first position, first channel
+    uint32_t chunk, part, g0;   // g0: first group
+    int np, nc;                 // positions, channels
+    int tx, ty;                 // this thread's vector and first position
+    bool mine;                  // the thread has channels
+    __device__ Tile(const Plan &q, uint32_t t, int V) {
+        const uint32_t rest = t / q.slices, slice = t - rest * q.slices, sample = rest / q.chunks;
+        i = sample;
+        chunk = rest - sample * q.chunks;
         p0 = chunk * q.chunk;
         np = (int)(q.p - p0 < q.chunk ? q.p - p0 : q.chunk);
-        const int64_t g = q.parts > 1 ? slice / q.parts : 0;
-        part = q.parts > 1 ? (int)(slice % q.parts) : 0;
-        c0 = q.parts > 1 ? g * q.gc + (int64_t)part * q.cs : slice * q.cs;
-        const int64_t end = q.parts > 1 ? (g + 1) * q.gc : q.c;
+        int64_t end;
+        if (q.parts > 1) {
+            g0 = slice / q.parts, part = slice - g0 * q.parts;
+            c0 = (int64_t)g0 * q.gc + (int64_t)part * q.cs;
+            end = (int64_t)(g0 + 1) * q.gc;
+        } else {
+            c0 = (int64_t)slice * q.cs, end = q.c;
+            g0 = (uint32_t)c0 / q.gc, part = 0;
+        }
         nc = (int)(end - c0 < q.cs ? end - c0 : q.cs);
-        tx = threadIdx.x % q.tx;
         ty = threadIdx.x / q.tx;
-        if (ty >= q.ty) tx = q.tx, ty = 0;  // threads beyond the last whole row of them
+        tx = threadIdx.x - ty * q.tx;
+        mine = ty < q.ty && tx * V < nc;
+        if (ty >= q.ty) ty = q.ty;  // threads beyond the last whole row of them
     }
     __device__ int groups(const Plan &q) const { return q.parts > 1 ? 1 : nc / (int)q.gc; }
-    __device__ int64_t first_group(const Plan &q) const { return c0 / q.gc; }
-    __device__ int group_width(const Plan &q) const { return q.parts > 1 ? nc : (int)q.gc; }
+    __device__ int width(const Plan &q) const { return q.parts > 1 ? nc : (int)q.gc; }  // of a group, here
+    // groups of this thread's channels, counted from g0
+    template <int V>
+    __device__ void groups_of(const Plan &q, int (&g)[V]) const {
+        const int w = width(q), first = mine ? tx * V : 0;
+        int at = first / w, rem = first - at * w;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            g[v] = at;
+            if (++rem == w) rem = 0, at++;
+        }
+    }
+    // the first value of a group, counted from g0
+    template <typename T>
+    __device__ __forceinline__ float first_of(const Args &a, int g) const {
+        return (float)((const T *)a.x)[i * a.xs + (int64_t)(g0 + g) * a.q.gc];
+    }
+    // the first values of this thread's groups
+    template <typename T, int V>
+    __device__ void firsts(const Args &a, float (&first)[V]) const {
+        int g[V];
+        groups_of<V>(a.q, g);
+#pragma unroll
+        for (int v = 0; v < V; v++) first[v] = v % a.q.unit == 0 ? first_of<T>(a, g[v]) : first[v > 0 ? v - 1 : 0];
+    }
+    template <typename T>
+    __device__ const T *in(const void *base, int64_t sample, int64_t pixel, int V) const {
+        return (const T *)base + i * sample + (p0 + ty) * pixel + c0 + tx * V;
+    }
+    template <typename T>
+    __device__ T *out(const Args &a, int V) const {
+        return (T *)a.out + i * a.os + (p0 + ty) * a.op + c0 + tx * V;
+    }
 };
+
+// Count, mean, squared distances from it.
+struct Stat {
+    float n, m, d;
+};
+
+__device__ __forceinline__ Stat join(Stat a, Stat b) {
+    // written so that a set with a count of 0 changes nothing
+    const float n = a.n + b.n, f = n > 0.0f ? b.n * __builtin_amdgcn_rcpf(n) : 0.0f, e = b.n > 0.0f ? b.m - a.m : 0.0f;
+    return Stat{n, a.n > 0.0f ? a.m + e * f : b.m, a.d + b.d + (a.n > 0.0f ? e * e * (a.n * f) : 0.0f)};
+}
+
+__device__ __forceinline__ Stat from(Stat s, int off) { return Stat{__shfl_xor(s.n, off), __shfl_xor(s.m, off), __shfl_xor(s.d, off)}; }
+
+// Joins the statistics of the wave's lanes; each gets the same bits.
+__device__ __forceinline__ Stat join_wave(Stat s, int first, int end) {
+    for (int off = first; off < end; off *= 2) {
+        const Stat o = from(s, off);
+        s = threadIdx.x & off ? join(o, s) : join(s, o);
+    }
+    return s;
+}
+
+constexpr int kStatRows = 16;
+constexpr int kSerial = 16;  // entries of a group that one thread joins
+
+// Joins the threads' statistics (n values each of V channels, mean m from the group's first value, distances d)
+// into the groups': grp[g].
+// Ends with a barrier.  `entries`: LDS for one Stat a thread and unit, or a wave's column and unit.
+template <int V>
+__device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V], float (&d)[V], float *lds, Stat *grp) {
+    // channels of a unit first: equal counts
+    float count = n;
+#pragma unroll
+    for (int w = 1; w < V; w *= 2)
+        if (q.unit > w) {
+#pragma unroll
+            for (int v = 0; v < V; v += 2 * w) {
+                const float e = m[v + w] - m[v];
+                m[v] += 0.5f * e;
+                d[v] += d[v + w] + e * e * (0.5f * count);
+            }
+            count *= 2.0f;
+        }
+    const int units = q.cs / q.unit;  // of a row of threads
+    int rows = q.ty, row = t.ty;
+    bool writes = t.mine;
+    Stat *entry = (Stat *)lds;
+    const bool joined = q.tx < 64 && (q.tx & (q.tx - 1)) == 0;  // a wave holds whole rows
+    if (joined) {
+        rows = q.threads / 64, row = threadIdx.x / 64;
+        writes = (int)(threadIdx.x % 64) < q.tx && t.tx * V < t.nc;
+    }
+    const bool even = t.np % q.ty == 0 && t.nc == q.cs;  // all threads have equal counts
+#pragma unroll
+    for (int v = 0; v < V; v++)
+        if (v % q.unit == 0) {
+            Stat s{t.mine ? count : 0.0f, m[v], d[v]};
+            if (joined && even) {
+                for (int off = q.tx; off < 64; off *= 2) {
+                    // the pair's lanes get the same bits: their sum, and the square of their difference
+                    const float m2 = __shfl_xor(s.m, off), d2 = __shfl_xor(s.d, off), e = m2 - s.m;
+                    s.m = 0.5f * (s.m + m2);
+                    s.d = (s.d + d2) + e * e * (0.5f * s.n);
+                    s.n *= 2.0f;
+                }
+            } else if (joined) {
+                s = join_wave(s, q.tx, 64);
+            }
+            if (writes) entry[row * units + (t.tx * V + v) / q.unit] = s;
+        }
+    __syncthreads();
+    const int ng = t.groups(q), per = t.width(q) / q.unit;
+    if (rows * per <= kSerial) {  // a thread a group
+        for (int g = threadIdx.x; g < ng; g += q.threads) {
+            Stat s = entry[g * per];
+            for (int y = 0; y < rows; y++)
+                for (int e = y == 0; e < per; e++) s = join(s, entry[y * units + g * per + e]);
+            grp[g] = s;
+        }
+    } else {  // a wave a group
+        const int lane = threadIdx.x % 64;
+        for (int g = threadIdx.x / 64; g < ng; g += q.threads / 64) {
+            Stat s{0.0f, 0.0f, 0.0f};
+            for (int e = lane; e < rows * per; e += 64) s = join(s, entry[e / per * units + g * per + e % per]);
+            s = join_wave(s, 1, 64);
+            if (lane == 0) grp[g] = s;
+        }
+    }
+    __syncthreads();
+}
 
 // Sums K values a thread has for each of its V channels over the threads of a channel, in a fixed order;
 // chan[k * cs + channel] gets them.  Ends with a barrier.
 template <int K, int V>
 __device__ void channel_sums(const Plan &q, const Tile &t, float (&acc)[K][V], float *lds, float *chan) {
-    const int cs = q.tx * V;
+    const int cs = q.cs;
     int rows = q.ty, row = t.ty;
-    bool writes = t.tx < q.tx;
+    bool writes = t.ty < q.ty;
     if (q.tx < 64 && (q.tx & (q.tx - 1)) == 0) {  // a wave holds whole rows: join them in registers first
 #pragma unroll
         for (int k = 0; k < K; k++)
@@ -166,8 +335,7 @@ __device__ void channel_sums(const Plan &q, const Tile &t, float (&acc)[K][V], f
 #pragma unroll
             for (int v = 0; v < V; v++) lds[(row * K + k) * cs + t.tx * V + v] = acc[k][v];
     __syncthreads();
-    int stride = 1;
-    if (rows > 16) {  // many rows: 16 threads a channel where there are enough, in place
+    if (rows > kStatRows) {  // many rows: up to 16 threads a channel, in place
         int segs = q.threads / (K * cs);
         segs = segs < 1 ? 1 : segs > 16 ? 16 : segs;
         if (segs > 1) {
@@ -183,18 +351,18 @@ __device__ void channel_sums(const Plan &q, const Tile &t, float (&acc)[K][V], f
     }
     for (int at = threadIdx.x; at < K * cs; at += q.threads) {
         float s = 0.0f;
-        for (int y = 0; y < rows; y += stride) s += lds[y * K * cs + at];
+        for (int y = 0; y < rows; y++) s += lds[y * K * cs + at];
         chan[at] = s;
     }
     __syncthreads();
 }
 
 // Sums chan (times gamma where given) over each group's channels: a wave a group, lanes strided, then a
-// butterfly.  grp[k * kStride + group].  Ends with a barrier.
+// butterfly.  grp[k * stride + group].  Ends with a barrier.
 template <int K>
 __device__ void group_sums(const Plan &q, const Tile &t, const float *chan, int cs, const float *gamma, float *grp,
                            int stride) {
-    const int ng = t.groups(q), gw = t.group_width(q), lane = threadIdx.x % 64;
+    const int ng = t.groups(q), gw = t.width(q), lane = threadIdx.x % 64;
     for (int g = threadIdx.x / 64; g < ng; g += q.threads / 64) {
         float s[K] = {};
         for (int j = lane; j < gw; j += 64) {
@@ -212,170 +380,114 @@ __device__ void group_sums(const Plan &q, const Tile &t, const float *chan, int 
     __syncthreads();
 }
 
-// (count, mean, squared distances) of two sets joined
-__device__ __forceinline__ void join(float &na, float &ma, float &qa, float nb, float mb, float qb) {
-    const float n = na + nb;
-    if (nb == 0.0f) return;
-    const float d = mb - ma, f = nb / n;
-    ma = na == 0.0f ? mb : ma + d * f;
-    qa = na == 0.0f ? qb : qa + qb + d * d * na * f;
-    na = n;
-}
-
-template <typename T, int V, int R>
-__device__ void load_tile(const Tile &t, const Plan &q, const void *base, int64_t sample, int64_t pixel,
-                          Pack<T, V> (&v)[R]) {
-    const T *at = (const T *)base + t.i * sample + (t.p0 + t.ty) * pixel + t.c0 + t.tx * V;
-    const bool mine = t.tx * V < t.nc;
+// This thread's positions of the tile, U at a time with their loads ahead: fn(position's number, vectors).
+template <typename T, int V, int U, int N, typename F>
+__device__ __forceinline__ void each_position(const Plan &q, const Tile &t, const T *const (&at)[N], const int64_t (&pixel)[N], F fn) {
+    if (!t.mine) return;
+    for (int r = 0; t.ty + r * q.ty < t.np; r += U) {
+        Pack<T, V> v[U][N];
+        const bool all = t.ty + (r + U - 1) * q.ty < t.np;
 #pragma unroll
-    for (int r = 0; r < R; r++) {
-        if (mine && t.ty + r * q.ty < t.np)
-            v[r] = *(const Pack<T, V> *)(at + (int64_t)r * q.ty * pixel);
-        else
+        for (int u = 0; u < U; u++)
+            if (all || t.ty + (r + u) * q.ty < t.np)
 #pragma unroll
-            for (int k = 0; k < V; k++) v[r].v[k] = (T)0.0f;
+                for (int j = 0; j < N; j++) v[u][j] = *(const Pack<T, V> *)(at[j] + (int64_t)(r + u) * q.ty * pixel[j]);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (all || t.ty + (r + u) * q.ty < t.np) {
+                fn(r + u, v[u]);
+                __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time, not U
+            }
     }
 }
 
-template <typename T, int V, int R, bool WHOLE>
-__global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(Args a) {
-    extern __shared__ float lds[];
-    const Plan &q = a.q;
-    const int cs = q.cs;
-    for (int64_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
-        const Tile t(q, tile, V);
-        // chan | group means | group squared distances | reduction's rows
-        float *chan = lds, *gmean = chan + cs, *gdist = gmean + cs, *rows = gdist + cs;
-        Pack<T, V> x[R];
-        load_tile<T, V, R>(t, q, a.x, a.xs, a.xp, x);
-        const float inv = 1.0f / ((float)t.np * (float)t.group_width(q));
-        float acc[1][V] = {};
-#pragma unroll
-        for (int r = 0; r < R; r++)
-#pragma unroll
-            for (int v = 0; v < V; v++) acc[0][v] += (float)x[r].v[v];
-        channel_sums<1, V>(q, t, acc, rows, chan);
-        group_sums<1>(q, t, chan, cs, nullptr, gmean, cs);
-        const bool mine = t.tx * V < t.nc;
-        const int gw = t.group_width(q);
+// The affine part of y of a thread's channels: (x - m) s + b.
+template <int V>
+struct Affine {
+    float m[V], s[V], b[V];
+    template <typename Mean, typename Rstd>
+    __device__ Affine(const Args &a, const Tile &t, Mean mean, Rstd rstd) {
         int g[V];
-        float m[V];
+        t.groups_of<V>(a.q, g);
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            g[v] = mine ? (t.tx * V + v) / gw : 0;
-            m[v] = gmean[g[v]] * inv;
-            acc[0][v] = 0.0f;
+            const int64_t c = t.c0 + (t.mine ? t.tx * V + v : 0);
+            m[v] = mean(g[v]);
+            s[v] = rstd(g[v]) * (a.gamma ? a.gamma[c] : 1.0f);
+            b[v] = a.beta ? a.beta[c] : 0.0f;
         }
-#pragma unroll
-        for (int r = 0; r < R; r++)
-            if (mine && t.ty + r * q.ty < t.np)
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const float d = (float)x[r].v[v] - m[v];
-                    acc[0][v] += d * d;
-                }
-        __syncthreads();
-        channel_sums<1, V>(q, t, acc, rows, chan);
-        group_sums<1>(q, t, chan, cs, nullptr, gdist, cs);
-        if constexpr (!WHOLE) {
-            for (int j = threadIdx.x; j < t.groups(q); j += q.threads)
-                a.part[((t.i * q.groups + t.first_group(q) + j) * q.chunks + t.chunk) * q.parts + t.part] =
-                    make_float2(gmean[j] * inv, gdist[j]);
-        } else {
-            for (int j = threadIdx.x; j < t.groups(q); j += q.threads) {
-                a.mean[t.i * q.groups + t.first_group(q) + j] = gmean[j] * inv;
-                a.rstd[t.i * q.groups + t.first_group(q) + j] = 1.0f / sqrtf(gdist[j] * inv + a.eps);
-            }
-            if (mine) {
-                float s[V], b[V];
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const int64_t c = t.c0 + t.tx * V + v;
-                    s[v] = 1.0f / sqrtf(gdist[g[v]] * inv + a.eps);
-                    s[v] *= a.gamma ? a.gamma[c] : 1.0f;
-                    b[v] = a.beta ? a.beta[c] : 0.0f;
-                }
-                T *at = (T *)a.out + t.i * a.os + (t.p0 + t.ty) * a.op + t.c0 + t.tx * V;
-                with_act(a.act, [&](auto act) {
-#pragma unroll
-                    for (int r = 0; r < R; r++)
-                        if (t.ty + r * q.ty < t.np) {
-                            Pack<T, V> y;
-#pragma unroll
-                            for (int v = 0; v < V; v++)
-                                y.v[v] = round_to<T>(act_value<act.value>(((float)x[r].v[v] - m[v]) * s[v] + b[v]));
-                            *(Pack<T, V> *)(at + (int64_t)r * q.ty * a.op) = y;
-                        }
-                });
-            }
-        }
-        __syncthreads();
     }
+    __device__ __forceinline__ float z(float x, int v) const { return (x - m[v]) * s[v] + b[v]; }
+};
+
+template <int ACT, typename T, int V>
+__device__ __forceinline__ Pack<T, V> normalised(const Affine<V> &f, const Pack<T, V> &x) {
+    Pack<T, V> y;
+#pragma unroll
+    for (int v = 0; v < V; v++) y.v[v] = round_to<T>(act_value<ACT>(f.z((float)x.v[v], v)));
+    return y;
 }
 
-// Second kernel of a large sample: joins the chunks' statistics, normalises its chunk.
+// Forward, a whole slice in registers.
 template <typename T, int V, int R>
-__global__ __launch_bounds__(512) void norm_apply_kernel(Args a) {
+__global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
-    for (int64_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
         const Tile t(q, tile, V);
-        float *gmean = lds, *grstd = lds + q.cs;
+        Stat *grp = (Stat *)lds;
+        float *entries = lds + 3 * q.head;
         Pack<T, V> x[R];
-        load_tile<T, V, R>(t, q, a.x, a.xs, a.xp, x);
-        const int ng = t.groups(q), lane = threadIdx.x % 64;
-        const int64_t entries = q.chunks * q.parts;
-        for (int g = threadIdx.x / 64; g < ng; g += q.threads / 64) {
-            const int64_t group = t.first_group(q) + g;
-            float n = 0.0f, m = 0.0f, d = 0.0f;
-            for (int64_t e = lane; e < entries; e += 64) {
-                const int64_t np = min(q.chunk, q.p - e / q.parts * q.chunk);
-                const int64_t nc = q.parts > 1 ? min((int64_t)q.cs, q.gc - e % q.parts * q.cs) : q.gc;
-                const float2 v = a.part[(t.i * q.groups + group) * entries + e];
-                join(n, m, d, (float)(np * nc), v.x, v.y);
-            }
-            for (int off = 1; off < 64; off *= 2) {
-                // both sides of a pair join in the same order and get the same values
-                const float n2 = __shfl_xor(n, off), m2 = __shfl_xor(m, off), d2 = __shfl_xor(d, off);
-                if (lane & off) {
-                    float n1 = n2, m1 = m2, d1 = d2;
-                    join(n1, m1, d1, n, m, d);
-                    n = n1, m = m1, d = d1;
-                } else {
-                    join(n, m, d, n2, m2, d2);
+        const T *at = t.in<T>(a.x, a.xs, a.xp, V);
+        int count = 0;
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (t.mine && t.ty + r * q.ty < t.np) x[r] = *(const Pack<T, V> *)(at + (int64_t)r * q.ty * a.xp), count++;
+        // counted from the thread's first value, x[0]
+        float m[V] = {}, d[V] = {}, first[V];
+        t.firsts<T, V>(a, first);
+#pragma unroll
+        for (int r = 1; r < R; r++)
+            if (r < count)
+#pragma unroll
+                for (int v = 0; v < V; v++) m[v] += (float)x[r].v[v] - (float)x[0].v[v];
+        const float inv = count ? __builtin_amdgcn_rcpf((float)count) : 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) m[v] *= inv;
+#pragma unroll
+        for (int r = 0; r < R; r++) keep_packed(x[r]);
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (r < count)
+#pragma unroll
+                for (int v = 0; v < V; v++) {
+                    const float e = ((float)x[r].v[v] - (float)x[0].v[v]) - m[v];
+                    d[v] += e * e;
                 }
-            }
-            if (lane == 0) {
-                const float rstd = 1.0f / sqrtf(d / ((float)q.p * (float)q.gc) + a.eps);
-                gmean[g] = m, grstd[g] = rstd;
-                if (t.chunk == 0 && t.part == 0) {
-                    a.mean[t.i * q.groups + group] = m;
-                    a.rstd[t.i * q.groups + group] = rstd;
-                }
-            }
+        if (count)
+#pragma unroll
+            for (int v = 0; v < V; v++) m[v] += (float)x[0].v[v] - first[v];
+#pragma unroll
+        for (int r = 0; r < R; r++) keep_packed(x[r]);
+        group_stats<V>(q, t, (float)count, m, d, entries, grp);
+        const float m1 = 1.0f / ((float)q.p * (float)q.gc);
+        auto mean = [&](int g) { return grp[g].m; };
+        auto rstd = [&](int g) { return 1.0f / sqrtf(grp[g].d * m1 + a.eps); };
+        for (int g = threadIdx.x; g < t.groups(q); g += q.threads) {
+            grp[g].m += t.first_of<T>(a, g);
+            a.mean[t.i * q.groups + t.g0 + g] = grp[g].m;
+            a.rstd[t.i * q.groups + t.g0 + g] = rstd(g);
         }
         __syncthreads();
-        if (t.tx * V < t.nc) {
-            const int gw = t.group_width(q);
-            float m[V], s[V], b[V];
-#pragma unroll
-            for (int v = 0; v < V; v++) {
-                const int g = (t.tx * V + v) / gw;
-                const int64_t c = t.c0 + t.tx * V + v;
-                m[v] = gmean[g];
-                s[v] = grstd[g] * (a.gamma ? a.gamma[c] : 1.0f);
-                b[v] = a.beta ? a.beta[c] : 0.0f;
-            }
-            T *at = (T *)a.out + t.i * a.os + (t.p0 + t.ty) * a.op + t.c0 + t.tx * V;
+        if (t.mine) {
+            const Affine<V> f(a, t, mean, rstd);
+            T *to = t.out<T>(a, V);
             with_act(a.act, [&](auto act) {
 #pragma unroll
                 for (int r = 0; r < R; r++)
-                    if (t.ty + r * q.ty < t.np) {
-                        Pack<T, V> y;
-#pragma unroll
-                        for (int v = 0; v < V; v++)
-                            y.v[v] = round_to<T>(act_value<act.value>(((float)x[r].v[v] - m[v]) * s[v] + b[v]));
-                        *(Pack<T, V> *)(at + (int64_t)r * q.ty * a.op) = y;
+                    if (r < count) {
+                        *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[r]);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
             });
         }
@@ -383,87 +495,204 @@ __global__ __launch_bounds__(512) void norm_apply_kernel(Args a) {
     }
 }
 
-// What a thread needs of its V channels in the backward pass.
-template <int V>
-struct Channel {
-    float m[V], rs[V], gamma[V], beta[V];
-    __device__ Channel(const Args &a, const Tile &t) {
-        const bool mine = t.tx * V < t.nc;
+// Forward, first kernel of a large sample: the chunk's statistics.  A thread sums about its first value.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
+    extern __shared__ float lds[];
+    const Plan &q = a.q;
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        const Tile t(q, tile, V);
+        Stat *grp = (Stat *)lds;
+        float pivot[V] = {}, s[V] = {}, d[V] = {}, first[V];
+        t.firsts<T, V>(a, first);
+        int count = 0;
+        const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
+        const int64_t pixel[1] = {a.xp};
+        each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Pack<T, V>(&x)[1]) {
+            if (r == 0)
+#pragma unroll
+                for (int v = 0; v < V; v++) pivot[v] = (float)x[0].v[v];
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                const float e = (float)x[0].v[v] - pivot[v];
+                s[v] += e, d[v] += e * e;
+            }
+            count++;
+        });
+        const float inv = count ? __builtin_amdgcn_rcpf((float)count) : 0.0f;
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            const int64_t c = t.c0 + (mine ? t.tx * V + v : 0);
-            const int64_t g = t.i * a.q.groups + c / a.q.gc;
-            m[v] = a.mean[g], rs[v] = a.rstd[g];
-            gamma[v] = a.gamma ? a.gamma[c] : 1.0f;
-            beta[v] = a.beta ? a.beta[c] : 0.0f;
+            // NaN and infinities go on as NaN; what rounding leaves below 0 does not
+            const float e = d[v] - s[v] * s[v] * inv;
+            d[v] = e < 0.0f ? 0.0f : e;
+            pivot[v] = (pivot[v] - first[v]) + s[v] * inv;
         }
+        group_stats<V>(q, t, (float)count, pivot, d, lds + 3 * q.head, grp);
+        if (t.chunk == 0 && t.part == 0)
+            for (int g = threadIdx.x; g < t.groups(q); g += q.threads) a.first[t.i * q.groups + t.g0 + g] = t.first_of<T>(a, g);
+        for (int g = threadIdx.x; g < t.groups(q); g += q.threads)
+            a.part[((t.i * q.groups + t.g0 + g) * q.chunks + t.chunk) * q.parts + t.part] = make_float2(grp[g].m, grp[g].d);
+        __syncthreads();
     }
-};
-
-template <typename T, int V, int R>
-__device__ void store_dx(const Args &a, const Tile &t, const Channel<V> &ch, const float (&s1)[V], const float (&s2)[V],
-                         const Pack<T, V> (&x)[R], const Pack<T, V> (&dy)[R]) {
-    T *at = (T *)a.out + t.i * a.os + (t.p0 + t.ty) * a.op + t.c0 + t.tx * V;
-    with_act(a.act, [&](auto act) {
-#pragma unroll
-        for (int r = 0; r < R; r++)
-            if (t.ty + r * a.q.ty < t.np) {
-                Pack<T, V> d;
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const float xh = ((float)x[r].v[v] - ch.m[v]) * ch.rs[v];
-                    const float dz = (float)dy[r].v[v] * act_slope<act.value>(xh * ch.gamma[v] + ch.beta[v]);
-                    d.v[v] = round_to<T>(ch.rs[v] * (ch.gamma[v] * dz - s1[v] - xh * s2[v]));
-                }
-                *(Pack<T, V> *)(at + (int64_t)r * a.q.ty * a.op) = d;
-            }
-    });
 }
 
-// First kernel of the backward pass: the channels' A and B; whole samples: dx too.
-template <typename T, int V, int R, bool WHOLE>
-__global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(Args a) {
+// Second kernel of a large sample: joins the chunks' statistics, a wave a group.
+__global__ __launch_bounds__(256) void norm_join_kernel(Args a) {
+    const Plan &q = a.q;
+    const int lane = threadIdx.x % 64;
+    const uint32_t all = (uint32_t)q.n * q.groups, entries = q.chunks * q.parts;
+    for (uint32_t group = blockIdx.x * 4 + threadIdx.x / 64; group < all; group += gridDim.x * 4) {
+        Stat s{0.0f, 0.0f, 0.0f};
+        for (uint32_t e = lane; e < entries; e += 64) {
+            const uint32_t chunk = e / q.parts, part = e - chunk * q.parts;
+            const int64_t np = min(q.chunk, q.p - chunk * q.chunk);
+            const uint32_t nc = q.parts > 1 ? min((uint32_t)q.cs, q.gc - part * q.cs) : q.gc;
+            const float2 v = a.part[(int64_t)group * entries + e];
+            s = join(s, Stat{(float)np * (float)nc, v.x, v.y});
+        }
+        s = join_wave(s, 1, 64);
+        if (lane == 0) {
+            a.mean[group] = s.m + a.first[group];
+            a.rstd[group] = 1.0f / sqrtf(s.d / ((float)q.p * (float)q.gc) + a.eps);
+        }
+    }
+}
+
+// Third kernel of a large sample: normalises a chunk.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void norm_apply_kernel(Args a) {
+    const Plan &q = a.q;
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        const Tile t(q, tile, V);
+        if (!t.mine) continue;
+        const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
+        const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
+        T *to = t.out<T>(a, V);
+        const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
+        const int64_t pixel[1] = {a.xp};
+        with_act(a.act, [&](auto act) {
+            each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Pack<T, V>(&x)[1]) {
+                *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[0]);
+            });
+        });
+    }
+}
+
+// dz of a value, for the sums and for dx
+template <int ACT, typename T, int V>
+__device__ __forceinline__ float slope_of(const Affine<V> &f, float x, T dy, int v) {
+    return (float)dy * act_slope<ACT>((x - f.m[v]) * f.s[v] + f.b[v]);
+}
+
+// A and B of this thread's values; B without rstd, which channel_total() multiplies
+template <int ACT, typename T, int V>
+__device__ __forceinline__ void add_values(const Affine<V> &f, const Pack<T, V> &x, const Pack<T, V> &dy, float (&acc)[2][V]) {
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+        const float e = (float)x.v[v] - f.m[v];
+        const float dz = slope_of<ACT>(f, (float)x.v[v], dy.v[v], v);
+        acc[0][v] += dz;
+        acc[1][v] += dz * e;
+    }
+}
+
+// dx = s dz + (x - m) k1 + k0 with s = rstd gamma, k1 = -rstd^2 S2, k0 = -rstd S1
+template <int ACT, typename T, int V>
+__device__ __forceinline__ Pack<T, V> gradient(const Affine<V> &f, const float (&k1)[V], const float (&k0)[V], const Pack<T, V> &x,
+                                               const Pack<T, V> &dy) {
+    Pack<T, V> d;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+        const float e = (float)x.v[v] - f.m[v];
+        d.v[v] = round_to<T>(slope_of<ACT>(f, (float)x.v[v], dy.v[v], v) * f.s[v] + (e * k1[v] + k0[v]));
+    }
+    return d;
+}
+
+// Backward, a whole slice in registers: the channels' A and B, and dx.
+template <typename T, int V, int R>
+__global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
     const int cs = q.cs;
-    for (int64_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
         const Tile t(q, tile, V);
         float *chan = lds, *grp = chan + 2 * cs, *rows = grp + 2 * cs;
+        const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
         Pack<T, V> x[R], dy[R];
-        load_tile<T, V, R>(t, q, a.x, a.xs, a.xp, x);
-        load_tile<T, V, R>(t, q, a.dy, a.ds, a.dp, dy);
-        const Channel<V> ch(a, t);
-        const bool mine = t.tx * V < t.nc;
+        const T *xat = t.in<T>(a.x, a.xs, a.xp, V), *dat = t.in<T>(a.dy, a.ds, a.dp, V);
+        int count = 0;
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (t.mine && t.ty + r * q.ty < t.np) {
+                x[r] = *(const Pack<T, V> *)(xat + (int64_t)r * q.ty * a.xp);
+                dy[r] = *(const Pack<T, V> *)(dat + (int64_t)r * q.ty * a.dp);
+                count++;
+            }
+        const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
         float acc[2][V] = {};
-        if (mine)
+        with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int r = 0; r < R; r++)
+                if (r < count) {
+                    add_values<act.value>(f, x[r], dy[r], acc);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        });
+#pragma unroll
+        for (int r = 0; r < R; r++) keep_packed(x[r]), keep_packed(dy[r]);
+        channel_sums<2, V>(q, t, acc, rows, chan);
+        for (int j = threadIdx.x; j < t.nc; j += q.threads) {
+            chan[cs + j] *= rstd[j / (int)q.gc];
+            a.total[t.i * q.c + t.c0 + j] = make_float2(chan[j], chan[cs + j]);
+        }
+        __syncthreads();
+        group_sums<2>(q, t, chan, cs, a.gamma, grp, cs);
+        if (t.mine) {
+            const float inv = 1.0f / ((float)q.p * (float)q.gc);
+            float k0[V], k1[V];
+            int g[V];
+            t.groups_of<V>(q, g);
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                const float rs = rstd[g[v]];
+                k0[v] = -rs * (grp[g[v]] * inv), k1[v] = -rs * (rs * (grp[cs + g[v]] * inv));
+            }
+            T *to = t.out<T>(a, V);
             with_act(a.act, [&](auto act) {
 #pragma unroll
                 for (int r = 0; r < R; r++)
-                    if (t.ty + r * q.ty < t.np)
-#pragma unroll
-                        for (int v = 0; v < V; v++) {
-                            const float xh = ((float)x[r].v[v] - ch.m[v]) * ch.rs[v];
-                            const float dz = (float)dy[r].v[v] * act_slope<act.value>(xh * ch.gamma[v] + ch.beta[v]);
-                            acc[0][v] += dz;
-                            acc[1][v] += dz * xh;
-                        }
+                    if (r < count) {
+                        *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, x[r], dy[r]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
             });
-        channel_sums<2, V>(q, t, acc, rows, chan);
-        float2 *to = WHOLE ? a.total + t.i * q.c : a.part + (t.i * q.chunks + t.chunk) * q.c;
-        for (int j = threadIdx.x; j < t.nc; j += q.threads) to[t.c0 + j] = make_float2(chan[j], chan[cs + j]);
-        if constexpr (WHOLE) {
-            group_sums<2>(q, t, chan, cs, a.gamma, grp, cs);
-            if (mine) {
-                const float inv = 1.0f / ((float)q.p * (float)q.gc);
-                float s1[V], s2[V];
-#pragma unroll
-                for (int v = 0; v < V; v++) {
-                    const int g = (t.tx * V + v) / (int)q.gc;
-                    s1[v] = grp[g] * inv, s2[v] = grp[cs + g] * inv;
-                }
-                store_dx<T, V, R>(a, t, ch, s1, s2, x, dy);
-            }
         }
+        __syncthreads();
+    }
+}
+
+// Backward, first kernel of a large sample: the channels' A and B of a chunk.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void norm_backward_sums_kernel(Args a) {
+    extern __shared__ float lds[];
+    const Plan &q = a.q;
+    const int cs = q.cs;
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        const Tile t(q, tile, V);
+        float *chan = lds, *rows = chan + 2 * cs;
+        const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
+        const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
+        float acc[2][V] = {};
+        const T *const at[2] = {t.in<T>(a.x, a.xs, a.xp, V), t.in<T>(a.dy, a.ds, a.dp, V)};
+        const int64_t pixel[2] = {a.xp, a.dp};
+        with_act(a.act, [&](auto act) {
+            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Pack<T, V>(&v)[2]) { add_values<act.value>(f, v[0], v[1], acc); });
+        });
+        channel_sums<2, V>(q, t, acc, rows, chan);
+        const int w = t.width(q);
+        for (int j = threadIdx.x; j < t.nc; j += q.threads)
+            a.part[(t.i * q.chunks + t.chunk) * q.c + t.c0 + j] = make_float2(chan[j], chan[cs + j] * rstd[j / w]);
         __syncthreads();
     }
 }
@@ -471,20 +700,21 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(Args a) {
 // Large samples: adds the chunks' A and B per channel, and S1 and S2 per group.  A block a group and sample.
 __global__ __launch_bounds__(256) void norm_backward_totals_kernel(Args a) {
     __shared__ float sums[2][4];
+    __shared__ float2 row[256];
     const Plan &q = a.q;
-    for (int64_t ig = blockIdx.x; ig < q.n * q.groups; ig += gridDim.x) {
-        const int64_t i = ig / q.groups, g = ig % q.groups;
+    const uint32_t all = (uint32_t)q.n * q.groups;
+    for (uint32_t ig = blockIdx.x; ig < all; ig += gridDim.x) {
+        const uint32_t i = ig / q.groups, g = ig - i * q.groups;
         // lanes of a channel: as many as fit, each takes chunks in turn
-        const int gc = q.gc < 256 ? (int)q.gc : 256, lanes = 256 / gc > 16 ? 16 : 256 / gc;
-        __shared__ float2 row[256];
+        const int gc = q.gc < 256 ? (int)q.gc : 256, lanes = min(256 / gc, 16);
+        const int lane = threadIdx.x / gc, j = threadIdx.x - lane * gc;
         float s1 = 0.0f, s2 = 0.0f;
-        for (int64_t j0 = 0; j0 < q.gc; j0 += gc) {
-            const int j = threadIdx.x % gc, lane = threadIdx.x / gc;
-            const int64_t c = g * q.gc + j0 + j;
+        for (uint32_t j0 = 0; j0 < q.gc; j0 += gc) {
+            const int64_t c = (int64_t)g * q.gc + j0 + j;
             float A = 0.0f, B = 0.0f;
             if (j0 + j < q.gc && lane < lanes)
-                for (int64_t k = lane; k < q.chunks; k += lanes) {
-                    const float2 v = a.part[(i * q.chunks + k) * q.c + c];
+                for (uint32_t k = lane; k < q.chunks; k += lanes) {
+                    const float2 v = a.part[((int64_t)i * q.chunks + k) * q.c + c];
                     A += v.x, B += v.y;
                 }
             row[threadIdx.x] = make_float2(A, B);
@@ -509,24 +739,32 @@ __global__ __launch_bounds__(256) void norm_backward_totals_kernel(Args a) {
     }
 }
 
-template <typename T, int V, int R>
-__global__ __launch_bounds__(512) void norm_backward_apply_kernel(Args a) {
+template <typename T, int V>
+__global__ __launch_bounds__(256) void norm_backward_apply_kernel(Args a) {
     const Plan &q = a.q;
-    for (int64_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
         const Tile t(q, tile, V);
-        Pack<T, V> x[R], dy[R];
-        load_tile<T, V, R>(t, q, a.x, a.xs, a.xp, x);
-        load_tile<T, V, R>(t, q, a.dy, a.ds, a.dp, dy);
-        const Channel<V> ch(a, t);
-        if (t.tx * V < t.nc) {
-            float s1[V], s2[V];
+        if (!t.mine) continue;
+        const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
+        const float2 *sums = a.sums + t.i * q.groups + t.g0;
+        const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
+        float k0[V], k1[V];
+        int g[V];
+        t.groups_of<V>(q, g);
 #pragma unroll
-            for (int v = 0; v < V; v++) {
-                const float2 s = a.sums[t.i * q.groups + (t.c0 + t.tx * V + v) / q.gc];
-                s1[v] = s.x, s2[v] = s.y;
-            }
-            store_dx<T, V, R>(a, t, ch, s1, s2, x, dy);
+        for (int v = 0; v < V; v++) {
+            const float rs = rstd[g[v]];
+            const float2 s = sums[g[v]];
+            k0[v] = -rs * s.x, k1[v] = -rs * (rs * s.y);
         }
+        T *to = t.out<T>(a, V);
+        const T *const at[2] = {t.in<T>(a.x, a.xs, a.xp, V), t.in<T>(a.dy, a.ds, a.dp, V)};
+        const int64_t pixel[2] = {a.xp, a.dp};
+        with_act(a.act, [&](auto act) {
+            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Pack<T, V>(&v)[2]) {
+                *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, v[0], v[1]);
+            });
+        });
     }
 }
 
@@ -557,42 +795,51 @@ __global__ void norm_empty_kernel(float *mean, float *rstd, int64_t count, float
 
 unsigned grid_of(int64_t tiles) { return (unsigned)(tiles < kMaxGrid ? tiles : kMaxGrid); }
 
-// LDS of the reductions: `k` sums a channel, the channels' results and the groups'.
-size_t reduction_bytes(const Plan &q, int k, int head) {
-    const bool joined = q.tx < 64 && (q.tx & (q.tx - 1)) == 0;
-    const size_t rows = joined ? q.threads / 64 : q.ty;
-    return sizeof(float) * ((size_t)head * q.cs + rows * k * q.cs);
-}
+// rows of threads that leave an entry in LDS
+size_t lds_rows(const Plan &q) { return q.tx < 64 && (q.tx & (q.tx - 1)) == 0 ? q.threads / 64 : q.ty; }
 
-template <typename T, int V, int R>
+size_t stat_bytes(const Plan &q) { return sizeof(float) * (3 * q.head + lds_rows(q) * 3 * (q.cs / q.unit)); }
+
+size_t sum_bytes(const Plan &q, int head) { return sizeof(float) * q.cs * (head + 2 * lds_rows(q)); }
+
+template <typename T, int V>
 int launch_forward(const Args &a, hipStream_t s) {
-    const size_t lds = reduction_bytes(a.q, 1, 3);
-    if (whole(a.q)) {
-        norm_forward_kernel<T, V, R, true><<<grid_of(a.q.tiles), a.q.threads, lds, s>>>(a);
-    } else if constexpr (R <= 8) {
-        norm_forward_kernel<T, V, R, false><<<grid_of(a.q.tiles), a.q.threads, lds, s>>>(a);
-        BYZ_HIP(hipGetLastError());
-        norm_apply_kernel<T, V, R><<<grid_of(a.q.tiles), a.q.threads, 2 * a.q.cs * sizeof(float), s>>>(a);
+    const unsigned grid = grid_of(a.q.tiles);
+    const int threads = a.q.threads;
+    const size_t lds = stat_bytes(a.q);
+    switch (a.q.r) {
+        case 1: norm_whole_kernel<T, V, 1><<<grid, threads, lds, s>>>(a); break;
+        case 2: norm_whole_kernel<T, V, 2><<<grid, threads, lds, s>>>(a); break;
+        case 4: norm_whole_kernel<T, V, 4><<<grid, threads, lds, s>>>(a); break;
+        case 8: norm_whole_kernel<T, V, 8><<<grid, threads, lds, s>>>(a); break;
+        default:
+            norm_stats_kernel<T, V><<<grid, threads, lds, s>>>(a);
+            BYZ_HIP(hipGetLastError());
+            norm_join_kernel<<<grid_of((a.q.n * a.q.groups + 3) / 4), 256, 0, s>>>(a);
+            BYZ_HIP(hipGetLastError());
+            norm_apply_kernel<T, V><<<grid, threads, 0, s>>>(a);
     }
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
 
-template <typename T, int V, int R>
+template <typename T, int V>
 int launch_backward(const Args &a, hipStream_t s) {
-    const size_t lds = reduction_bytes(a.q, 2, 4);
-    if constexpr (R <= 8) {
-        if (whole(a.q)) {
-            norm_backward_kernel<T, V, R, true><<<grid_of(a.q.tiles), a.q.threads, lds, s>>>(a);
-        } else {
-            norm_backward_kernel<T, V, R, false><<<grid_of(a.q.tiles), a.q.threads, lds, s>>>(a);
+    const unsigned grid = grid_of(a.q.tiles);
+    const int threads = a.q.threads;
+    switch (a.q.r) {
+        case 1: norm_backward_whole_kernel<T, V, 1><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
+        case 2: norm_backward_whole_kernel<T, V, 2><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
+        case 4: norm_backward_whole_kernel<T, V, 4><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
+        case 8: norm_backward_whole_kernel<T, V, 8><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
+        default:
+            norm_backward_sums_kernel<T, V><<<grid, threads, sum_bytes(a.q, 2), s>>>(a);
             BYZ_HIP(hipGetLastError());
             norm_backward_totals_kernel<<<grid_of(a.q.n * a.q.groups), 256, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
-            norm_backward_apply_kernel<T, V, R><<<grid_of(a.q.tiles), a.q.threads, 0, s>>>(a);
-        }
-        BYZ_HIP(hipGetLastError());
+            norm_backward_apply_kernel<T, V><<<grid, threads, 0, s>>>(a);
     }
+    BYZ_HIP(hipGetLastError());
     if (a.dgamma) {
         norm_parameters_kernel<<<(unsigned)((a.q.c + 31) / 32), 1024, 0, s>>>(a.total, a.q.n, a.q.c, a.dgamma, a.dbeta);
         BYZ_HIP(hipGetLastError());
@@ -600,26 +847,13 @@ int launch_backward(const Args &a, hipStream_t s) {
     return BYZ_OK;
 }
 
-template <typename T, int V, bool FORWARD>
-int launch_r(const Args &a, hipStream_t s) {
-    switch (a.q.r) {
-        case 1: return FORWARD ? launch_forward<T, V, 1>(a, s) : launch_backward<T, V, 1>(a, s);
-        case 2: return FORWARD ? launch_forward<T, V, 2>(a, s) : launch_backward<T, V, 2>(a, s);
-        case 4: return FORWARD ? launch_forward<T, V, 4>(a, s) : launch_backward<T, V, 4>(a, s);
-        case 8: return FORWARD ? launch_forward<T, V, 8>(a, s) : launch_backward<T, V, 8>(a, s);
-        default:
-            if constexpr (FORWARD) return launch_forward<T, V, 16>(a, s);
-            return BYZ_EINTERNAL;
-    }
-}
-
 template <typename T, bool FORWARD>
 int launch_vec(const Args &a, hipStream_t s) {
     constexpr int wide = 16 / sizeof(T), narrow = 4 / sizeof(T);
-    if (a.q.vec == wide) return launch_r<T, wide, FORWARD>(a, s);
+    if (a.q.vec == wide) return FORWARD ? launch_forward<T, wide>(a, s) : launch_backward<T, wide>(a, s);
     if constexpr (narrow > 1)
-        if (a.q.vec == narrow) return launch_r<T, narrow, FORWARD>(a, s);
-    return launch_r<T, 1, FORWARD>(a, s);
+        if (a.q.vec == narrow) return FORWARD ? launch_forward<T, narrow>(a, s) : launch_backward<T, narrow>(a, s);
+    return FORWARD ? launch_forward<T, 1>(a, s) : launch_backward<T, 1>(a, s);
 }
 
 template <bool FORWARD>
@@ -629,10 +863,6 @@ int launch(const Args &a, int dtype, hipStream_t s) {
     return launch_vec<f16, FORWARD>(a, s);
 }
 
-constexpr int kForwardR = 16, kBackwardR = 8;
-
-// Workspace of either direction, for any alignment: the plan with one element a vector has the most chunks or
-// parts of those that a call can take.
 size_t round_up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 bool sizes_ok(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
@@ -641,20 +871,21 @@ bool sizes_ok(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
            !__builtin_mul_overflow(n, p, &all) && !__builtin_mul_overflow(all, c, &all) && all <= (INT64_MAX >> 8);
 }
 
+// Workspace of either direction, for any alignment: the most that a plan takes of the widths that a call can have.
 template <typename F>
-size_t most_bytes(int elem, int64_t c, F bytes) {
+size_t most_bytes(int64_t n, int64_t p, int64_t c, int groups, int elem, bool forward, F bytes) {
     size_t most = 0;
     for (int vec : {16 / elem, 4 / elem, 1}) {
-        if (vec < 1 || c % vec) continue;
-        const size_t b = bytes(vec);
-        most = b > most ? b : most;
+        Plan q;
+        if (vec < 1 || c % vec || !make_plan(q, n, p, c, groups, elem, vec, forward)) continue;
+        most = std::max(most, bytes(q));
     }
     return most;
 }
 
-size_t forward_bytes(const Plan &q) {
-    return whole(q) ? 0 : round_up(sizeof(float2) * q.n * q.groups * q.chunks * q.parts);
-}
+size_t first_at(const Plan &q) { return round_up(sizeof(float2) * q.n * q.groups * q.chunks * q.parts); }
+
+size_t forward_bytes(const Plan &q) { return whole(q) ? 0 : first_at(q) + round_up(sizeof(float) * q.n * q.groups); }
 
 struct BackwardLayout {
     size_t total, sums, part, bytes;
@@ -671,7 +902,7 @@ struct BackwardLayout {
 extern "C" size_t byz_group_norm_workspace_bytes(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
     if (!sizes_ok(n, p, c, groups, dtype) || n == 0 || p == 0) return 0;
     const int elem = (int)dtype_size(dtype);
-    return most_bytes(elem, c, [&](int vec) { return forward_bytes(make_plan(n, p, c, groups, elem, vec, kForwardR)); });
+    return most_bytes(n, p, c, groups, elem, true, [](const Plan &q) { return forward_bytes(q); });
 }
 
 extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, int64_t n, int64_t p, int64_t c,
@@ -695,19 +926,20 @@ extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, 
     if (n > 1 && y_sample < (p - 1) * y_pixel + c) return BYZ_EINVAL;  // samples of the output may not overlap
     const int vec = widest_vec(elem, c, {{x, x_sample, x_pixel}, {y, y_sample, y_pixel}});
     Args a{};
-    a.q = make_plan(n, p, c, groups, elem, vec, kForwardR);
-    if (forward_bytes(a.q) > workspace_bytes || (forward_bytes(a.q) && !workspace)) return BYZ_ENOMEM;
+    if (!make_plan(a.q, n, p, c, groups, elem, vec, true)) return BYZ_EUNSUPPORTED;
+    if (forward_bytes(a.q) > workspace_bytes || (forward_bytes(a.q) && (!workspace || !aligned(workspace, 16)))) return BYZ_ENOMEM;
     a.x = x, a.xs = x_sample, a.xp = x_pixel;
     a.out = y, a.os = y_sample, a.op = y_pixel;
     a.gamma = gamma, a.beta = beta, a.mean = mean, a.rstd = rstd, a.eps = eps, a.act = act;
     a.part = (float2 *)workspace;
+    a.first = (float *)((char *)workspace + (whole(a.q) ? 0 : first_at(a.q)));
     return launch<true>(a, dtype, s);
 }
 
 extern "C" size_t byz_group_norm_backward_workspace_bytes(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
     if (!sizes_ok(n, p, c, groups, dtype) || n == 0 || p == 0) return 0;
     const int elem = (int)dtype_size(dtype);
-    return most_bytes(elem, c, [&](int vec) { return BackwardLayout(make_plan(n, p, c, groups, elem, vec, kBackwardR)).bytes; });
+    return most_bytes(n, p, c, groups, elem, false, [](const Plan &q) { return BackwardLayout(q).bytes; });
 }
 
 extern "C" int byz_group_norm_backward(const void *dy, int64_t dy_sample, int64_t dy_pixel, const void *x,
@@ -735,7 +967,7 @@ extern "C" int byz_group_norm_backward(const void *dy, int64_t dy_sample, int64_
         return BYZ_EINVAL;
     if (n > 1 && dx_sample < (p - 1) * dx_pixel + c) return BYZ_EINVAL;
     const int vec = widest_vec(elem, c, {{dy, dy_sample, dy_pixel}, {x, x_sample, x_pixel}, {dx, dx_sample, dx_pixel}});
-    a.q = make_plan(n, p, c, groups, elem, vec, kBackwardR);
+    if (!make_plan(a.q, n, p, c, groups, elem, vec, false)) return BYZ_EUNSUPPORTED;
     const BackwardLayout lay(a.q);
     if (!workspace || lay.bytes > workspace_bytes || !aligned(workspace, 16)) return BYZ_ENOMEM;
     a.x = x, a.xs = x_sample, a.xp = x_pixel;

@@ -37,6 +37,19 @@ struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
+// The compiler takes what it has made of these bytes (values widened to fp32) for lost: they stay packed in
+// registers, and are widened again where they are used.
+template <typename T, int V>
+__device__ __forceinline__ void keep_packed(Pack<T, V> &p) {
+    if constexpr (sizeof(p) % 4 == 0) {
+        uint32_t w[sizeof(p) / 4];
+        __builtin_memcpy(w, &p, sizeof(p));
+#pragma unroll
+        for (uint32_t &x : w) asm volatile("" : "+v"(x));
+        __builtin_memcpy(&p, w, sizeof(p));
+    }
+}
+
 // fp32 -> T, to the nearest, ties to even
 template <typename T>
 __device__ __forceinline__ T round_to(float x) {
@@ -45,11 +58,21 @@ __device__ __forceinline__ T round_to(float x) {
 
 __device__ __forceinline__ float sigmoidf(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
+// The normal distribution's upper tail at |z|, from e = exp(-z^2 / 2): the rational approximation 7.1.26 of
+// Abramowitz and Stegun for erfc(|z| / sqrt 2) / 2, good to 7.5e-8.
+__device__ __forceinline__ float normal_tail(float z, float e) {
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164190f * fabsf(z));  // 0.3275911 / sqrt 2
+    return ((((0.5307027145f * t - 0.7265760130f) * t + 0.7107068705f) * t - 0.1422483680f) * t + 0.1274147960f) * t * e;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == BYZ_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if constexpr (ACT == BYZ_ACT_SILU) return z * sigmoidf(z);
-    if constexpr (ACT == BYZ_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == BYZ_ACT_GELU) {
+        const float tail = normal_tail(z, __expf(-0.5f * z * z));
+        return z * (z < 0.0f ? tail : 1.0f - tail);
+    }
     if constexpr (ACT == BYZ_ACT_SIGMOID) return sigmoidf(z);
     return z;
 }
@@ -61,8 +84,10 @@ __device__ __forceinline__ float act_slope(float z) {
         const float s = sigmoidf(z);
         return s * (1.0f + z * (1.0f - s));
     }
-    if constexpr (ACT == BYZ_ACT_GELU)
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if constexpr (ACT == BYZ_ACT_GELU) {
+        const float e = __expf(-0.5f * z * z), tail = normal_tail(z, e);
+        return (z < 0.0f ? tail : 1.0f - tail) + z * e * 0.39894228040143268f;
+    }
     if constexpr (ACT == BYZ_ACT_SIGMOID) {
         const float s = sigmoidf(z);
         return s * (1.0f - s);
