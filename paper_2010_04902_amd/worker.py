@@ -7,6 +7,7 @@ Inputs are never copied: a layout the kernels do not read is refused.  Results d
 alone, bit for bit, which is what the server's vote over the copies of a file's gradient needs.
 """
 import ctypes
+import functools
 
 from . import binding as _b
 
@@ -17,15 +18,16 @@ BYZ_MAX_TEACHER = 1024
 BYZ_F32, BYZ_BF16, BYZ_F16 = range(3)
 
 _lib = None
+_torch = None
 _dtypes = {}
 
 
 def _load():
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     L = _b._load()
-    torch = _b._torch()
+    torch = _torch = _b._torch()
     _dtypes.update({torch.float32: BYZ_F32, torch.bfloat16: BYZ_BF16, torch.float16: BYZ_F16})
     vp, c_int, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     sig = {
@@ -53,17 +55,25 @@ def _load():
     return L
 
 
-def _on_gpu(tensors):
-    """Every tensor on one GPU, the current one."""
-    device = tensors[0][0].device
-    for t, what in tensors:
-        if not t.is_cuda:
-            raise ValueError("%s must be a CUDA tensor" % what)
-        if t.device != device:
-            raise ValueError("%s is on %s, %s on %s" % (what, t.device, tensors[0][1], device))
-    if device.index != _b._torch().cuda.current_device():
-        raise ValueError("%s is not on the current device" % tensors[0][1])
+# The small calls are bound by the host: each argument is tested by one expression of cheap terms, and only where that
+# is false a second function finds the words.
+
+
+def _device(x, what):
+    """Index of the GPU that x is on, which is the current one."""
+    device = x.get_device()
+    if device < 0:
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if device != _torch.cuda.current_device():
+        raise ValueError("%s is on cuda:%d, which is not the current device" % (what, device))
     return device
+
+
+def _refuse_device(t, what, device):
+    if t.get_device() < 0:
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if t.get_device() != device:
+        raise ValueError("%s is on cuda:%d, the call on cuda:%d" % (what, t.get_device(), device))
 
 
 def _dtype(t, what):
@@ -73,34 +83,49 @@ def _dtype(t, what):
     return code
 
 
-def _vector(t, n, what, dtype="float32"):
-    """Address of a contiguous 1-D tensor of n elements, None for None."""
+def _stream(stream, device):
+    if stream is None and _b._raw_current_stream is not None:
+        return _b._raw_current_stream(device)
+    return _b._stream_ptr(stream)
+
+
+def _floats(t, shape, what, device):
+    """Address of a contiguous float32 tensor of this shape, None for None."""
     if t is None:
         return None
-    at = _b._dev_ptr(t, (dtype,), what)
-    if t.dim() != 1 or t.shape[0] != n:
-        raise ValueError("%s has shape %s, the call needs (%d,)" % (what, tuple(t.shape), n))
-    return at
+    if t.dtype is _torch.float32 and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _refuse_device(t, what, device)
+    raise ValueError("%s is %s of shape %s%s, the call needs contiguous float32 of shape %s"
+                     % (what, t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with gaps", tuple(shape)))
 
 
 def _matrix(t, what, shape=None, dtype=None):
     """(rows, columns, pitch) of a 2-D tensor whose columns are neighbours in memory."""
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError("%s has shape %s%s" % (what, tuple(t.shape), "" if shape is None else
-                                                ", the call needs %s" % (shape,)))
-    if dtype is not None and t.dtype != dtype:
+                                                ", the call needs %s" % (tuple(shape),)))
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError("%s has dtype %s, the call needs %s" % (what, t.dtype, dtype))
     rows, cols = t.shape
-    pitch = t.stride(0) if rows > 1 else max(cols, t.stride(0))
-    if cols > 1 and t.stride(1) != 1 or pitch < cols and rows > 1:
+    pitch, step = t.stride()
+    if rows <= 1 and pitch < cols:
+        pitch = cols
+    if (step != 1 and cols > 1) or pitch < cols:
         raise ValueError("%s must have neighbouring columns and rows that do not overlap" % what)
     return rows, cols, pitch
 
 
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(name, *sizes):
+    return getattr(_lib, name)(*sizes)
+
+
 def _workspace(nbytes, empty, device):
+    """(tensor, its address): the tensor is to be held until the call has been enqueued."""
     if nbytes == 0:
         return None, None
-    t = empty(nbytes, dtype=_b._torch().uint8, device=device)
+    t = empty(nbytes, dtype=_torch.uint8, device=device)
     return t, t.data_ptr()
 
 
@@ -127,17 +152,23 @@ def _features(x, what):
     return n, p, c, sn, pixel
 
 
-def _features_like(x, empty):
+def _features_like(x, dense, empty, device):
+    if dense and empty is _torch.empty:
+        return _torch.empty_like(x)  # the same strides
     if x.dim() == 4:
         n, c, h, w = x.shape
-        return empty((n, h, w, c), dtype=x.dtype, device=x.device).permute(0, 3, 1, 2)
-    return empty(tuple(x.shape), dtype=x.dtype, device=x.device)
+        return empty((n, h, w, c), dtype=x.dtype, device=device).permute(0, 3, 1, 2)
+    return empty(x.shape, dtype=x.dtype, device=device)
 
 
-def _same(t, x, what, like):
-    if t.shape != x.shape or t.dtype != x.dtype:
-        raise ValueError("%s is %s of shape %s, %s is %s of shape %s"
-                         % (what, t.dtype, tuple(t.shape), like, x.dtype, tuple(x.shape)))
+def _strides_of(t, x, what, device, xs, xp):
+    """(sample stride, pixel stride) of features with x's shape and type."""
+    if t.shape != x.shape or t.dtype is not x.dtype:
+        raise ValueError("%s is %s of shape %s, x is %s of shape %s"
+                         % (what, t.dtype, tuple(t.shape), x.dtype, tuple(x.shape)))
+    if t.get_device() != device:
+        _refuse_device(t, what, device)
+    return (xs, xp) if t.stride() == x.stride() else _features(t, what)[3:]
 
 
 def byz_group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act=BYZ_ACT_NONE, out=None, stream=None):
@@ -145,24 +176,22 @@ def byz_group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act=BYZ_ACT_NONE,
 
     x: [n, c, h, w] in torch's channels_last memory format or [n, p, c]; float32, bfloat16 or float16.
     gamma, beta: float32 [c] or None.  out may be x."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
+    if _lib is None:
+        _load()
     n, p, c, xs, xp = _features(x, "x")
-    device = _on_gpu([(t, w) for t, w in ((x, "x"), (gamma, "gamma"), (beta, "beta"), (out, "out")) if t is not None])
-    dtype, groups = _dtype(x, "x"), int(groups)
+    index = _device(x, "x")
+    device, dtype, groups = x.device, _dtype(x, "x"), int(groups)
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    g, b = _floats(gamma, (c,), "gamma", index), _floats(beta, (c,), "beta", index)
     if out is None:
-        out = _features_like(x, empty)
-    else:
-        _same(out, x, "out", "x")
-    _, _, _, ys, yp = _features(out, "out")
-    mean = empty((n, max(groups, 0)), dtype=torch.float32, device=device)
-    rstd = empty((n, max(groups, 0)), dtype=torch.float32, device=device)
-    nbytes = L.byz_group_norm_workspace_bytes(n, p, c, groups, dtype)
+        out = _features_like(x, xp == c and (n <= 1 or xs == p * c), empty, device)
+    ys, yp = _strides_of(out, x, "out", index, xs, xp)
+    mean = empty((n, max(groups, 0)), dtype=_torch.float32, device=device)
+    rstd = empty((n, max(groups, 0)), dtype=_torch.float32, device=device)
+    nbytes = _workspace_bytes("byz_group_norm_workspace_bytes", n, p, c, groups, dtype)
     ws, at = _workspace(nbytes, empty, device)
-    _b._check(L.byz_group_norm(x.data_ptr(), xs, xp, n, p, c, groups, dtype, _vector(gamma, c, "gamma"),
-                               _vector(beta, c, "beta"), float(eps), int(act), out.data_ptr(), ys, yp,
-                               mean.data_ptr(), rstd.data_ptr(), at, nbytes, _b._stream_ptr(stream)), "byz_group_norm")
+    _b._check(_lib.byz_group_norm(x.data_ptr(), xs, xp, n, p, c, groups, dtype, g, b, eps, act, out.data_ptr(), ys, yp,
+                                  mean.data_ptr(), rstd.data_ptr(), at, nbytes, _stream(stream, index)), "byz_group_norm")
     return out, mean, rstd
 
 
@@ -171,51 +200,58 @@ def byz_group_norm_backward(dy, x, groups, mean, rstd, gamma=None, beta=None, ac
     """-> (dx, dgamma[c] float32, dbeta[c] float32) for dy, from x and byz_group_norm's mean and rstd.
 
     out (dx) may be dy.  parameters=False: dgamma and dbeta are None and not computed."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
+    if _lib is None:
+        _load()
     n, p, c, xs, xp = _features(x, "x")
-    device = _on_gpu([(t, w) for t, w in ((x, "x"), (dy, "dy"), (mean, "mean"), (rstd, "rstd"), (gamma, "gamma"),
-                                          (beta, "beta"), (out, "out")) if t is not None])
-    dtype, groups = _dtype(x, "x"), int(groups)
-    _same(dy, x, "dy", "x")
-    _, _, _, ds, dp = _features(dy, "dy")
+    index = _device(x, "x")
+    device, dtype, groups = x.device, _dtype(x, "x"), int(groups)
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    ds, dp = _strides_of(dy, x, "dy", index, xs, xp)
+    g, b = _floats(gamma, (c,), "gamma", index), _floats(beta, (c,), "beta", index)
+    m, r = _floats(mean, (n, groups), "mean", index), _floats(rstd, (n, groups), "rstd", index)
     if out is None:
-        out = _features_like(x, empty)
-    else:
-        _same(out, x, "out", "x")
-    _, _, _, os, op = _features(out, "out")
-    for t, what in ((mean, "mean"), (rstd, "rstd")):
-        if tuple(t.shape) != (n, groups) or t.dtype != torch.float32 or not t.is_contiguous():
-            raise ValueError("%s must be contiguous float32 [%d, %d]" % (what, n, groups))
+        out = _features_like(x, xp == c and (n <= 1 or xs == p * c), empty, device)
+    os, op = _strides_of(out, x, "out", index, xs, xp)
     dgamma = dbeta = None
     if parameters:
-        dgamma = empty(c, dtype=torch.float32, device=device)
-        dbeta = empty(c, dtype=torch.float32, device=device)
-    nbytes = L.byz_group_norm_backward_workspace_bytes(n, p, c, groups, dtype)
+        dgamma = empty(c, dtype=_torch.float32, device=device)
+        dbeta = empty(c, dtype=_torch.float32, device=device)
+    nbytes = _workspace_bytes("byz_group_norm_backward_workspace_bytes", n, p, c, groups, dtype)
     ws, at = _workspace(nbytes, empty, device)
-    _b._check(L.byz_group_norm_backward(
-        dy.data_ptr(), ds, dp, x.data_ptr(), xs, xp, n, p, c, groups, dtype, _vector(gamma, c, "gamma"),
-        _vector(beta, c, "beta"), mean.data_ptr(), rstd.data_ptr(), int(act), out.data_ptr(), os, op,
+    _b._check(_lib.byz_group_norm_backward(
+        dy.data_ptr(), ds, dp, x.data_ptr(), xs, xp, n, p, c, groups, dtype, g, b, m, r, act, out.data_ptr(), os, op,
         dgamma.data_ptr() if parameters else None, dbeta.data_ptr() if parameters else None, at, nbytes,
-        _b._stream_ptr(stream)), "byz_group_norm_backward")
+        _stream(stream, index)), "byz_group_norm_backward")
     return out, dgamma, dbeta
 
 
 # ------------------------------------------------------------------ distillation
 
 
-def _distill_arguments(logits, teacher, index, more=()):
+def _distill_arguments(logits, teacher, index):
+    """(rows, vocab, pitch, k, teacher's pitch, GPU)"""
     rows, vocab, ld = _matrix(logits, "logits")
-    trows, k, tld = _matrix(teacher, "teacher", dtype=_b._torch().float32)
-    _, _, ild = _matrix(index, "index", (trows, k), _b._torch().int32)
+    trows, k, tld = _matrix(teacher, "teacher", dtype=_torch.float32)
+    _, _, ild = _matrix(index, "index", teacher.shape, _torch.int32)
     if trows != rows:
         raise ValueError("teacher has %d rows, logits %d" % (trows, rows))
     if tld != ild and rows > 1:
         raise ValueError("teacher and index must have one row pitch")
-    device = _on_gpu([(t, w) for t, w in ((logits, "logits"), (teacher, "teacher"), (index, "index")) + tuple(more)
-                      if t is not None])
+    device = _device(logits, "logits")
+    if teacher.get_device() != device or index.get_device() != device:
+        _refuse_device(teacher, "teacher", device)
+        _refuse_device(index, "index", device)
     return rows, vocab, ld, k, tld, device
+
+
+def _gradient_out(out, logits, empty, index):
+    """(dlogits, pitch)"""
+    if out is None:
+        out = empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        return out, out.shape[1]
+    if out.get_device() != index:
+        _refuse_device(out, "out", index)
+    return out, _matrix(out, "out", logits.shape, logits.dtype)[2]
 
 
 def byz_distill_loss(logits, teacher, index, temperature=1.0, stream=None):
@@ -223,72 +259,71 @@ def byz_distill_loss(logits, teacher, index, temperature=1.0, stream=None):
 
     logits [rows, vocab] float32, bfloat16 or float16; teacher float32 and index int32 [rows, k]: the
     teacher's logits and their places, a negative place is no entry."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
-    rows, vocab, ld, k, tld, device = _distill_arguments(logits, teacher, index)
-    dtype = _dtype(logits, "logits")
-    loss = empty(rows, dtype=torch.float32, device=device)
-    lse = empty(rows, dtype=torch.float32, device=device)
-    nbytes = L.byz_distill_loss_workspace_bytes(rows, vocab, k, dtype)
+    if _lib is None:
+        _load()
+    rows, vocab, ld, k, tld, gpu = _distill_arguments(logits, teacher, index)
+    device, dtype = logits.device, _dtype(logits, "logits")
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    loss = empty(rows, dtype=_torch.float32, device=device)
+    lse = empty(rows, dtype=_torch.float32, device=device)
+    nbytes = _workspace_bytes("byz_distill_loss_workspace_bytes", rows, vocab, k, dtype)
     ws, at = _workspace(nbytes, empty, device)
-    _b._check(L.byz_distill_loss(logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k, tld,
-                                 float(temperature), loss.data_ptr(), lse.data_ptr(), at, nbytes,
-                                 _b._stream_ptr(stream)), "byz_distill_loss")
+    _b._check(_lib.byz_distill_loss(logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k, tld,
+                                    temperature, loss.data_ptr(), lse.data_ptr(), at, nbytes, _stream(stream, gpu)),
+              "byz_distill_loss")
     return loss, lse
 
 
 def byz_distill_loss_backward(dloss, logits, teacher, index, lse, temperature=1.0, out=None, stream=None):
     """-> dlogits (type of logits) for dloss[rows] float32, from byz_distill_loss' lse.  out may be logits."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
-    rows, vocab, ld, k, tld, device = _distill_arguments(logits, teacher, index, ((dloss, "dloss"), (lse, "lse"),
-                                                                                  (out, "out")))
+    if _lib is None:
+        _load()
+    rows, vocab, ld, k, tld, gpu = _distill_arguments(logits, teacher, index)
     dtype = _dtype(logits, "logits")
-    if out is None:
-        out = empty((rows, vocab), dtype=logits.dtype, device=device)
-    _, _, old = _matrix(out, "out", (rows, vocab), logits.dtype)
-    _b._check(L.byz_distill_loss_backward(
-        _vector(dloss, rows, "dloss"), logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k,
-        tld, _vector(lse, rows, "lse"), float(temperature), out.data_ptr(), old, _b._stream_ptr(stream)),
-        "byz_distill_loss_backward")
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    d, l = _floats(dloss, (rows,), "dloss", gpu), _floats(lse, (rows,), "lse", gpu)
+    out, old = _gradient_out(out, logits, empty, gpu)
+    _b._check(_lib.byz_distill_loss_backward(d, logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(),
+                                             index.data_ptr(), k, tld, l, temperature, out.data_ptr(), old,
+                                             _stream(stream, gpu)), "byz_distill_loss_backward")
     return out
 
 
 def byz_distill_loss_step(logits, teacher, index, dloss, temperature=1.0, out=None, stream=None):
     """Loss and gradient in one call, for weights dloss[rows] float32 known beforehand
     -> (loss[rows] float32, dlogits).  out (dlogits) may be logits."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
-    rows, vocab, ld, k, tld, device = _distill_arguments(logits, teacher, index, ((dloss, "dloss"), (out, "out")))
-    dtype = _dtype(logits, "logits")
-    if out is None:
-        out = empty((rows, vocab), dtype=logits.dtype, device=device)
-    _, _, old = _matrix(out, "out", (rows, vocab), logits.dtype)
-    loss = empty(rows, dtype=torch.float32, device=device)
-    nbytes = L.byz_distill_loss_workspace_bytes(rows, vocab, k, dtype)
+    if _lib is None:
+        _load()
+    rows, vocab, ld, k, tld, gpu = _distill_arguments(logits, teacher, index)
+    device, dtype = logits.device, _dtype(logits, "logits")
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    d = _floats(dloss, (rows,), "dloss", gpu)
+    out, old = _gradient_out(out, logits, empty, gpu)
+    loss = empty(rows, dtype=_torch.float32, device=device)
+    nbytes = _workspace_bytes("byz_distill_loss_workspace_bytes", rows, vocab, k, dtype)
     ws, at = _workspace(nbytes, empty, device)
-    _b._check(L.byz_distill_loss_step(
-        logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k, tld,
-        _vector(dloss, rows, "dloss"), float(temperature), loss.data_ptr(), None, out.data_ptr(), old, at, nbytes,
-        _b._stream_ptr(stream)), "byz_distill_loss_step")
+    _b._check(_lib.byz_distill_loss_step(logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k,
+                                         tld, d, temperature, loss.data_ptr(), None, out.data_ptr(), old, at, nbytes,
+                                         _stream(stream, gpu)), "byz_distill_loss_step")
     return loss, out
 
 
 # ------------------------------------------------------------------ gated feed-forward
 
 
-def _ffn_arguments(x, w_gate, w_up, more=()):
+def _ffn_arguments(x, w_gate, w_up):
+    """(m, k, n, x's pitch, the weights' pitch, GPU)"""
     m, k, x_ld = _matrix(x, "x")
-    n, wk, w_ld = _matrix(w_gate, "w_gate", dtype=x.dtype)
-    _, _, u_ld = _matrix(w_up, "w_up", (n, wk), x.dtype)
+    n, wk, w_ld = _matrix(w_gate, "w_gate", None, x.dtype)
+    _, _, u_ld = _matrix(w_up, "w_up", w_gate.shape, x.dtype)
     if wk != k:
         raise ValueError("x has %d columns, the weights %d" % (k, wk))
     if u_ld != w_ld and n > 1:
         raise ValueError("w_gate and w_up must have one row pitch")
-    device = _on_gpu([(t, w) for t, w in ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up")) + tuple(more) if t is not None])
+    device = _device(x, "x")
+    if w_gate.get_device() != device or w_up.get_device() != device:
+        _refuse_device(w_gate, "w_gate", device)
+        _refuse_device(w_up, "w_up", device)
     return m, k, n, x_ld, w_ld, device
 
 
@@ -297,43 +332,53 @@ def byz_gated_ffn(x, w_gate, w_up, act=BYZ_ACT_SILU, save=False, out=None, strea
     backward pass.
 
     x [m, k], w_gate and w_up [n, k], bfloat16 or float16."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
-    m, k, n, x_ld, w_ld, device = _ffn_arguments(x, w_gate, w_up, ((out, "out"),))
-    dtype = _dtype(x, "x")
+    if _lib is None:
+        _load()
+    m, k, n, x_ld, w_ld, gpu = _ffn_arguments(x, w_gate, w_up)
+    device, dtype, kind = x.device, _dtype(x, "x"), x.dtype
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
     if out is None:
-        out = empty((m, n), dtype=x.dtype, device=device)
-    _, _, h_ld = _matrix(out, "out", (m, n), x.dtype)
+        out, h_ld = empty((m, n), dtype=kind, device=device), n
+    else:
+        if out.get_device() != gpu:
+            _refuse_device(out, "out", gpu)
+        h_ld = _matrix(out, "out", (m, n), kind)[2]
     gate = up = None
+    wide = n
     if save:  # rows of whole 16 bytes: the backward pass reads them in pieces
         wide = (n + 3) // 4 * 4
-        gate, up = (empty((m, wide), dtype=torch.float32, device=device)[:, :n] for _ in range(2))
-    _b._check(L.byz_gated_ffn(x.data_ptr(), x_ld, w_gate.data_ptr(), w_up.data_ptr(), w_ld, m, k, n, dtype, int(act),
-                              out.data_ptr(), h_ld, gate.data_ptr() if save else None, up.data_ptr() if save else None,
-                              gate.stride(0) if save else 0, _b._stream_ptr(stream)), "byz_gated_ffn")
+        gate = empty((m, wide), dtype=_torch.float32, device=device)
+        up = empty((m, wide), dtype=_torch.float32, device=device)
+        if wide != n:
+            gate, up = gate[:, :n], up[:, :n]
+    _b._check(_lib.byz_gated_ffn(x.data_ptr(), x_ld, w_gate.data_ptr(), w_up.data_ptr(), w_ld, m, k, n, dtype, act,
+                                 out.data_ptr(), h_ld, gate.data_ptr() if save else None, up.data_ptr() if save else None,
+                                 wide, _stream(stream, gpu)), "byz_gated_ffn")
     return (out, gate, up) if save else out
 
 
 def byz_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, act=BYZ_ACT_SILU, stream=None):
     """-> (dx, dw_gate, dw_up) for dh [m, n], from byz_gated_ffn's gate and up."""
-    L = _load()
-    torch = _b._torch()
-    empty = torch.empty if stream is None else _b._empty_on(stream)
-    m, k, n, x_ld, w_ld, device = _ffn_arguments(x, w_gate, w_up, ((dh, "dh"), (gate, "gate"), (up, "up")))
-    dtype = _dtype(x, "x")
-    _, _, dh_ld = _matrix(dh, "dh", (m, n), x.dtype)
-    _, _, gate_ld = _matrix(gate, "gate", (m, n), torch.float32)
-    _, _, up_ld = _matrix(up, "up", (m, n), torch.float32)
+    if _lib is None:
+        _load()
+    m, k, n, x_ld, w_ld, gpu = _ffn_arguments(x, w_gate, w_up)
+    device, dtype, kind = x.device, _dtype(x, "x"), x.dtype
+    empty = _torch.empty if stream is None else _b._empty_on(stream)
+    _, _, dh_ld = _matrix(dh, "dh", (m, n), kind)
+    _, _, gate_ld = _matrix(gate, "gate", (m, n), _torch.float32)
+    _, _, up_ld = _matrix(up, "up", (m, n), _torch.float32)
     if gate_ld != up_ld and m > 1:
         raise ValueError("gate and up must have one row pitch")
-    dx = empty((m, k), dtype=x.dtype, device=device)
-    dw_gate = empty((n, k), dtype=x.dtype, device=device)
-    dw_up = empty((n, k), dtype=x.dtype, device=device)
-    nbytes = L.byz_gated_ffn_backward_workspace_bytes(m, k, n, dtype)
+    for t, what in ((dh, "dh"), (gate, "gate"), (up, "up")):
+        if t.get_device() != gpu:
+            _refuse_device(t, what, gpu)
+    dx = empty((m, k), dtype=kind, device=device)
+    dw_gate = empty((n, k), dtype=kind, device=device)
+    dw_up = empty((n, k), dtype=kind, device=device)
+    nbytes = _workspace_bytes("byz_gated_ffn_backward_workspace_bytes", m, k, n, dtype)
     ws, at = _workspace(nbytes, empty, device)
-    _b._check(L.byz_gated_ffn_backward(
+    _b._check(_lib.byz_gated_ffn_backward(
         dh.data_ptr(), dh_ld, x.data_ptr(), x_ld, w_gate.data_ptr(), w_up.data_ptr(), w_ld, gate.data_ptr(),
-        up.data_ptr(), gate_ld, m, k, n, dtype, int(act), dx.data_ptr(), k, dw_gate.data_ptr(), dw_up.data_ptr(), k,
-        at, nbytes, _b._stream_ptr(stream)), "byz_gated_ffn_backward")
+        up.data_ptr(), gate_ld, m, k, n, dtype, act, dx.data_ptr(), k, dw_gate.data_ptr(), dw_up.data_ptr(), k,
+        at, nbytes, _stream(stream, gpu)), "byz_gated_ffn_backward")
     return dx, dw_gate, dw_up
