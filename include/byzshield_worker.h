@@ -110,11 +110,14 @@ int byz_distill_loss_step(const void *logits, int64_t rows, int64_t vocab, int64
  *     gate = x w_gate^T,  up = x w_up^T,  h = act(gate) * up
  * in one kernel; the products are summed in fp32 and h (pitch h_ld) comes from the unrounded sums.
  * gate_out and up_out (m x n, pitch gate_ld; both or neither may be NULL) keep the sums for the
- * backward pass.  fp32 is BYZ_EUNSUPPORTED.
+ * backward pass.  fp32 is BYZ_EUNSUPPORTED.  The workspace is for more than 16 tokens whose x or weights have to be
+ * copied first: k not a multiple of 8, or rows that do not start at 16-byte boundaries; else it may be NULL.
  */
+size_t byz_gated_ffn_workspace_bytes(int64_t m, int64_t k, int64_t n, int dtype);
 int byz_gated_ffn(const void *x, int64_t x_ld, const void *w_gate, const void *w_up, int64_t w_ld,
                   int64_t m, int64_t k, int64_t n, int dtype, int act, void *h, int64_t h_ld,
-                  float *gate_out, float *up_out, int64_t gate_ld, void *stream);
+                  float *gate_out, float *up_out, int64_t gate_ld, void *workspace,
+                  size_t workspace_bytes, void *stream);
 
 /*
  * Its gradients for dh (m x n, pitch dh_ld) from the saved gate and up (pitch gate_ld):

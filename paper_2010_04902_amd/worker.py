@@ -42,7 +42,8 @@ def _load():
         "byz_distill_loss_backward": (c_int, [vp, vp, i64, i64, i64, c_int, vp, vp, c_int, i64, vp, f32, vp, i64, vp]),
         "byz_distill_loss_step": (c_int, [vp, i64, i64, i64, c_int, vp, vp, c_int, i64, vp, f32, vp, vp, vp, i64,
                                           vp, sz, vp]),
-        "byz_gated_ffn": (c_int, [vp, i64, vp, vp, i64, i64, i64, i64, c_int, c_int, vp, i64, vp, vp, i64, vp]),
+        "byz_gated_ffn_workspace_bytes": (sz, [i64, i64, i64, c_int]),
+        "byz_gated_ffn": (c_int, [vp, i64, vp, vp, i64, i64, i64, i64, c_int, c_int, vp, i64, vp, vp, i64, vp, sz, vp]),
         "byz_gated_ffn_backward_workspace_bytes": (sz, [i64, i64, i64, c_int]),
         "byz_gated_ffn_backward": (c_int, [vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, i64, c_int, c_int,
                                            vp, i64, vp, vp, i64, vp, sz, vp]),
@@ -351,9 +352,14 @@ def byz_gated_ffn(x, w_gate, w_up, act=BYZ_ACT_SILU, save=False, out=None, strea
         up = empty((m, wide), dtype=_torch.float32, device=device)
         if wide != n:
             gate, up = gate[:, :n], up[:, :n]
-    _b._check(_lib.byz_gated_ffn(x.data_ptr(), x_ld, w_gate.data_ptr(), w_up.data_ptr(), w_ld, m, k, n, dtype, act,
-                                 out.data_ptr(), h_ld, gate.data_ptr() if save else None, up.data_ptr() if save else None,
-                                 wide, _stream(stream, gpu)), "byz_gated_ffn")
+    xa, ga, ua = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    nbytes, ws, at = 0, None, None
+    if m > 16 and (k | x_ld | w_ld) % 8 | (xa | ga | ua) % 16:  # rows that the kernel cannot read as they lie
+        nbytes = _workspace_bytes("byz_gated_ffn_workspace_bytes", m, k, n, dtype)
+        ws, at = _workspace(nbytes, empty, device)
+    _b._check(_lib.byz_gated_ffn(xa, x_ld, ga, ua, w_ld, m, k, n, dtype, act, out.data_ptr(), h_ld,
+                                 gate.data_ptr() if save else None, up.data_ptr() if save else None, wide, at, nbytes,
+                                 _stream(stream, gpu)), "byz_gated_ffn")
     return (out, gate, up) if save else out
 
 

@@ -134,8 +134,9 @@ def test_distill_needs_its_outputs():
         assert call(rows=0, logits=None) == OK
 
 
-def _ffn(x=P, x_ld=32, wg=P, wu=P, w_ld=32, m=4, k=32, n=8, dtype=1, act=2, h=P, h_ld=8, gate=None, up=None, gate_ld=0):
-    return worker._load().byz_gated_ffn(x, x_ld, wg, wu, w_ld, m, k, n, dtype, act, h, h_ld, gate, up, gate_ld, None)
+def _ffn(x=P, x_ld=32, wg=P, wu=P, w_ld=32, m=4, k=32, n=8, dtype=1, act=2, h=P, h_ld=8, gate=None, up=None, gate_ld=0,
+         ws=None, nbytes=0):
+    return worker._load().byz_gated_ffn(x, x_ld, wg, wu, w_ld, m, k, n, dtype, act, h, h_ld, gate, up, gate_ld, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("bad", [
@@ -149,6 +150,17 @@ def test_gated_ffn_refusals(bad):
 def test_gated_ffn_types_and_empty_calls():
     assert _ffn(dtype=0) == EUNSUPPORTED
     assert _ffn(m=0) == OK and _ffn(n=0) == OK and _ffn(m=0, x=None, h=None) == OK
+
+
+def test_gated_ffn_needs_its_workspace():
+    # more tokens than the kernel for few takes, rows that do not start at 16-byte boundaries
+    need = worker._load().byz_gated_ffn_workspace_bytes(40, 31, 8, 1)
+    assert need > 0 and worker._load().byz_gated_ffn_workspace_bytes(16, 31, 8, 1) == 0
+    odd = dict(m=40, k=31, x_ld=31, w_ld=31)
+    assert _ffn(**odd) == ENOMEM
+    assert _ffn(**odd, ws=P, nbytes=need - 1) == ENOMEM
+    assert _ffn(**odd, ws=P + 2, nbytes=need) == ENOMEM
+    assert _ffn(m=40, x=P + 2) == ENOMEM
 
 
 def _ffn_backward(dh=P, dh_ld=8, x=P, x_ld=32, wg=P, wu=P, w_ld=32, gate=P, up=P, gate_ld=8, m=4, k=32, n=8, dtype=1, act=2,
