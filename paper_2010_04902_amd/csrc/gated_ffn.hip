@@ -67,17 +67,17 @@ struct Product {
     int act;
     int tiles_m, tiles_n;
     bool direct;             // whole steps go from memory to LDS without registers
+    bool out_wide, gate_wide;  // rows of results start at 16-byte boundaries
 };
 
-// A step of the sum is 32 values of k.  In LDS an operand by rows has 64 bytes a row, in four 16-byte pieces; by columns 32
-// rows (of k) of a tile's width.  A wave's load instruction fills 1024 bytes in lane order, so pieces are exchanged on
-// the way by the global addresses: without that, lanes that read one piece of 16 rows, or four rows of k, would meet
-// in the same banks.
-constexpr int kStep = 32;
+// A step of the sum is 64 values of k.  In LDS an operand by rows has 128 bytes a row, in eight 16-byte pieces; by columns
+// 64 rows (of k) of a tile's width.  A wave's load instruction fills 1024 bytes in lane order, so pieces are exchanged
+// on the way by the global addresses: without that, lanes that read one piece of 16 rows, or four rows of k, would
+// meet in the same banks.
+constexpr int kStep = 64;
 
-template <int WIDTH>
 __device__ __forceinline__ int row_piece(int row, int piece) {  // by rows: byte of a piece
-    return row * 64 + ((piece ^ ((row >> 2) & 3)) * 16);
+    return row * 128 + ((piece ^ ((row >> 1) & 7)) * 16);
 }
 template <int WIDTH>
 __device__ __forceinline__ int column_turn(int row) {  // by columns: what the 64-byte slots of a row of k are exchanged by
@@ -99,7 +99,7 @@ __device__ __forceinline__ void load_to_lds(const void *from, uint32_t lds) {
 template <typename T, int WIDTH, bool COLUMNS>
 struct Side {
     using frag = typename Frag<T>::type;
-    static constexpr int kBytes = WIDTH * 64, kChunks = WIDTH / 16;
+    static constexpr int kChunks = WIDTH / 8;  // load instructions of a step
 
     // Byte offset from the tile's corner of what lane `lane` of chunk `chunk` loads.  `outer`: outer indices from
     // the corner on; rows and pieces past the end load the last, and their products are not stored.
@@ -110,7 +110,7 @@ struct Side {
             const int piece = (((at >> 2) ^ column_turn<WIDTH>(row)) << 2) | (at & 3);
             return (uint32_t)((row * ld + std::min<int64_t>(piece * 8, outer - 8)) * sizeof(T));
         }
-        const int row = chunk * 16 + lane / 4, piece = (lane % 4) ^ ((row >> 2) & 3);
+        const int row = chunk * 8 + lane / 8, piece = (lane % 8) ^ ((row >> 1) & 7);
         return (uint32_t)((std::min<int64_t>(row, outer - 1) * ld + piece * 8) * sizeof(T));
     }
 
@@ -123,9 +123,9 @@ struct Side {
             if (row < ks) v = *(const frag *)(at + row * ld + std::min<int64_t>(piece * 8, outer - 8));
             *(frag *)(lds + row * WIDTH * 2 + (((piece >> 2) ^ column_turn<WIDTH>(row)) << 6) + (piece & 3) * 16) = v;
         } else {
-            const int row = number / 4, piece = number % 4;
+            const int row = number / 8, piece = number % 8;
             if (piece * 8 < ks) v = *(const frag *)(at + std::min<int64_t>(row, outer - 1) * ld + piece * 8);
-            *(frag *)(lds + row_piece<WIDTH>(row, piece)) = v;
+            *(frag *)(lds + row_piece(row, piece)) = v;
         }
     }
 
@@ -135,11 +135,11 @@ struct Side {
             const int q = lane % 16 / 4;  // the row of four that the lane reads for its group of 16
             return (lane / 32 * 8 + q) * WIDTH * 2 + (((first / 32) ^ column_turn<WIDTH>(q)) << 6) + lane / 16 % 2 * 32 + lane % 4 * 8;
         }
-        return row_piece<WIDTH>(first + lane % 32, lane / 32);
+        return row_piece(first + lane % 32, lane / 32);
     }
 
-    // Values 16 half .. 16 half + 15 of the step: lane l has outer index l % 32 and k = 8 (l / 32) .. + 7.
-    static __device__ __forceinline__ frag read(const char *lds, int at, int half) {
+    // Values 16 quarter .. 16 quarter + 15 of the step: lane l has outer index l % 32 and k = 8 (l / 32) .. + 7.
+    static __device__ __forceinline__ frag read(const char *lds, int at, int quarter) {
         if constexpr (COLUMNS) {
             // four rows of k, 16 outer indices, turned by the load: a lane gets its index's four values
             typedef short s4 __attribute__((ext_vector_type(4)));
@@ -148,192 +148,272 @@ struct Side {
                 s4 v[2];
             } two;
 #pragma unroll
-            for (int i = 0; i < 2; i++) two.v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(lds + at + (half * 16 + i * 4) * WIDTH * 2));
+            for (int i = 0; i < 2; i++)
+                two.v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(lds + at + (quarter * 16 + i * 4) * WIDTH * 2));
             return __builtin_bit_cast(frag, two);
         }
-        return *(const frag *)(lds + (at ^ (half * 32)));
+        return *(const frag *)(lds + (at ^ (quarter * 32)));
     }
 };
 
+// The same number, of which the compiler knows nothing: what is computed from it is not kept over a loop, where the
+// registers are wanted for sums.
+__device__ __forceinline__ int afresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// A block's place among the output tiles, and what its loads need.
+template <typename T, int BM, int BN, int WM, int WN, Kind KIND>
+struct Place {
+    using A = Side<T, BM, KIND == kWeight>;
+    using B = Side<T, KIND == kForward ? BN / 2 : BN, KIND != kForward>;  // kForward: two sides, w_gate's and w_up's
+    static constexpr int kWaves = WM * WN, kLoads = (BM + BN) / 8 / kWaves, kOut = KIND == kForward ? BN / 2 : BN;
+    int64_t m0, n0, outer_a, outer_b;
+    const T *corner_a, *corner_b, *corner_b2;  // corners of the tile's sides in memory
+    T *out;
+    uint32_t offset[kLoads];
+
+    __device__ __forceinline__ Place(const Product &p, int tile, int wave, int lane) {
+        const T *a = (const T *)p.a;
+        out = (T *)p.out;
+        if (KIND == kWeight && tile >= p.tiles_m * p.tiles_n) {
+            tile -= p.tiles_m * p.tiles_n;
+            a += p.turn;
+            out = (T *)p.out2;
+        }
+        const int across = tile / p.tiles_m;
+        m0 = (int64_t)(tile - across * p.tiles_m) * BM, n0 = (int64_t)across * kOut;
+        corner_a = KIND == kWeight ? a + m0 : a + m0 * p.a_ld;
+        corner_b = KIND == kForward ? (const T *)p.b + n0 * p.b_ld : (const T *)p.b + n0;
+        corner_b2 = KIND == kForward ? (const T *)p.b2 + n0 * p.b_ld : KIND == kInput ? (const T *)p.b2 + n0 : nullptr;
+        outer_a = p.a_outer - m0, outer_b = p.b_outer - n0;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int chunk = i * kWaves + wave;
+            offset[i] = i * kWaves < A::kChunks ? A::offset(chunk, lane, outer_a, p.a_ld)
+                                                : B::offset((chunk - A::kChunks) % B::kChunks, lane, outer_b, p.b_ld);
+        }
+    }
+};
+
+// A block a tile: while its results drain the next block on the compute unit is at its loads already.  (Blocks that stay
+// and send the next tile's first steps before they store were 2 % slower on 8192 x 4096 x 10944: loads are counted
+// off behind the stores, so the first steps wait for all of them.)
 template <typename T, int BM, int BN, int WM, int WN, Kind KIND, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     using frag = typename Frag<T>::type;
-    using A = Side<T, BM, KIND == kWeight>;
-    using B = Side<T, KIND == kForward ? BN / 2 : BN, KIND != kForward>;  // kForward: two sides, w_gate's and w_up's
-    constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32, kBytes = (BM + BN) * 64;
-    constexpr int kLoads = (BM + BN) / 16 / kWaves, kOut = KIND == kForward ? BN / 2 : BN;
-    static_assert((BM + BN) / 16 % kWaves == 0 && STAGES >= 3, "");
+    using Pl = Place<T, BM, BN, WM, WN, KIND>;
+    using A = typename Pl::A;
+    using B = typename Pl::B;
+    constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32, kBytes = (BM + BN) * 128, kLoads = Pl::kLoads;
+    constexpr int kWide = (KIND == kForward ? FN / 2 : FN) * 32;  // outputs of a wave across
+    static_assert(A::kChunks % kWaves == 0 && B::kChunks % kWaves == 0 && (kWide == 32 || kWide == 64) && STAGES >= 2 && STAGES * kLoads < 64, "");
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN, wn = wave % WN;
-    int tile = blockIdx.x;
-    const T *a = (const T *)p.a;
-    T *out = (T *)p.out;
-    if (KIND == kWeight && tile >= p.tiles_m * p.tiles_n) {
-        tile -= p.tiles_m * p.tiles_n;
-        a += p.turn;
-        out = (T *)p.out2;
-    }
-    const int64_t m0 = (int64_t)(tile % p.tiles_m) * BM, n0 = (int64_t)(tile / p.tiles_m) * kOut;
-    // corners of the tile's sides in memory, and what a step moves them by
-    const T *corner_a = KIND == kWeight ? a + m0 : a + m0 * p.a_ld;
-    const T *corner_b = KIND == kForward ? (const T *)p.b + n0 * p.b_ld : (const T *)p.b + n0;
-    const T *corner_b2 = KIND == kForward ? (const T *)p.b2 + n0 * p.b_ld : KIND == kInput ? (const T *)p.b2 + n0 : nullptr;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    char *const scratch = lds + STAGES * kBytes + wave * 4096;  // this wave's, for turning results
     const int64_t move_a = KIND == kWeight ? kStep * p.a_ld : kStep, move_b = KIND == kForward ? kStep : kStep * p.b_ld;
-    const int64_t outer_a = p.a_outer - m0, outer_b = p.b_outer - n0;
-
-    uint32_t offset[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; i++) {
-        const int chunk = i * kWaves + wave;
-        offset[i] = chunk < A::kChunks ? A::offset(chunk, lane, outer_a, p.a_ld)
-                                       : B::offset((chunk - A::kChunks) % B::kChunks, lane, outer_b, p.b_ld);
-    }
     // kInput: steps of w_gate, then of w_up; `turn` is a multiple of the step
     const int steps = (int)((p.k + kStep - 1) / kStep), turn = KIND == kInput ? (int)(p.turn / kStep) : steps;
-    auto corner_of_b = [&](int t) { return KIND == kInput && t >= turn ? corner_b2 + (t - turn) * move_b : corner_b + t * move_b; };
+    // whole steps go from memory to LDS without registers
+    const int whole = !p.direct ? 0 : (int)((KIND == kInput ? p.k - p.turn : p.k) / kStep);
+    auto is_direct = [&](int t) { return t < steps && (t >= turn ? t - turn : t) < whole; };
     // values of k that step t has
     auto values = [&](int t) -> int64_t {
         if (KIND == kInput) return std::min<int64_t>(kStep, std::max<int64_t>(0, p.k - p.turn - (int64_t)(t >= turn ? t - turn : t) * kStep));
         return std::min<int64_t>(kStep, p.k - (int64_t)t * kStep);
-    };
-    // whole steps from memory to LDS without registers
-    const int whole = !p.direct ? 0 : (int)((KIND == kInput ? p.k - p.turn : p.k) / kStep);
-    auto is_direct = [&](int t) { return t < steps && (t >= turn ? t - turn : t) < whole; };
-    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    auto load_direct = [&](int t) {
-        const T *at_a = corner_a + t * move_a, *at_b = corner_of_b(t), *at_b2 = corner_b2 + (KIND == kForward ? t * move_b : 0);
-        const uint32_t to = lds_at + t % STAGES * kBytes;
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int chunk = i * kWaves + wave;
-            const T *at = chunk < A::kChunks ? at_a : KIND == kForward && chunk >= A::kChunks + B::kChunks ? at_b2 : at_b;
-            load_to_lds((const char *)at + offset[i], to + chunk * 1024);
-        }
-    };
-    auto load = [&](int t) {
-        if (is_direct(t)) {
-            load_direct(t);
-        } else if (t < steps) {
-            const T *at_a = corner_a + t * move_a, *at_b = corner_of_b(t);
-            char *to = lds + t % STAGES * kBytes;
-            const int64_t ks = values(t);
-            for (int i = threadIdx.x; i < BM * 4; i += kWaves * 64) A::copy_piece(at_a, p.a_ld, outer_a, ks, i, to);
-            for (int i = threadIdx.x; i < BN * 4; i += kWaves * 64) {
-                const bool second = KIND == kForward && i >= BN * 2;
-                B::copy_piece(second ? corner_b2 + t * move_b : at_b, p.b_ld, outer_b, ks, second ? i - BN * 2 : i,
-                              to + BM * 64 + (second ? BN * 32 : 0));
-            }
-        }
     };
     int place_a[FM], place_b[FN];
 #pragma unroll
     for (int i = 0; i < FM; i++) place_a[i] = A::fragment((wm * FM + i) * 32, lane);
 #pragma unroll
     for (int j = 0; j < FN; j++)
-        place_b[j] = BM * 64 + (KIND == kForward ? j % 2 * (BN * 32) + B::fragment((wn * (FN / 2) + j / 2) * 32, lane)
-                                                 : B::fragment((wn * FN + j) * 32, lane));
-    auto read = [&](frag(&fa)[FM], frag(&fb)[FN], int t, int half) {
-        const char *at = lds + t % STAGES * kBytes;
+        place_b[j] = BM * 128 + (KIND == kForward ? j % 2 * (BN * 64) + B::fragment((wn * (FN / 2) + j / 2) * 32, lane)
+                                                  : B::fragment((wn * FN + j) * 32, lane));
+    const Pl at(p, blockIdx.x, wave, lane);
+    // Addresses of this thread's loads of a step; which operand a load is of goes by its number, for all waves.
+    const T *from[kLoads];
+    auto address = [&](int t) {
+        const T *at_a = at.corner_a + t * move_a;
+        const T *at_b = KIND == kInput && t >= turn ? at.corner_b2 + (t - turn) * move_b : at.corner_b + t * move_b;
+        const T *at_b2 = KIND == kForward ? at.corner_b2 + t * move_b : nullptr;
 #pragma unroll
-        for (int i = 0; i < FM; i++) fa[i] = A::read(at, place_a[i], half);
+        for (int i = 0; i < kLoads; i++)
+            from[i] = (const T *)((const char *)(i * kWaves < A::kChunks ? at_a
+                                                 : KIND == kForward && i * kWaves >= A::kChunks + B::kChunks ? at_b2 : at_b) +
+                                  at.offset[i]);
+    };
+    auto load_direct = [&](int t) {
+        const uint32_t to = lds_at + t % STAGES * kBytes;
 #pragma unroll
-        for (int j = 0; j < FN; j++) fb[j] = B::read(at, place_b[j], half);
+        for (int i = 0; i < kLoads; i++) load_to_lds(from[i], to + (i * kWaves + wave) * 1024);
+    };
+    auto load = [&](int t) {
+        if (is_direct(t)) {
+            address(t);
+            load_direct(t);
+        } else if (t < steps) {
+            const T *at_a = at.corner_a + t * move_a;
+            const T *at_b = KIND == kInput && t >= turn ? at.corner_b2 + (t - turn) * move_b : at.corner_b + t * move_b;
+            char *to = lds + t % STAGES * kBytes;
+            const int64_t ks = values(t);
+            const int thread = afresh(threadIdx.x);
+#pragma unroll 1
+            for (int i = thread; i < BM * 8; i += kWaves * 64) A::copy_piece(at_a, p.a_ld, at.outer_a, ks, i, to);
+#pragma unroll 1
+            for (int i = thread; i < BN * 8; i += kWaves * 64) {
+                const bool second = KIND == kForward && i >= BN * 4;
+                B::copy_piece(second ? at.corner_b2 + t * move_b : at_b, p.b_ld, at.outer_b, ks, second ? i - BN * 4 : i,
+                              to + BM * 128 + (second ? BN * 64 : 0));
+            }
+        }
+    };
+    auto read = [&](frag(&fa)[FM], frag(&fb)[FN], int t, int quarter) {
+        const char *from = lds + t % STAGES * kBytes;
+#pragma unroll
+        for (int i = 0; i < FM; i++) fa[i] = A::read(from, place_a[i], quarter);
+#pragma unroll
+        for (int j = 0; j < FN; j++) fb[j] = B::read(from, place_b[j], quarter);
     };
     f32x16 acc[FM][FN] = {};
     auto multiply = [&](frag(&fa)[FM], frag(&fb)[FN]) {
 #pragma unroll
         for (int i = 0; i < FM; i++)
 #pragma unroll
-            for (int j = 0; j < FN; j++) acc[i][j] = mma32(fa[i], fb[j], acc[i][j]);
+            for (int j = 0; j < FN; j++) acc[i][j] = mma32(fb[j], fa[i], acc[i][j]);
     };
-    // Steps t + 1 .. t + STAGES - 1 are on their way while step t is multiplied, and fragments are read half a step ahead:
-    // two sets of registers.  Before half a step is multiplied, the reads that its fragments came by are
-    // waited for; before the second half also step t + 1's loads, then a barrier: step t + 1 is there for
-    // everybody, and everybody has read step t - 1, whose place the next load takes.
     auto barrier = [&] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    auto done_reading = [&] { __builtin_amdgcn_s_waitcnt(0xC07F); };  // lgkmcnt(0)
+    auto keep_order = [&] { __builtin_amdgcn_sched_barrier(0); };
+
     frag a0[FM], b0[FN], a1[FM], b1[FN];
-    auto step = [&](int t, auto fast) {  // fast: steps t + 2 .. t + STAGES - 1 are there and direct
-        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-        __builtin_amdgcn_sched_barrier(0);
-        read(a1, b1, t, 1);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(a0, b0);
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0xC07F);
-        if constexpr (fast.value)
-            asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 3) * kLoads) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        barrier();
+    // Fragments are read a quarter of a step ahead, into two sets of registers, and a quarter's own reads are waited for
+    // before the next are sent.  Before the last quarter everybody's reads of step t are done and step t + 1 is
+    // there (its loads were sent STAGES - 1 steps ago): one barrier, then step t + STAGES is sent to step t's place.
+    auto step = [&](int t, auto fast) {  // fast: steps up to t + STAGES are there and direct
+        done_reading(), keep_order();
+        read(a1, b1, t, 1), keep_order();
+        multiply(a0, b0), keep_order();
+        done_reading(), keep_order();
+        read(a0, b0, t, 2), keep_order();
+        multiply(a1, b1), keep_order();
+        done_reading(), keep_order();
+        read(a1, b1, t, 3), keep_order();
+        multiply(a0, b0), keep_order();
+        done_reading();
         if constexpr (fast.value) {
-            load_direct(t + STAGES - 1);
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 2) * kLoads) : "memory");
+            barrier();
+            load_direct(t + STAGES);
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) from[i] += i * kWaves < A::kChunks ? move_a : move_b;
             read(a0, b0, t + 1, 0);
         } else {
-            load(t + STAGES - 1);
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+            barrier();
+            load(t + STAGES);
             if (t + 1 < steps) read(a0, b0, t + 1, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(a1, b1);
-        __builtin_amdgcn_sched_barrier(0);
+        keep_order();
+        multiply(a1, b1), keep_order();
     };
-    // end of the fast steps that t is among
+    // end of the fast steps that t is among: those behind t that are counted off are direct, too, and their loads
+    // move on in one operand
     auto fast_end = [&](int t) {
-        if (KIND == kInput && whole == turn) return 2 * whole - (STAGES - 1);
-        return (KIND == kInput && t + 2 >= turn ? turn : 0) + whole - (STAGES - 1);
+        if (KIND != kInput || t + STAGES < turn) return whole - STAGES;
+        return whole == turn || t + 2 >= turn ? turn + whole - STAGES : t;
     };
     if (steps > 0) {
-        for (int t = 0; t < STAGES - 1; t++) load(t);
-        __builtin_amdgcn_s_waitcnt(0xC07F);
-        if (whole >= STAGES - 1)
-            asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 2) * kLoads) : "memory");
+        for (int t = 0; t < STAGES; t++) load(t);
+        done_reading();
+        if (whole >= STAGES)
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 1) * kLoads) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         barrier();
         read(a0, b0, 0, 0);
         for (int t = 0; t < steps;) {
-            for (const int end = fast_end(t); t < end; t++) step(t, std::true_type{});
+            const int end = fast_end(t);
+            if (t < end) address(t + STAGES);
+            for (; t < end; t++) step(t, std::true_type{});
             if (t < steps) step(t++, std::false_type{});
         }
     }
-    // a lane holds one column and, of a fragment, rows 8 * (r / 4) + 4 * (lane / 32) + r % 4
-    auto each = [&](auto fn) {
+    const int64_t m0 = at.m0 + wm * FM * 32, n0 = at.n0 + wn * kWide;
+    T *const out = at.out;
+    // Results: of a fragment, lane l holds row l % 32 and columns 8 (r / 4) + 4 (l / 32) + r % 4.  32 rows at a time
+    // go through the wave's scratch, where a row's pieces of 16 bytes are exchanged as above, and out in rows.
+    const bool full = m0 + FM * 32 <= p.m && n0 + kWide <= p.n;
+    const int own = afresh(lane), row = own % 32, high = own / 32;
+    auto exchange = [&](int bytes) { return bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
+    auto flush = [&](auto type, int i, auto bytes_, auto *to, int64_t ld, bool wide) {
+        // rows of bytes_ bytes from the scratch to memory
+        asm volatile("" ::: "memory");
+        using U = decltype(type);
+        constexpr int bytes = bytes_.value, pieces = bytes / 16, per = 16 / sizeof(U);
 #pragma unroll
-        for (int i = 0; i < FM; i++)
+        for (int c = 0; c < 32 * pieces / 64; c++) {
+            const int r = c * (64 / pieces) + own / pieces, piece = own % pieces;
+            const int turned = piece ^ (bytes == 128 ? (r >> 1) & 7 : (r >> 2) & 3);
+            const Pack<U, per> v = *(const Pack<U, per> *)(scratch + r * bytes + turned * 16);
+            U *at_row = to + (m0 + i * 32 + r) * ld + n0 + piece * per;
+            if (full && wide) {
+                *(Pack<U, per> *)at_row = v;
+            } else if (m0 + i * 32 + r < p.m) {
+                const int64_t left = p.n - n0 - piece * per;
+                if (wide && left >= per) {
+                    *(Pack<U, per> *)at_row = v;
+                } else {
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int64_t row = m0 + (wm * FM + i) * 32 + (r / 4) * 8 + (lane / 32) * 4 + r % 4;
-                if (row < p.m) fn(i, r, row);
+                    for (int e = 0; e < per; e++)
+                        if (e < left) at_row[e] = v.v[e];
+                }
             }
+        }
+        asm volatile("" ::: "memory");
     };
-    if constexpr (KIND == kForward) {
-        with_act(p.act, [&](auto act) {
-            each([&](int i, int r, int64_t row) {
+    constexpr std::integral_constant<int, kWide * 2> out_bytes{};
+    with_act(KIND == kForward ? p.act : BYZ_ACT_NONE, [&](auto act) {
 #pragma unroll
-                for (int j = 0; j < FN; j += 2) {
-                    const int64_t col = n0 + (wn * (FN / 2) + j / 2) * 32 + lane % 32;
-                    if (col >= p.n) continue;
-                    const float g = acc[i][j][r], u = acc[i][j + 1][r];
-                    out[row * p.out_ld + col] = round_to<T>(act_value<act.value>(g) * u);
-                    if (p.gate) {
-                        p.gate[row * p.gate_ld + col] = g;
-                        p.up[row * p.gate_ld + col] = u;
+        for (int i = 0; i < FM; i++) {
+#pragma unroll
+            for (int j = 0; j < FN; j += KIND == kForward ? 2 : 1)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    Pack<T, 4> v;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const float x = acc[i][j][g * 4 + e];
+                        if constexpr (KIND == kForward)
+                            v.v[e] = round_to<T>(act_value<act.value>(x) * acc[i][j + 1][g * 4 + e]);
+                        else
+                            v.v[e] = round_to<T>(x);
+                    }
+                    const int piece = (KIND == kForward ? j / 2 : j) * 4 + g;
+                    *(Pack<T, 4> *)(scratch + row * out_bytes.value + (piece ^ exchange(out_bytes.value)) * 16 + high * 8) = v;
+                }
+            flush(T{}, i, out_bytes, out, p.out_ld, p.out_wide);
+            if constexpr (KIND == kForward)
+                if (p.gate) {
+#pragma unroll
+                    for (int j = 0; j < FN; j++) {
+#pragma unroll
+                        for (int g = 0; g < 4; g++) {
+                            Pack<float, 4> v;
+#pragma unroll
+                            for (int e = 0; e < 4; e++) v.v[e] = acc[i][j][g * 4 + e];
+                            *(Pack<float, 4> *)(scratch + row * 128 + ((g * 2 + high) ^ exchange(128)) * 16) = v;
+                        }
+                        flush(0.0f, i, std::integral_constant<int, 128>{}, (j % 2 ? p.up : p.gate) + j / 2 * 32, p.gate_ld, p.gate_wide);
                     }
                 }
-            });
-        });
-    } else {
-        each([&](int i, int r, int64_t row) {
-#pragma unroll
-            for (int j = 0; j < FN; j++) {
-                const int64_t col = n0 + (wn * FN + j) * 32 + lane % 32;
-                if (col < p.n) out[row * p.out_ld + col] = round_to<T>(acc[i][j][r]);
-            }
-        });
-    }
+        }
+    });
 }
 
 // Up to 16 tokens.  Block: 16 outputs, kSkinnyWaves shares of k.
@@ -448,16 +528,19 @@ unsigned grid_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads 
 
 template <typename T, int BM, int BN, int WM, int WN, Kind KIND, int STAGES>
 int launch_tile(Product p, hipStream_t s) {
-    constexpr int kOut = KIND == kForward ? BN / 2 : BN, kThreads = WM * WN * 64, kLds = STAGES * (BM + BN) * 64;
-    const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + kOut - 1) / kOut, blocks = tm * tn * (KIND == kWeight ? 2 : 1);
-    if (blocks > INT32_MAX / kThreads) return BYZ_EUNSUPPORTED;
+    constexpr int kOut = KIND == kForward ? BN / 2 : BN, kThreads = WM * WN * 64;
+    constexpr int kLds = STAGES * (BM + BN) * 128 + WM * WN * 4096;
+    const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + kOut - 1) / kOut, tiles = tm * tn * (KIND == kWeight ? 2 : 1);
+    if (tiles > INT32_MAX / kThreads) return BYZ_EUNSUPPORTED;
     p.tiles_m = (int)tm, p.tiles_n = (int)tn;
     // a lane's place in a tile's side is a 32-bit offset
     const int64_t most = INT32_MAX / (int64_t)sizeof(T);
     p.direct = (KIND == kWeight ? kStep : BM) * p.a_ld + BM < most && (KIND == kForward ? BN : kStep) * p.b_ld + BN < most;
+    p.out_wide = aligned(p.out, 16) && p.out_ld % 8 == 0 && (!p.out2 || aligned(p.out2, 16));
+    p.gate_wide = p.gate && aligned(p.gate, 16) && aligned(p.up, 16) && p.gate_ld % 4 == 0;
     auto *kernel = &product_kernel<T, BM, BN, WM, WN, KIND, STAGES>;
     BYZ_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
-    kernel<<<(unsigned)blocks, kThreads, kLds, s>>>(p);
+    kernel<<<(unsigned)tiles, kThreads, kLds, s>>>(p);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -467,9 +550,10 @@ template <typename T, Kind KIND>
 int launch_product(const Product &p, hipStream_t s) {
     const int64_t across = KIND == kInput ? p.n : 2 * p.n;
     auto tiles = [&](int bm, int bn) { return ((p.m + bm - 1) / bm) * ((across + bn - 1) / bn); };
-    if (tiles(256, 256) >= 192) return launch_tile<T, 256, 256, 2, 4, KIND, 4>(p, s);
-    if (tiles(128, 128) >= 192) return launch_tile<T, 128, 128, 2, 2, KIND, 4>(p, s);
-    return launch_tile<T, 64, 128, 2, 2, KIND, 4>(p, s);
+    if (tiles(256, 256) >= 192) return launch_tile<T, 256, 256, 2, 4, KIND, 2>(p, s);
+    if (tiles(128, 128) >= 192) return launch_tile<T, 128, 128, 2, 2, KIND, 2>(p, s);
+    if (KIND == kForward || tiles(64, 128) >= 192) return launch_tile<T, 64, 128, 2, 2, KIND, 2>(p, s);
+    if constexpr (KIND != kForward) return launch_tile<T, 64, 64, 2, 2, KIND, 4>(p, s);
 }
 
 int64_t padded(int64_t v) { return (v + 63) / 64 * 64; }
