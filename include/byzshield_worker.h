@@ -79,11 +79,9 @@ int byz_group_norm_backward(const void *dy, int64_t dy_sample, int64_t dy_pixel,
  * logit of -inf is a banned one: q = 0 there.  An index of vocab or more makes the row's loss NaN,
  * and its gradient.  lse may be NULL.  temperature > 0; 1 <= k <= BYZ_MAX_TEACHER.
  */
-size_t byz_distill_loss_workspace_bytes(int64_t rows, int64_t vocab, int k, int dtype);
 int byz_distill_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
                      const float *teacher, const int32_t *index, int k, int64_t teacher_ld,
-                     float temperature, float *loss, float *lse, void *workspace,
-                     size_t workspace_bytes, void *stream);
+                     float temperature, float *loss, float *lse, void *stream);
 
 /*
  * The gradient for dloss (one value a row), from the call's lse:
@@ -97,6 +95,7 @@ int byz_distill_loss_backward(const float *dloss, const void *logits, int64_t ro
 
 /* Loss and gradient in one call, for a dloss that is known beforehand (the weight of a row in a mean): the logits
  * are read once where a row fits a compute unit.  Same outputs as the two calls; lse may be NULL. */
+size_t byz_distill_loss_step_workspace_bytes(int64_t rows, int64_t vocab, int k, int dtype);
 int byz_distill_loss_step(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
                           const float *teacher, const int32_t *index, int k, int64_t teacher_ld,
                           const float *dloss, float temperature, float *loss, float *lse,

@@ -2,10 +2,15 @@
 //
 // A row's loss needs two sums: the teacher's softmax over its k entries, done in fp64 (a loss near 0 is a
 // difference of larger terms, and k values cost nothing next to the vocabulary), and the student's
-// log-sum-exp over the vocabulary: one pass with a running maximum m and a sum S of exp((s - m) / T) per
-// thread, joined over the row's threads in a fixed order.  The gradient is dense, dloss T q_v, with the
-// few places of the teacher's entries written again after it (each thread that owns an entry adds up all
-// p at its place, so entries at one place write one value).  Bound by memory: logits in, gradients out.
+// log-sum-exp over the vocabulary, joined over the row's threads in a fixed order.  The gradient is dense, dloss T q_v,
+// with the few places of the teacher's entries written again after it (each thread that owns an entry adds up all
+// p at its place, so entries at one place write one value).
+//
+// Bound by memory: logits in, gradients out.  Loss and gradient in one call hold a long row in registers ("resident"): it
+// is read once, and as soon as a thread has stored a piece of its gradient it loads that piece of its next row, so reads,
+// the two exponentials of a value and writes overlap although a row fills a compute unit's registers.  The fp64
+// functions would take those registers, so the teacher's softmax and the losses are kernels before and behind it.
+// Rows that are too long, short rows and the other calls stream: with a running maximum m and a sum of exp((s - m) / T).
 #include <algorithm>
 
 #include "worker_internal.h"
@@ -15,6 +20,7 @@ using namespace byz_worker;
 namespace {
 
 constexpr int64_t kMaxGrid = 1 << 20;
+constexpr int kCus = 256;  // compute units
 
 enum Mode { kLoss, kGradient, kStep };
 
@@ -57,69 +63,57 @@ struct RunningSum {
     }
 };
 
-// Reductions over the NT threads of a row: a butterfly in the wave, then the waves in order.  `lds` has room
-// for 2 * NT / 64 doubles.  Every thread gets the result.
-template <int NT>
-__device__ RunningSum row_join(RunningSum r, float c, double *lds) {
-    for (int off = 1; off < 64; off *= 2) {
-        // both sides of a pair join lower lane first and get the same bits
-        const float m2 = __shfl_xor(r.m, off), s2 = __shfl_xor(r.s, off);
-        RunningSum lo = r;
-        if (threadIdx.x & off) {
-            lo.m = m2, lo.s = s2;
-            lo.join(r.m, r.s, c);
-        } else {
-            lo.join(m2, s2, c);
-        }
+// Reductions over the NT threads of a row: a butterfly in the wave, then every wave does one over the waves' results.
+// `lds` has room for NT / 64 doubles.  Every thread gets the result.
+__device__ __forceinline__ RunningSum butterfly_join(RunningSum r, float c, int end) {
+    for (int off = 1; off < end; off *= 2) {
+        // both sides of a pair join the lower lane first and get the same bits
+        RunningSum other;
+        other.m = __shfl_xor(r.m, off), other.s = __shfl_xor(r.s, off);
+        const bool upper = threadIdx.x & off;
+        RunningSum lo = upper ? other : r;
+        const RunningSum hi = upper ? r : other;
+        lo.join(hi.m, hi.s, c);
         r = lo;
-    }
-    if constexpr (NT > 64) {
-        float *f = reinterpret_cast<float *>(lds);
-        __syncthreads();
-        if (threadIdx.x % 64 == 0) f[threadIdx.x / 64 * 2] = r.m, f[threadIdx.x / 64 * 2 + 1] = r.s;
-        __syncthreads();
-        RunningSum all;
-        for (int w = 0; w < NT / 64; w++) all.join(f[2 * w], f[2 * w + 1], c);
-        r = all;
     }
     return r;
 }
 
 template <int NT>
-__device__ double row_sum(double v, double *lds) {
-    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
+__device__ __forceinline__ RunningSum row_join(RunningSum r, float c, double *lds) {
+    r = butterfly_join(r, c, 64);
+    if constexpr (NT > 64) {
+        float *f = reinterpret_cast<float *>(lds);
+        const int from = threadIdx.x % (NT / 64);
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) f[threadIdx.x / 64 * 2] = r.m, f[threadIdx.x / 64 * 2 + 1] = r.s;
+        __syncthreads();
+        r.m = f[2 * from], r.s = f[2 * from + 1];
+        r = butterfly_join(r, c, NT / 64);
+    }
+    return r;
+}
+
+template <int NT, typename F>
+__device__ __forceinline__ double row_reduce(double v, double *lds, F join) {
+    for (int off = 32; off; off >>= 1) v = join(v, __shfl_xor(v, off));
     if constexpr (NT > 64) {
         __syncthreads();
         if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
         __syncthreads();
-        v = 0.0;
-        for (int w = 0; w < NT / 64; w++) v += lds[w];
+        v = lds[threadIdx.x % (NT / 64)];
+        for (int off = NT / 128; off; off >>= 1) v = join(v, __shfl_xor(v, off));
     }
     return v;
 }
-
 template <int NT>
-__device__ double row_max(double v, double *lds) {
-    for (int off = 32; off; off >>= 1) v = fmax(v, __shfl_xor(v, off));
-    if constexpr (NT > 64) {
-        __syncthreads();
-        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-        __syncthreads();
-        v = lds[0];
-        for (int w = 1; w < NT / 64; w++) v = fmax(v, lds[w]);
-    }
-    return v;
+__device__ __forceinline__ double row_sum(double v, double *lds) {
+    return row_reduce<NT>(v, lds, [](double a, double b) { return a + b; });
 }
-
-// A row's teacher in LDS: places, p, and the student's logits there.
-struct Teacher {
-    int32_t *index;
-    float *p, *student;
-    double top, total;
-    bool some;
-};
-
-size_t teacher_bytes(int k) { return ((size_t)k * 12 + 15) / 16 * 16; }
+template <int NT>
+__device__ __forceinline__ double row_max(double v, double *lds) {
+    return row_reduce<NT>(v, lds, [](double a, double b) { return fmax(a, b); });
+}
 
 // A row's vocabulary as 16-byte vectors between a few single elements on either side.
 template <typename T>
@@ -138,6 +132,108 @@ struct Row {
     __device__ int64_t edge(int t) const { return t < head ? t : vectors * V + t; }  // the t-th single element
 };
 
+// A row's teacher in LDS: places (-1: no entry), exp(z - top), p, and the student's logits there.
+struct Teacher {
+    double *weight;
+    int32_t *index;
+    float *p, *student;
+    double top, total;
+    bool some;  // an entry at all
+    __device__ Teacher(char *lds, int k) {
+        weight = (double *)lds, index = (int32_t *)(weight + k), p = (float *)(index + k), student = p + k;
+    }
+};
+
+constexpr int kTeacherBytes = 20;  // of an entry
+__host__ __device__ inline size_t teacher_bytes(int k) { return ((size_t)k * kTeacherBytes + 15) / 16 * 16; }
+
+// Softmax over the entries that are there; `at`: the student's row.  Starts with a barrier (of the row's threads).
+template <typename T, int NT>
+__device__ __forceinline__ void read_teacher(const Args &a, int64_t row, const T *at, Teacher &t, int tid, double *red) {
+    const double tau = a.temperature;
+    double top = -INFINITY, total = 0.0;
+    __syncthreads();
+#pragma unroll 1
+    for (int j = tid; j < a.k; j += NT) {
+        const int32_t i = a.index[row * a.teacher_ld + j];
+        const double z = (double)a.teacher[row * a.teacher_ld + j] / tau;
+        const bool in = i >= 0 && i < a.vocab;
+        if (in) top = fmax(top, z);
+        t.index[j] = in ? i : -1;
+        t.weight[j] = z;
+        t.student[j] = in ? (float)at[i] : 0.0f;
+        if (i >= a.vocab || (i >= 0 && z != z)) total = NAN;
+    }
+    t.top = row_max<NT>(top, red);
+    const double shift = t.top > -INFINITY ? t.top : 0.0;
+#pragma unroll 1
+    for (int j = tid; j < a.k; j += NT)
+        if (t.index[j] >= 0) total += t.weight[j] = exp(t.weight[j] - shift);
+    t.total = row_sum<NT>(total, red);
+    t.some = t.total > 0.0 || t.total != t.total;
+}
+
+// p, and the loss with the student's log-sum-exp lse
+template <int NT>
+__device__ __forceinline__ double loss_of(const Args &a, Teacher &t, double lse, int tid, double *red) {
+    const double tau = a.temperature;
+    double part = 0.0;
+#pragma unroll 1
+    for (int j = tid; j < a.k; j += NT) {
+        const double p = t.index[j] < 0 ? 0.0 : t.weight[j] / t.total;
+        t.p[j] = (float)p;
+        if (p > 0.0) part += p * (log(p) - ((double)t.student[j] / tau - lse));
+        if (p != p) part = NAN;
+    }
+    part = row_sum<NT>(part, red);
+    return !t.some ? 0.0 : t.total != t.total ? NAN : tau * tau * part;
+}
+
+// q_v times a weight, from a logit.  The exponent is (x - m) c - l, with c = log2(e) / T in two parts where the result is fp32.
+// The instruction's exp2 gives 0 below 2^-126, where a product with the weight still has a value: there the
+// exponent is raised by 32 and the product lowered by it.
+template <typename T>
+struct Softmax {
+    float m, c, c_low, l, w;
+    __device__ Softmax(double m_, double log_sum, double temperature, float weight) {
+        const double s = 1.4426950408889634 / temperature;
+        m = (float)m_, c = (float)s, c_low = (float)(s - (double)c), l = (float)(log_sum * 1.4426950408889634), w = weight;
+    }
+    // from a maximum and a sum in fp32; c is log2(e) / T
+    __device__ Softmax(float m_, float sum, float temperature, float weight, float c_) {
+        m = m_, c = c_, l = __builtin_amdgcn_logf(sum), w = weight;
+        // what c is short of: log2(e) = hi + lo, and the remainder of hi - c T
+        c_low = sizeof(T) == 4 ? (fmaf(-c, temperature, 0x1.715476p+0f) + 0x1.4ae0c0p-26f) / temperature : 0.0f;
+    }
+    __device__ __forceinline__ float weighted(float x) const { return less(x, 0.0f); }
+    // w (q - p)
+    __device__ __forceinline__ float less(float x, float p) const {
+        const float d = x - m;
+        if constexpr (sizeof(T) == 4) {
+            const float e = fmaf(d, c, fmaf(d, c_low, -l));
+            const bool low = e < -100.0f;
+            const float q = __builtin_amdgcn_exp2f(low ? e + 32.0f : e);
+            return low ? (q - p * 0x1p32f) * (w * 0x1p-32f) : (q - p) * w;
+        } else {
+            return (__builtin_amdgcn_exp2f(fmaf(d, c, 32.0f - l)) - p * 0x1p32f) * (w * 0x1p-32f);
+        }
+    }
+};
+
+// The gradient at the teacher's places; the dense part is written.
+template <typename T, int NT>
+__device__ __forceinline__ void write_places(const Args &a, const Teacher &t, const Softmax<T> &q, T *out, int tid) {
+#pragma unroll 1
+    for (int j = tid; j < a.k; j += NT) {
+        const int32_t i = t.index[j];
+        if (i < 0) continue;
+        float p = 0.0f;
+#pragma unroll 1
+        for (int l = 0; l < a.k; l++) p += t.index[l] == i ? t.p[l] : 0.0f;
+        out[i] = round_to<T>(q.less(t.student[j], p));
+    }
+}
+
 template <typename T, int NT, Mode MODE>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
     extern __shared__ char lds_raw[];
@@ -145,32 +241,14 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
     constexpr int V = 16 / sizeof(T), kRows = NT == 64 ? 4 : 1, kUnroll = 4;
     const int tid = threadIdx.x % NT, sub = threadIdx.x / NT;
     const double tau = a.temperature;
-    const float c = (float)(1.0 / tau * 1.4426950408889634);
-    Teacher t;
-    char *mine = lds_raw + sub * (((size_t)a.k * 12 + 15) / 16 * 16);
-    t.index = (int32_t *)mine, t.p = (float *)(t.index + a.k), t.student = t.p + a.k;
+    const float c = (float)(1.4426950408889634 / tau);
+    Teacher t(lds_raw + sub * teacher_bytes(a.k), a.k);
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
         // a wave whose row lies behind the last works on the last one again and writes nothing
         const bool there = row0 + sub < a.rows;
         const int64_t row = there ? row0 + sub : a.rows - 1;
         const Row<T> r(a.logits, row, a.ld, a.vocab);
-        __syncthreads();
-        // teacher: softmax over the entries that are there
-        double top = -INFINITY, total = 0.0;
-        for (int j = tid; j < a.k; j += NT) {
-            const int32_t i = a.index[row * a.teacher_ld + j];
-            const double z = (double)a.teacher[row * a.teacher_ld + j] / tau;
-            if (i >= 0 && i < a.vocab) top = fmax(top, z);
-            t.index[j] = i < a.vocab ? i : -1;
-            t.student[j] = i >= 0 && i < a.vocab ? (float)r.at[i] : 0.0f;
-            if (i >= a.vocab || (i >= 0 && z != z)) total = NAN;
-        }
-        top = row_max<NT>(top, red);
-        const double shift = top > -INFINITY ? top : 0.0;
-        for (int j = tid; j < a.k; j += NT)
-            if (t.index[j] >= 0) total += exp((double)a.teacher[row * a.teacher_ld + j] / tau - shift);
-        total = row_sum<NT>(total, red);
-        t.some = total > 0.0 || total != total;
+        read_teacher<T, NT>(a, row, r.at, t, tid, red);
         double m, log_sum;  // the student's log-sum-exp is m / tau + log_sum
         if constexpr (MODE != kGradient) {
             RunningSum s;
@@ -178,82 +256,231 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
                 const float x[1] = {(float)r.at[r.edge(tid)]};
                 s.add(x, c);
             }
-            const Pack<T, V> *at = (const Pack<T, V> *)(r.at + r.head);
+            const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
             int64_t i = tid;
             for (; i + (kUnroll - 1) * NT < r.vectors; i += kUnroll * NT) {
-                Pack<T, V> v[kUnroll];
+                Words<T, V> v[kUnroll];
 #pragma unroll
                 for (int u = 0; u < kUnroll; u++) v[u] = at[i + u * NT];
 #pragma unroll
                 for (int u = 0; u < kUnroll; u++) {
                     float x[V];
 #pragma unroll
-                    for (int e = 0; e < V; e++) x[e] = (float)v[u].v[e];
+                    for (int e = 0; e < V; e++) x[e] = v[u][e];
                     s.add(x, c);
                 }
             }
             for (; i < r.vectors; i += NT) {
-                const Pack<T, V> v = at[i];
+                const Words<T, V> v = at[i];
                 float x[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) x[e] = (float)v.v[e];
+                for (int e = 0; e < V; e++) x[e] = v[e];
                 s.add(x, c);
             }
             s = row_join<NT>(s, c, red);
             m = s.m, log_sum = log((double)s.s);
-            double part = 0.0;
-            for (int j = tid; j < a.k; j += NT) {
-                const double p = t.index[j] < 0 ? 0.0 : exp((double)a.teacher[row * a.teacher_ld + j] / tau - shift) / total;
-                t.p[j] = (float)p;
-                if (p > 0.0) part += p * (log(p) - (((double)t.student[j] - m) / tau - log_sum));
-                if (p != p) part = NAN;
-            }
-            part = row_sum<NT>(part, red);
+            const double loss = loss_of<NT>(a, t, m / tau + log_sum, tid, red);
             if (there && tid == 0) {
-                a.loss[row] = t.some ? (total != total ? NAN : (float)(tau * tau * part)) : 0.0f;
+                a.loss[row] = (float)loss;
                 if (a.lse) a.lse[row] = (float)(m / tau + log_sum);
             }
         } else {
             m = 0.0, log_sum = a.lse[row];
-            for (int j = tid; j < a.k; j += NT)
-                t.p[j] = t.index[j] < 0 ? 0.0f : (float)(exp((double)a.teacher[row * a.teacher_ld + j] / tau - shift) / total);
+        #pragma unroll 1
+    for (int j = tid; j < a.k; j += NT) t.p[j] = t.index[j] < 0 ? 0.0f : (float)(t.weight[j] / t.total);
         }
         if constexpr (MODE != kLoss) {
-            // q is taken times 2^32 and the weight times 2^-32: the instruction's exp2 gives 0 below 2^-126, where
-            // a product with the weight still has a value
-            const float w = total != total ? NAN : a.temperature * a.dloss[row] * 0x1p-32f;
-            const float m0 = (float)m, ls = (float)(log_sum * 1.4426950408889634) - 32.0f;
-            auto q = [&](float x) { return __builtin_amdgcn_exp2f((x - m0) * c - ls); };
+            const Softmax<T> q(m, log_sum, tau, t.total != t.total ? NAN : a.temperature * a.dloss[row]);
             T *out = (T *)a.dlogits + row * a.dlogits_ld;
             const bool pieces = (((uintptr_t)out ^ (uintptr_t)r.at) & 15) == 0;
             __syncthreads();  // the logits at the teacher's places are read: they may be written now
             if (there && tid < r.head + r.tail) {
                 const int64_t e = r.edge(tid);
-                out[e] = t.some ? round_to<T>(w * q((float)r.at[e])) : (T)0.0f;
+                out[e] = t.some ? round_to<T>(q.weighted((float)r.at[e])) : (T)0.0f;
             }
-            const Pack<T, V> *at = (const Pack<T, V> *)(r.at + r.head);
+            const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
             for (int64_t i = tid; there && i < r.vectors; i += NT) {
-                const Pack<T, V> v = at[i];
-                Pack<T, V> d;
-#pragma unroll
-                for (int e = 0; e < V; e++) d.v[e] = t.some ? round_to<T>(w * q((float)v.v[e])) : (T)0.0f;
+                const Words<T, V> v = at[i];
+                const Words<T, V> d = Words<T, V>::of([&](int e) { return t.some ? q.weighted(v[e]) : 0.0f; });
                 if (pieces) {
-                    ((Pack<T, V> *)(out + r.head))[i] = d;
+                    ((Words<T, V> *)(out + r.head))[i] = d;
                 } else {
 #pragma unroll
-                    for (int e = 0; e < V; e++) out[r.head + i * V + e] = d.v[e];
+                    for (int e = 0; e < V; e++) out[r.head + i * V + e] = round_to<T>(d[e]);
                 }
             }
             __syncthreads();  // the dense part is written: the teacher's places again
-            if (there && t.some)
-                for (int j = tid; j < a.k; j += NT) {
-                    const int32_t i = t.index[j];
-                    if (i < 0) continue;
-                    float p = 0.0f;
-                    for (int l = 0; l < a.k; l++) p += t.index[l] == i ? t.p[l] : 0.0f;
-                    out[i] = round_to<T>(w * (q(t.student[j]) - p * 0x1p32f));
-                }
+            if (there && t.some) write_places<T, NT>(a, t, q, out, tid);
         }
+    }
+}
+
+// A row's part of the workspace of the resident kernel, beside its p (k doubles).
+struct RowSums {
+    double entropy;  // sum of p log p
+    double dot, ps;  // sums of p s and p over the places
+    float m, s;      // the student's maximum and sum
+    int flags;       // kSome: an entry at all; kBroken: the row is NaN
+    int pad;
+};
+enum { kSome = 1, kBroken = 2 };
+
+// The teacher's softmax, a wave a row.
+__global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, double *p, RowSums *sums) {
+    const double tau = a.temperature;
+    const int lane = threadIdx.x % 64;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
+        const float *t = a.teacher + row * a.teacher_ld;
+        const int32_t *index = a.index + row * a.teacher_ld;
+        double top = -INFINITY, total = 0.0, entropy = 0.0;
+        bool broken = false;
+        for (int j = lane; j < a.k; j += 64)
+            if (index[j] >= 0) {
+                const double z = (double)t[j] / tau;
+                top = fmax(top, z);
+                broken = broken || z != z || index[j] >= a.vocab;
+            }
+        top = row_max<64>(top, nullptr);
+        const double shift = top > -INFINITY ? top : 0.0;
+        for (int j = lane; j < a.k; j += 64)
+            if (index[j] >= 0) total += exp((double)t[j] / tau - shift);
+        total = row_sum<64>(total, nullptr);
+        broken = __ballot(broken) != 0 || total != total;
+        const bool some = total > 0.0 || broken;
+        for (int j = lane; j < a.k; j += 64) {
+            const double w = index[j] < 0 || !some ? 0.0 : broken ? NAN : exp((double)t[j] / tau - shift) / total;
+            p[row * a.k + j] = w;
+            if (w > 0.0) entropy += w * log(w);
+        }
+        entropy = row_sum<64>(entropy, nullptr);
+        if (lane == 0) sums[row].entropy = entropy, sums[row].flags = (some ? kSome : 0) | (broken ? kBroken : 0);
+    }
+}
+
+__global__ __launch_bounds__(256) void distill_losses_kernel(Args a, const RowSums *sums) {
+    const double tau = a.temperature;
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= a.rows) return;
+    const RowSums r = sums[row];
+    const double lse = (double)r.m / tau + log((double)r.s);
+    a.loss[row] = r.flags & kBroken ? NAN : r.flags & kSome ? (float)(tau * tau * (r.entropy - r.dot / tau + r.ps * lse)) : 0.0f;
+    if (a.lse) a.lse[row] = (float)lse;
+}
+
+// The gradients, and the sums for the losses.  R vectors of a row in each of 1024 threads' registers; for rows whose logits
+// and gradients lie at the same place within 16 bytes.
+template <typename T, int R>
+__global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, const double *p, RowSums *sums) {
+    constexpr int V = 16 / sizeof(T), NT = 1024;
+    extern __shared__ char lds_raw[];
+    __shared__ double red[32];
+    const int tid = threadIdx.x;
+    const float c = (float)(1.4426950408889634 / (double)a.temperature);
+    Teacher t(lds_raw, a.k);
+    Words<T, V> x[R];
+    T edge = (T)0.0f;
+    // A row here is shorter than 2^31 bytes.  A thread's number `own` is made afresh for each use, or the places of all R
+    // vectors would be kept in registers; threads without a v-th vector load the last, without a branch, and leave it.
+    auto vector_of = [](const T *base, int number) { return (Words<T, V> *)((char *)base + (uint32_t)number * 16u); };
+    auto load = [&](const Row<T> &r, int own, int v) {
+        x[v] = *vector_of(r.at + r.head, std::min(own + v * NT, (int)r.vectors - 1));
+    };
+    auto load_edge = [&](const Row<T> &r) {
+        if (tid < r.head + r.tail) edge = r.at[r.edge(tid)];
+    };
+    {
+        const Row<T> r(a.logits, blockIdx.x, a.ld, a.vocab);
+#pragma unroll
+        for (int v = 0; v < R; v++) load(r, tid, v);
+        load_edge(r);
+    }
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const Row<T> r(a.logits, row, a.ld, a.vocab);
+        __syncthreads();  // the last row's places are written
+        double dot = 0.0, ps = 0.0;
+#pragma unroll 1
+        for (int j = tid; j < a.k; j += NT) {
+            const int32_t i = a.index[row * a.teacher_ld + j];
+            const double w = p[row * a.k + j];
+            const bool in = i >= 0 && i < a.vocab;
+            const float s = in ? (float)r.at[i] : 0.0f;
+            t.index[j] = in ? i : -1, t.p[j] = (float)w, t.student[j] = s;
+            if (w > 0.0) dot += w * (double)s, ps += w;
+        }
+        // A thread's sum of exp2((x - m) c).  The maximum of its first values is m: a sum in fp32 holds values up to
+        // 2^127 times that.  What goes beyond (or is not finite) is summed again with a running maximum.
+        const bool has_edge = tid < r.head + r.tail;
+        RunningSum s;
+        if (tid < r.vectors) {
+            float top = x[0][0];
+#pragma unroll
+            for (int e = 1; e < V; e++) top = fmaxf(top, x[0][e]);
+            s.m = top;
+        } else if (has_edge) {
+            s.m = (float)edge;
+        }
+        const float m0 = s.m;
+        const int vectors = (int)r.vectors, own = afresh(tid);
+#pragma unroll
+        for (int v = 0; v < R; v++) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < V; e++) sum += __builtin_amdgcn_exp2f((x[v][e] - m0) * c);
+            s.s += own + v * NT < vectors ? sum : 0.0f;
+            x[v].keep();
+            __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
+        }
+        if (has_edge) s.s += __builtin_amdgcn_exp2f(((float)edge - m0) * c);
+        if (!(s.s < 0x1p120f)) {
+            s = RunningSum();
+#pragma unroll
+            for (int v = 0; v < R; v++) {
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; e++) y[e] = own + v * NT < vectors ? x[v][e] : -INFINITY;
+                s.add(y, c);
+                x[v].keep();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (has_edge) {
+                const float y[1] = {(float)edge};
+                s.add(y, c);
+            }
+        }
+        s = row_join<NT>(s, c, red);
+        dot = row_sum<NT>(dot, red);
+        ps = row_sum<NT>(ps, red);
+        const int flags = sums[row].flags;
+        if (tid == 0) sums[row].dot = dot, sums[row].ps = ps, sums[row].m = s.m, sums[row].s = s.s;
+        const bool some = flags & kSome;
+        const Softmax<T> q(s.m, s.s, a.temperature, flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
+        T *out = (T *)a.dlogits + row * a.dlogits_ld;
+        // here everybody has read the logits at the teacher's places (the barriers of the sums): they may be written
+        if (has_edge) {
+            const int64_t e = r.edge(tid);
+            out[e] = some ? round_to<T>(q.weighted((float)edge)) : (T)0.0f;
+        }
+        const int then = afresh(tid);
+        auto store = [&](int v) {
+            if (then + v * NT < vectors)
+                *vector_of(out + r.head, then + v * NT) = Words<T, V>::of([&](int e) { return some ? q.weighted(x[v][e]) : 0.0f; });
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (row + gridDim.x < a.rows) {
+            const Row<T> next(a.logits, row + gridDim.x, a.ld, a.vocab);
+            load_edge(next);
+#pragma unroll
+            for (int v = 0; v < R; v++) {
+                store(v);
+                load(next, then, v);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < R; v++) store(v);
+        }
+        __syncthreads();  // the dense part is written: the teacher's places again
+        if (some) write_places<T, NT>(a, t, q, out, tid);
     }
 }
 
@@ -262,6 +489,32 @@ int launch_threads(const Args &a, hipStream_t s) {
     constexpr int rows = NT == 64 ? 4 : 1;
     const int64_t blocks = (a.rows + rows - 1) / rows;
     distill_kernel<T, NT, MODE><<<(unsigned)std::min(blocks, kMaxGrid), NT == 64 ? 256 : NT, rows * teacher_bytes(a.k), s>>>(a);
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+// Rows that the resident kernel takes: their threads' vectors fit, and there is one for every compute unit.
+constexpr int kResident = 16;  // vectors of a thread
+bool fits_resident(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t vectors = vocab * (int64_t)dtype_size(dtype) / 16;
+    return vectors >= 1024 * 4 && vectors <= 1024 * kResident && rows >= kCus / 2;
+}
+
+size_t resident_bytes(int64_t rows, int k) { return (size_t)rows * (sizeof(RowSums) + (size_t)k * sizeof(double)); }
+
+template <typename T>
+int launch_resident(const Args &a, void *workspace, hipStream_t s) {
+    RowSums *sums = (RowSums *)workspace;
+    double *p = (double *)(sums + a.rows);
+    distill_teacher_kernel<<<(unsigned)std::min<int64_t>((a.rows + 3) / 4, kMaxGrid), 256, 0, s>>>(a, p, sums);
+    BYZ_HIP(hipGetLastError());
+    const unsigned grid = (unsigned)std::min<int64_t>(a.rows, kCus);
+    if (a.vocab * (int64_t)sizeof(T) / 16 <= 1024 * kResident / 2)
+        distill_resident_kernel<T, kResident / 2><<<grid, 1024, teacher_bytes(a.k), s>>>(a, p, sums);
+    else
+        distill_resident_kernel<T, kResident><<<grid, 1024, teacher_bytes(a.k), s>>>(a, p, sums);
+    BYZ_HIP(hipGetLastError());
+    distill_losses_kernel<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, sums);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -304,12 +557,13 @@ int check_gradient(const Args &a, int dtype) {
 
 }  // namespace
 
-extern "C" size_t byz_distill_loss_workspace_bytes(int64_t rows, int64_t vocab, int k, int dtype) { return 0; }
+extern "C" size_t byz_distill_loss_step_workspace_bytes(int64_t rows, int64_t vocab, int k, int dtype) {
+    return sizes_ok(rows, vocab, k, dtype) && fits_resident(rows, vocab, dtype) ? resident_bytes(rows, k) : 0;
+}
 
 extern "C" int byz_distill_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
                                 const float *teacher, const int32_t *index, int k, int64_t teacher_ld,
-                                float temperature, float *loss, float *lse, void *workspace, size_t workspace_bytes,
-                                void *stream) {
+                                float temperature, float *loss, float *lse, void *stream) {
     const Args a{logits, rows, vocab, ld, teacher, index, k, teacher_ld, temperature, nullptr, loss, lse, nullptr, 0};
     const int rc = check(a, dtype);
     if (rc != BYZ_OK || rows == 0) return rc;
@@ -337,5 +591,14 @@ extern "C" int byz_distill_loss_step(const void *logits, int64_t rows, int64_t v
     const int rc = check_gradient(a, dtype);
     if (rc != BYZ_OK || rows == 0) return rc;
     if (!loss) return BYZ_EINVAL;
+    const bool alike = ((((uintptr_t)logits ^ (uintptr_t)dlogits) | (uintptr_t)((ld - dlogits_ld) * dtype_size(dtype))) & 15) == 0;
+    if (fits_resident(rows, vocab, dtype)) {
+        if (workspace_bytes < resident_bytes(rows, k) || !workspace || !aligned(workspace, 16)) return BYZ_ENOMEM;
+        if (alike) {
+            const hipStream_t s = (hipStream_t)stream;
+            return dtype == BYZ_F32 ? launch_resident<float>(a, workspace, s)
+                   : dtype == BYZ_BF16 ? launch_resident<bf16>(a, workspace, s) : launch_resident<f16>(a, workspace, s);
+        }
+    }
     return launch<kStep>(a, dtype, (hipStream_t)stream);
 }

@@ -156,13 +156,6 @@ struct Side {
     }
 };
 
-// The same number, of which the compiler knows nothing: what is computed from it is not kept over a loop, where the
-// registers are wanted for sums.
-__device__ __forceinline__ int afresh(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 // A block's place among the output tiles, and what its loads need.
 template <typename T, int BM, int BN, int WM, int WN, Kind KIND>
 struct Place {

@@ -385,13 +385,13 @@ template <typename T, int V, int U, int N, typename F>
 __device__ __forceinline__ void each_position(const Plan &q, const Tile &t, const T *const (&at)[N], const int64_t (&pixel)[N], F fn) {
     if (!t.mine) return;
     for (int r = 0; t.ty + r * q.ty < t.np; r += U) {
-        Pack<T, V> v[U][N];
+        Words<T, V> v[U][N];
         const bool all = t.ty + (r + U - 1) * q.ty < t.np;
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (all || t.ty + (r + u) * q.ty < t.np)
 #pragma unroll
-                for (int j = 0; j < N; j++) v[u][j] = *(const Pack<T, V> *)(at[j] + (int64_t)(r + u) * q.ty * pixel[j]);
+                for (int j = 0; j < N; j++) v[u][j] = *(const Words<T, V> *)(at[j] + (int64_t)(r + u) * q.ty * pixel[j]);
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (all || t.ty + (r + u) * q.ty < t.np) {
@@ -421,11 +421,8 @@ struct Affine {
 };
 
 template <int ACT, typename T, int V>
-__device__ __forceinline__ Pack<T, V> normalised(const Affine<V> &f, const Pack<T, V> &x) {
-    Pack<T, V> y;
-#pragma unroll
-    for (int v = 0; v < V; v++) y.v[v] = round_to<T>(act_value<ACT>(f.z((float)x.v[v], v)));
-    return y;
+__device__ __forceinline__ Words<T, V> normalised(const Affine<V> &f, const Words<T, V> &x) {
+    return Words<T, V>::of([&](int v) { return act_value<ACT>(f.z(x[v], v)); });
 }
 
 // Forward, a whole slice in registers.
@@ -437,12 +434,12 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
         const Tile t(q, tile, V);
         Stat *grp = (Stat *)lds;
         float *entries = lds + 3 * q.head;
-        Pack<T, V> x[R];
+        Words<T, V> x[R];
         const T *at = t.in<T>(a.x, a.xs, a.xp, V);
         int count = 0;
 #pragma unroll
         for (int r = 0; r < R; r++)
-            if (t.mine && t.ty + r * q.ty < t.np) x[r] = *(const Pack<T, V> *)(at + (int64_t)r * q.ty * a.xp), count++;
+            if (t.mine && t.ty + r * q.ty < t.np) x[r] = *(const Words<T, V> *)(at + (int64_t)r * q.ty * a.xp), count++;
         // counted from the thread's first value, x[0]
         float m[V] = {}, d[V] = {}, first[V];
         t.firsts<T, V>(a, first);
@@ -450,25 +447,25 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
         for (int r = 1; r < R; r++)
             if (r < count)
 #pragma unroll
-                for (int v = 0; v < V; v++) m[v] += (float)x[r].v[v] - (float)x[0].v[v];
+                for (int v = 0; v < V; v++) m[v] += x[r][v] - x[0][v];
         const float inv = count ? __builtin_amdgcn_rcpf((float)count) : 0.0f;
 #pragma unroll
         for (int v = 0; v < V; v++) m[v] *= inv;
 #pragma unroll
-        for (int r = 0; r < R; r++) keep_packed(x[r]);
+        for (int r = 0; r < R; r++) x[r].keep();
 #pragma unroll
         for (int r = 0; r < R; r++)
             if (r < count)
 #pragma unroll
                 for (int v = 0; v < V; v++) {
-                    const float e = ((float)x[r].v[v] - (float)x[0].v[v]) - m[v];
+                    const float e = (x[r][v] - x[0][v]) - m[v];
                     d[v] += e * e;
                 }
         if (count)
 #pragma unroll
-            for (int v = 0; v < V; v++) m[v] += (float)x[0].v[v] - first[v];
+            for (int v = 0; v < V; v++) m[v] += x[0][v] - first[v];
 #pragma unroll
-        for (int r = 0; r < R; r++) keep_packed(x[r]);
+        for (int r = 0; r < R; r++) x[r].keep();
         group_stats<V>(q, t, (float)count, m, d, entries, grp);
         const float m1 = 1.0f / ((float)q.p * (float)q.gc);
         auto mean = [&](int g) { return grp[g].m; };
@@ -486,7 +483,7 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
 #pragma unroll
                 for (int r = 0; r < R; r++)
                     if (r < count) {
-                        *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[r]);
+                        *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[r]);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             });
@@ -508,13 +505,13 @@ __global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
         int count = 0;
         const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
         const int64_t pixel[1] = {a.xp};
-        each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Pack<T, V>(&x)[1]) {
+        each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Words<T, V>(&x)[1]) {
             if (r == 0)
 #pragma unroll
-                for (int v = 0; v < V; v++) pivot[v] = (float)x[0].v[v];
+                for (int v = 0; v < V; v++) pivot[v] = x[0][v];
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                const float e = (float)x[0].v[v] - pivot[v];
+                const float e = x[0][v] - pivot[v];
                 s[v] += e, d[v] += e * e;
             }
             count++;
@@ -571,26 +568,26 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(Args a) {
         const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
         const int64_t pixel[1] = {a.xp};
         with_act(a.act, [&](auto act) {
-            each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Pack<T, V>(&x)[1]) {
-                *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[0]);
+            each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Words<T, V>(&x)[1]) {
+                *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[0]);
             });
         });
     }
 }
 
 // dz of a value, for the sums and for dx
-template <int ACT, typename T, int V>
-__device__ __forceinline__ float slope_of(const Affine<V> &f, float x, T dy, int v) {
-    return (float)dy * act_slope<ACT>((x - f.m[v]) * f.s[v] + f.b[v]);
+template <int ACT, int V>
+__device__ __forceinline__ float slope_of(const Affine<V> &f, float x, float dy, int v) {
+    return dy * act_slope<ACT>((x - f.m[v]) * f.s[v] + f.b[v]);
 }
 
 // A and B of this thread's values; B without rstd, which channel_total() multiplies
 template <int ACT, typename T, int V>
-__device__ __forceinline__ void add_values(const Affine<V> &f, const Pack<T, V> &x, const Pack<T, V> &dy, float (&acc)[2][V]) {
+__device__ __forceinline__ void add_values(const Affine<V> &f, const Words<T, V> &x, const Words<T, V> &dy, float (&acc)[2][V]) {
 #pragma unroll
     for (int v = 0; v < V; v++) {
-        const float e = (float)x.v[v] - f.m[v];
-        const float dz = slope_of<ACT>(f, (float)x.v[v], dy.v[v], v);
+        const float e = x[v] - f.m[v];
+        const float dz = slope_of<ACT>(f, x[v], dy[v], v);
         acc[0][v] += dz;
         acc[1][v] += dz * e;
     }
@@ -598,15 +595,12 @@ __device__ __forceinline__ void add_values(const Affine<V> &f, const Pack<T, V> 
 
 // dx = s dz + (x - m) k1 + k0 with s = rstd gamma, k1 = -rstd^2 S2, k0 = -rstd S1
 template <int ACT, typename T, int V>
-__device__ __forceinline__ Pack<T, V> gradient(const Affine<V> &f, const float (&k1)[V], const float (&k0)[V], const Pack<T, V> &x,
-                                               const Pack<T, V> &dy) {
-    Pack<T, V> d;
-#pragma unroll
-    for (int v = 0; v < V; v++) {
-        const float e = (float)x.v[v] - f.m[v];
-        d.v[v] = round_to<T>(slope_of<ACT>(f, (float)x.v[v], dy.v[v], v) * f.s[v] + (e * k1[v] + k0[v]));
-    }
-    return d;
+__device__ __forceinline__ Words<T, V> gradient(const Affine<V> &f, const float (&k1)[V], const float (&k0)[V], const Words<T, V> &x,
+                                               const Words<T, V> &dy) {
+    return Words<T, V>::of([&](int v) {
+        const float e = x[v] - f.m[v];
+        return slope_of<ACT>(f, x[v], dy[v], v) * f.s[v] + (e * k1[v] + k0[v]);
+    });
 }
 
 // Backward, a whole slice in registers: the channels' A and B, and dx.
@@ -619,14 +613,14 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
         const Tile t(q, tile, V);
         float *chan = lds, *grp = chan + 2 * cs, *rows = grp + 2 * cs;
         const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
-        Pack<T, V> x[R], dy[R];
+        Words<T, V> x[R], dy[R];
         const T *xat = t.in<T>(a.x, a.xs, a.xp, V), *dat = t.in<T>(a.dy, a.ds, a.dp, V);
         int count = 0;
 #pragma unroll
         for (int r = 0; r < R; r++)
             if (t.mine && t.ty + r * q.ty < t.np) {
-                x[r] = *(const Pack<T, V> *)(xat + (int64_t)r * q.ty * a.xp);
-                dy[r] = *(const Pack<T, V> *)(dat + (int64_t)r * q.ty * a.dp);
+                x[r] = *(const Words<T, V> *)(xat + (int64_t)r * q.ty * a.xp);
+                dy[r] = *(const Words<T, V> *)(dat + (int64_t)r * q.ty * a.dp);
                 count++;
             }
         const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
@@ -640,7 +634,7 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
                 }
         });
 #pragma unroll
-        for (int r = 0; r < R; r++) keep_packed(x[r]), keep_packed(dy[r]);
+        for (int r = 0; r < R; r++) x[r].keep(), dy[r].keep();
         channel_sums<2, V>(q, t, acc, rows, chan);
         for (int j = threadIdx.x; j < t.nc; j += q.threads) {
             chan[cs + j] *= rstd[j / (int)q.gc];
@@ -663,7 +657,7 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
 #pragma unroll
                 for (int r = 0; r < R; r++)
                     if (r < count) {
-                        *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, x[r], dy[r]);
+                        *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, x[r], dy[r]);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             });
@@ -687,7 +681,7 @@ __global__ __launch_bounds__(256) void norm_backward_sums_kernel(Args a) {
         const T *const at[2] = {t.in<T>(a.x, a.xs, a.xp, V), t.in<T>(a.dy, a.ds, a.dp, V)};
         const int64_t pixel[2] = {a.xp, a.dp};
         with_act(a.act, [&](auto act) {
-            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Pack<T, V>(&v)[2]) { add_values<act.value>(f, v[0], v[1], acc); });
+            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Words<T, V>(&v)[2]) { add_values<act.value>(f, v[0], v[1], acc); });
         });
         channel_sums<2, V>(q, t, acc, rows, chan);
         const int w = t.width(q);
@@ -761,8 +755,8 @@ __global__ __launch_bounds__(256) void norm_backward_apply_kernel(Args a) {
         const T *const at[2] = {t.in<T>(a.x, a.xs, a.xp, V), t.in<T>(a.dy, a.ds, a.dp, V)};
         const int64_t pixel[2] = {a.xp, a.dp};
         with_act(a.act, [&](auto act) {
-            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Pack<T, V>(&v)[2]) {
-                *(Pack<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, v[0], v[1]);
+            each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Words<T, V>(&v)[2]) {
+                *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, v[0], v[1]);
             });
         });
     }

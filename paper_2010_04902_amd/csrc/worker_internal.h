@@ -9,6 +9,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "byz_internal.h"
 #include "byzshield_worker.h"
@@ -37,18 +38,65 @@ struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
-// The compiler takes what it has made of these bytes (values widened to fp32) for lost: they stay packed in
-// registers, and are widened again where they are used.
+// The same, held as 32-bit words: values of 16 bits that live over a loop or a barrier as such would take a register
+// each.
+typedef uint32_t __attribute__((may_alias)) word_t;
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
 template <typename T, int V>
-__device__ __forceinline__ void keep_packed(Pack<T, V> &p) {
-    if constexpr (sizeof(p) % 4 == 0) {
-        uint32_t w[sizeof(p) / 4];
-        __builtin_memcpy(w, &p, sizeof(p));
-#pragma unroll
-        for (uint32_t &x : w) asm volatile("" : "+v"(x));
-        __builtin_memcpy(&p, w, sizeof(p));
+struct alignas(sizeof(T) * V) Words {
+    static constexpr int N = sizeof(T) * V / 4;
+    word_t w[N];
+    __device__ __forceinline__ float operator[](int e) const {
+        if constexpr (sizeof(T) == 4) {
+            return __builtin_bit_cast(float, (uint32_t)w[e]);
+        } else if constexpr (std::is_same_v<T, bf16>) {
+            return __builtin_bit_cast(float, e % 2 ? (uint32_t)w[e / 2] & 0xffff0000u : (uint32_t)w[e / 2] << 16);
+        } else {
+            return (float)__builtin_bit_cast(f16x2, (uint32_t)w[e / 2])[e % 2];
+        }
     }
-}
+    // the values f(0) .. f(V - 1), rounded to the nearest, ties to even
+    template <typename F>
+    static __device__ __forceinline__ Words of(F f) {
+        Words r;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if constexpr (sizeof(T) == 4) {
+                r.w[i] = __builtin_bit_cast(uint32_t, (float)f(i));
+            } else {
+                const floatx2 x = {f(2 * i), f(2 * i + 1)};
+                if constexpr (std::is_same_v<T, bf16>)
+                    r.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+                else
+                    r.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+            }
+        }
+        return r;
+    }
+    // The compiler takes what it has made of the words (values widened to fp32) for lost, and makes it again where it is used.
+    __device__ __forceinline__ void keep() {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            uint32_t x = w[i];
+            asm volatile("" : "+v"(x));
+            w[i] = x;
+        }
+    }
+};
+
+template <typename T>
+struct Words<T, 1> {
+    T t;
+    __device__ __forceinline__ float operator[](int) const { return (float)t; }
+    template <typename F>
+    static __device__ __forceinline__ Words of(F f) {
+        return Words{(T)f(0)};
+    }
+    __device__ __forceinline__ void keep() {}
+};
 
 // fp32 -> T, to the nearest, ties to even
 template <typename T>
@@ -57,6 +105,13 @@ __device__ __forceinline__ T round_to(float x) {
 }
 
 __device__ __forceinline__ float sigmoidf(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+// The same number, of which the compiler knows nothing: what is computed from it is not kept over a loop, where the
+// registers are wanted for other things.
+__device__ __forceinline__ int afresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // The normal distribution's upper tail at |z|, from e = exp(-z^2 / 2): the rational approximation 7.1.26 of
 // Abramowitz and Stegun for erfc(|z| / sqrt 2) / 2, good to 7.5e-8.

@@ -37,8 +37,8 @@ def _load():
         "byz_group_norm_backward_workspace_bytes": (sz, [i64, i64, i64, c_int, c_int]),
         "byz_group_norm_backward": (c_int, [vp, i64, i64, vp, i64, i64, i64, i64, i64, c_int, c_int, vp, vp, vp, vp,
                                             c_int, vp, i64, i64, vp, vp, vp, sz, vp]),
-        "byz_distill_loss_workspace_bytes": (sz, [i64, i64, c_int, c_int]),
-        "byz_distill_loss": (c_int, [vp, i64, i64, i64, c_int, vp, vp, c_int, i64, f32, vp, vp, vp, sz, vp]),
+        "byz_distill_loss": (c_int, [vp, i64, i64, i64, c_int, vp, vp, c_int, i64, f32, vp, vp, vp]),
+        "byz_distill_loss_step_workspace_bytes": (sz, [i64, i64, c_int, c_int]),
         "byz_distill_loss_backward": (c_int, [vp, vp, i64, i64, i64, c_int, vp, vp, c_int, i64, vp, f32, vp, i64, vp]),
         "byz_distill_loss_step": (c_int, [vp, i64, i64, i64, c_int, vp, vp, c_int, i64, vp, f32, vp, vp, vp, i64,
                                           vp, sz, vp]),
@@ -267,11 +267,8 @@ def byz_distill_loss(logits, teacher, index, temperature=1.0, stream=None):
     empty = _torch.empty if stream is None else _b._empty_on(stream)
     loss = empty(rows, dtype=_torch.float32, device=device)
     lse = empty(rows, dtype=_torch.float32, device=device)
-    nbytes = _workspace_bytes("byz_distill_loss_workspace_bytes", rows, vocab, k, dtype)
-    ws, at = _workspace(nbytes, empty, device)
     _b._check(_lib.byz_distill_loss(logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k, tld,
-                                    temperature, loss.data_ptr(), lse.data_ptr(), at, nbytes, _stream(stream, gpu)),
-              "byz_distill_loss")
+                                    temperature, loss.data_ptr(), lse.data_ptr(), _stream(stream, gpu)), "byz_distill_loss")
     return loss, lse
 
 
@@ -301,7 +298,7 @@ def byz_distill_loss_step(logits, teacher, index, dloss, temperature=1.0, out=No
     d = _floats(dloss, (rows,), "dloss", gpu)
     out, old = _gradient_out(out, logits, empty, gpu)
     loss = empty(rows, dtype=_torch.float32, device=device)
-    nbytes = _workspace_bytes("byz_distill_loss_workspace_bytes", rows, vocab, k, dtype)
+    nbytes = _workspace_bytes("byz_distill_loss_step_workspace_bytes", rows, vocab, k, dtype)
     ws, at = _workspace(nbytes, empty, device)
     _b._check(_lib.byz_distill_loss_step(logits.data_ptr(), rows, vocab, ld, dtype, teacher.data_ptr(), index.data_ptr(), k,
                                          tld, d, temperature, loss.data_ptr(), None, out.data_ptr(), old, at, nbytes,

@@ -93,8 +93,7 @@ def test_group_norm_backward_needs_its_workspace():
 
 
 def _distill(logits=P, rows=4, vocab=100, ld=100, dtype=0, teacher=P, index=P, k=5, tld=5, temperature=1.0, loss=P, lse=P):
-    return worker._load().byz_distill_loss(logits, rows, vocab, ld, dtype, teacher, index, k, tld, temperature, loss, lse,
-                                           None, 0, None)
+    return worker._load().byz_distill_loss(logits, rows, vocab, ld, dtype, teacher, index, k, tld, temperature, loss, lse, None)
 
 
 def _distill_step(logits=P, rows=4, vocab=100, ld=100, dtype=0, teacher=P, index=P, k=5, tld=5, dloss=P, temperature=1.0,
@@ -124,6 +123,13 @@ def test_distill_refusals(bad):
 def test_distill_gradient_refusals(bad):
     assert _distill_step(**bad) == EINVAL
     assert _distill_backward(**bad) == EINVAL
+
+
+def test_distill_step_needs_its_workspace():
+    # long rows are held in registers between two kernels of their own
+    need = worker._load().byz_distill_loss_step_workspace_bytes(1000, 100000, 5, 1)
+    assert need > 0 and worker._load().byz_distill_loss_step_workspace_bytes(1000, 1000, 5, 1) == 0
+    assert _distill_step(rows=1000, vocab=100000, ld=100000, old=100000, dtype=1) == ENOMEM
 
 
 def test_distill_needs_its_outputs():
