@@ -5,9 +5,9 @@
 // same V channels at positions t / tx, t / tx + ty, ...
 //
 //   forward    a thread's own mean and squared distances from it, joined pairwise (count, mean, distances) over
-//              threads, waves and chunks in a fixed order, so there is no difference of large sums.  Means are
-//              counted from the group's first value: the pairwise differences of means then lose nothing where
-//              a group's mean is many times its deviation.  Then act((x - mean) rstd gamma + beta).
+//              threads, waves and chunks in a fixed order, so there is no difference of large sums.  The means are fp64:
+//              their pairwise differences then lose nothing where a group's mean is many times its deviation.
+//              Then act((x - mean) rstd gamma + beta).
 //   backward   with the activation's slope recomputed, dz = dy act'(z): per channel the sums A of dz and
 //              B of dz xhat are all that is needed,
 //                  dbeta = sum A,  dgamma = sum B  (over the samples, in order),
@@ -35,11 +35,14 @@ constexpr int kMaxLanes = 256;         // most vectors of a slice's row
 constexpr int kDepth = 32;             // positions of a thread in a chunk at most: what its sums about its first
                                        // value can lose is 2^-24 times this
 constexpr int64_t kMaxGrid = 1 << 20;  // blocks of a launch; more tiles are taken in turn
+// Blocks go to the eight dies in turn; neighbouring tiles (slices of the same rows share cache lines, chunks a group's
+// statistics) are numbered so that they meet on one die and its L2.
 
 struct Plan {
     int64_t n, p, c;
     uint32_t groups, gc;          // groups of gc channels
     uint32_t slices, chunks, tiles;
+    uint32_t per_xcd;             // tiles of a block number modulo 8
     int vec, cs, tx, ty, threads, r, unit;  // unit: neighbouring channels of a vector that are in one group
     int head;                     // groups of a slice
     uint32_t parts;               // blocks that share a group's channels (1: a slice has whole groups)
@@ -77,8 +80,8 @@ bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int ele
     // vectors where neither is possible
     for (;; vec = vec > 4 / elem ? (4 / elem > 1 ? 4 / elem : 1) : 1) {
         step = gc / gcd(gc, vec) * vec;
-        // eight units a thread: with 1024 threads their statistics would not fit 64 KB of LDS
-        max_threads = !forward ? kBackwardThreads : vec / gcd(gc, vec) >= 8 ? kForwardThreads / 2 : kForwardThreads;
+        // four units a thread or eight: the statistics of 1024 threads would not fit 64 KB of LDS
+        max_threads = !forward ? kBackwardThreads : kForwardThreads / (int)std::max<int64_t>(1, vec / gcd(gc, vec) / 2);
         if (step / vec <= kMaxLanes) {
             // 128 bytes of a row, a cache line, where the channels reach
             int64_t cs = step;
@@ -136,10 +139,17 @@ bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int ele
         n * groups > INT32_MAX)
         return false;
     q.slices = (uint32_t)slices, q.chunks = (uint32_t)chunks, q.tiles = (uint32_t)tiles;
+    q.per_xcd = (q.tiles + 7) / 8;
     return true;
 }
 
 bool whole(const Plan &q) { return q.r > 0; }
+
+// Mean, count, squared distances from it.
+struct Stat {
+    double m;
+    float n, d;
+};
 
 struct Args {
     Plan q;
@@ -150,8 +160,8 @@ struct Args {
     float *mean, *rstd;
     float eps;
     int act;
-    float2 *part;   // forward: (mean, squared distances) of [sample][group][chunk][part]; backward: (A, B) of [sample][chunk][channel]
-    float *first;   // forward: the groups' first values, which the third kernel may overwrite (y over x)
+    Stat *stat;     // forward: of [sample][group][chunk][part]
+    float2 *part;   // backward: (A, B) of [sample][chunk][channel]
     float2 *total;  // backward: (A, B) of [sample][channel]
     float2 *sums;   // backward: (S1, S2) of [sample][group]
     float *dgamma, *dbeta;
@@ -198,19 +208,6 @@ struct Tile {
             if (++rem == w) rem = 0, at++;
         }
     }
-    // the first value of a group, counted from g0
-    template <typename T>
-    __device__ __forceinline__ float first_of(const Args &a, int g) const {
-        return (float)((const T *)a.x)[i * a.xs + (int64_t)(g0 + g) * a.q.gc];
-    }
-    // the first values of this thread's groups
-    template <typename T, int V>
-    __device__ void firsts(const Args &a, float (&first)[V]) const {
-        int g[V];
-        groups_of<V>(a.q, g);
-#pragma unroll
-        for (int v = 0; v < V; v++) first[v] = v % a.q.unit == 0 ? first_of<T>(a, g[v]) : first[v > 0 ? v - 1 : 0];
-    }
     template <typename T>
     __device__ const T *in(const void *base, int64_t sample, int64_t pixel, int V) const {
         return (const T *)base + i * sample + (p0 + ty) * pixel + c0 + tx * V;
@@ -221,18 +218,15 @@ struct Tile {
     }
 };
 
-// Count, mean, squared distances from it.
-struct Stat {
-    float n, m, d;
-};
-
 __device__ __forceinline__ Stat join(Stat a, Stat b) {
     // written so that a set with a count of 0 changes nothing
-    const float n = a.n + b.n, f = n > 0.0f ? b.n * __builtin_amdgcn_rcpf(n) : 0.0f, e = b.n > 0.0f ? b.m - a.m : 0.0f;
-    return Stat{n, a.n > 0.0f ? a.m + e * f : b.m, a.d + b.d + (a.n > 0.0f ? e * e * (a.n * f) : 0.0f)};
+    const float n = a.n + b.n, f = n > 0.0f ? b.n * __builtin_amdgcn_rcpf(n) : 0.0f;
+    const double e = b.n > 0.0f ? b.m - a.m : 0.0;
+    const float e1 = (float)e;
+    return Stat{a.n > 0.0f ? a.m + e * (double)f : b.m, n, a.d + b.d + (a.n > 0.0f ? e1 * e1 * (a.n * f) : 0.0f)};
 }
 
-__device__ __forceinline__ Stat from(Stat s, int off) { return Stat{__shfl_xor(s.n, off), __shfl_xor(s.m, off), __shfl_xor(s.d, off)}; }
+__device__ __forceinline__ Stat from(Stat s, int off) { return Stat{__shfl_xor(s.m, off), __shfl_xor(s.n, off), __shfl_xor(s.d, off)}; }
 
 // Joins the statistics of the wave's lanes; each gets the same bits.
 __device__ __forceinline__ Stat join_wave(Stat s, int first, int end) {
@@ -246,11 +240,10 @@ __device__ __forceinline__ Stat join_wave(Stat s, int first, int end) {
 constexpr int kStatRows = 16;
 constexpr int kSerial = 16;  // entries of a group that one thread joins
 
-// Joins the threads' statistics (n values each of V channels, mean m from the group's first value, distances d)
-// into the groups': grp[g].
+// Joins the threads' statistics (n values each of V channels, mean m, distances d) into the groups': grp[g].
 // Ends with a barrier.  `entries`: LDS for one Stat a thread and unit, or a wave's column and unit.
 template <int V>
-__device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V], float (&d)[V], float *lds, Stat *grp) {
+__device__ void group_stats(const Plan &q, const Tile &t, float n, double (&m)[V], float (&d)[V], Stat *entry, Stat *grp) {
     // channels of a unit first: equal counts
     float count = n;
 #pragma unroll
@@ -258,8 +251,8 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V]
         if (q.unit > w) {
 #pragma unroll
             for (int v = 0; v < V; v += 2 * w) {
-                const float e = m[v + w] - m[v];
-                m[v] += 0.5f * e;
+                const float e = (float)(m[v + w] - m[v]);
+                m[v] = 0.5 * (m[v] + m[v + w]);
                 d[v] += d[v + w] + e * e * (0.5f * count);
             }
             count *= 2.0f;
@@ -267,7 +260,6 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V]
     const int units = q.cs / q.unit;  // of a row of threads
     int rows = q.ty, row = t.ty;
     bool writes = t.mine;
-    Stat *entry = (Stat *)lds;
     const bool joined = q.tx < 64 && (q.tx & (q.tx - 1)) == 0;  // a wave holds whole rows
     if (joined) {
         rows = q.threads / 64, row = threadIdx.x / 64;
@@ -277,12 +269,13 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V]
 #pragma unroll
     for (int v = 0; v < V; v++)
         if (v % q.unit == 0) {
-            Stat s{t.mine ? count : 0.0f, m[v], d[v]};
+            Stat s{m[v], t.mine ? count : 0.0f, d[v]};
             if (joined && even) {
                 for (int off = q.tx; off < 64; off *= 2) {
                     // the pair's lanes get the same bits: their sum, and the square of their difference
-                    const float m2 = __shfl_xor(s.m, off), d2 = __shfl_xor(s.d, off), e = m2 - s.m;
-                    s.m = 0.5f * (s.m + m2);
+                    const double m2 = __shfl_xor(s.m, off);
+                    const float d2 = __shfl_xor(s.d, off), e = (float)(m2 - s.m);
+                    s.m = 0.5 * (s.m + m2);
                     s.d = (s.d + d2) + e * e * (0.5f * s.n);
                     s.n *= 2.0f;
                 }
@@ -303,7 +296,7 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, float (&m)[V]
     } else {  // a wave a group
         const int lane = threadIdx.x % 64;
         for (int g = threadIdx.x / 64; g < ng; g += q.threads / 64) {
-            Stat s{0.0f, 0.0f, 0.0f};
+            Stat s{0.0, 0.0f, 0.0f};
             for (int e = lane; e < rows * per; e += 64) s = join(s, entry[e / per * units + g * per + e % per]);
             s = join_wave(s, 1, 64);
             if (lane == 0) grp[g] = s;
@@ -430,10 +423,11 @@ template <typename T, int V, int R>
 __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         Stat *grp = (Stat *)lds;
-        float *entries = lds + 3 * q.head;
         Words<T, V> x[R];
         const T *at = t.in<T>(a.x, a.xs, a.xp, V);
         int count = 0;
@@ -441,8 +435,7 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
         for (int r = 0; r < R; r++)
             if (t.mine && t.ty + r * q.ty < t.np) x[r] = *(const Words<T, V> *)(at + (int64_t)r * q.ty * a.xp), count++;
         // counted from the thread's first value, x[0]
-        float m[V] = {}, d[V] = {}, first[V];
-        t.firsts<T, V>(a, first);
+        float m[V] = {}, d[V] = {};
 #pragma unroll
         for (int r = 1; r < R; r++)
             if (r < count)
@@ -461,21 +454,20 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
                     const float e = (x[r][v] - x[0][v]) - m[v];
                     d[v] += e * e;
                 }
+        double centre[V] = {};
         if (count)
 #pragma unroll
-            for (int v = 0; v < V; v++) m[v] += x[0][v] - first[v];
+            for (int v = 0; v < V; v++) centre[v] = (double)x[0][v] + (double)m[v];
 #pragma unroll
         for (int r = 0; r < R; r++) x[r].keep();
-        group_stats<V>(q, t, (float)count, m, d, entries, grp);
+        group_stats<V>(q, t, (float)count, centre, d, grp + q.head, grp);
         const float m1 = 1.0f / ((float)q.p * (float)q.gc);
-        auto mean = [&](int g) { return grp[g].m; };
+        auto mean = [&](int g) { return (float)grp[g].m; };
         auto rstd = [&](int g) { return 1.0f / sqrtf(grp[g].d * m1 + a.eps); };
         for (int g = threadIdx.x; g < t.groups(q); g += q.threads) {
-            grp[g].m += t.first_of<T>(a, g);
-            a.mean[t.i * q.groups + t.g0 + g] = grp[g].m;
+            a.mean[t.i * q.groups + t.g0 + g] = mean(g);
             a.rstd[t.i * q.groups + t.g0 + g] = rstd(g);
         }
-        __syncthreads();
         if (t.mine) {
             const Affine<V> f(a, t, mean, rstd);
             T *to = t.out<T>(a, V);
@@ -497,11 +489,12 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         Stat *grp = (Stat *)lds;
-        float pivot[V] = {}, s[V] = {}, d[V] = {}, first[V];
-        t.firsts<T, V>(a, first);
+        float pivot[V] = {}, s[V] = {}, d[V] = {};
         int count = 0;
         const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
         const int64_t pixel[1] = {a.xp};
@@ -517,18 +510,17 @@ __global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
             count++;
         });
         const float inv = count ? __builtin_amdgcn_rcpf((float)count) : 0.0f;
+        double centre[V];
 #pragma unroll
         for (int v = 0; v < V; v++) {
             // NaN and infinities go on as NaN; what rounding leaves below 0 does not
             const float e = d[v] - s[v] * s[v] * inv;
             d[v] = e < 0.0f ? 0.0f : e;
-            pivot[v] = (pivot[v] - first[v]) + s[v] * inv;
+            centre[v] = (double)pivot[v] + (double)(s[v] * inv);
         }
-        group_stats<V>(q, t, (float)count, pivot, d, lds + 3 * q.head, grp);
-        if (t.chunk == 0 && t.part == 0)
-            for (int g = threadIdx.x; g < t.groups(q); g += q.threads) a.first[t.i * q.groups + t.g0 + g] = t.first_of<T>(a, g);
+        group_stats<V>(q, t, (float)count, centre, d, grp + q.head, grp);
         for (int g = threadIdx.x; g < t.groups(q); g += q.threads)
-            a.part[((t.i * q.groups + t.g0 + g) * q.chunks + t.chunk) * q.parts + t.part] = make_float2(grp[g].m, grp[g].d);
+            a.stat[((t.i * q.groups + t.g0 + g) * q.chunks + t.chunk) * q.parts + t.part] = grp[g];
         __syncthreads();
     }
 }
@@ -539,17 +531,11 @@ __global__ __launch_bounds__(256) void norm_join_kernel(Args a) {
     const int lane = threadIdx.x % 64;
     const uint32_t all = (uint32_t)q.n * q.groups, entries = q.chunks * q.parts;
     for (uint32_t group = blockIdx.x * 4 + threadIdx.x / 64; group < all; group += gridDim.x * 4) {
-        Stat s{0.0f, 0.0f, 0.0f};
-        for (uint32_t e = lane; e < entries; e += 64) {
-            const uint32_t chunk = e / q.parts, part = e - chunk * q.parts;
-            const int64_t np = min(q.chunk, q.p - chunk * q.chunk);
-            const uint32_t nc = q.parts > 1 ? min((uint32_t)q.cs, q.gc - part * q.cs) : q.gc;
-            const float2 v = a.part[(int64_t)group * entries + e];
-            s = join(s, Stat{(float)np * (float)nc, v.x, v.y});
-        }
+        Stat s{0.0, 0.0f, 0.0f};
+        for (uint32_t e = lane; e < entries; e += 64) s = join(s, a.stat[(int64_t)group * entries + e]);
         s = join_wave(s, 1, 64);
         if (lane == 0) {
-            a.mean[group] = s.m + a.first[group];
+            a.mean[group] = (float)s.m;
             a.rstd[group] = 1.0f / sqrtf(s.d / ((float)q.p * (float)q.gc) + a.eps);
         }
     }
@@ -559,7 +545,9 @@ __global__ __launch_bounds__(256) void norm_join_kernel(Args a) {
 template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_apply_kernel(Args a) {
     const Plan &q = a.q;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         if (!t.mine) continue;
         const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
@@ -609,7 +597,9 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
     extern __shared__ float lds[];
     const Plan &q = a.q;
     const int cs = q.cs;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         float *chan = lds, *grp = chan + 2 * cs, *rows = grp + 2 * cs;
         const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
@@ -672,7 +662,9 @@ __global__ __launch_bounds__(256) void norm_backward_sums_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
     const int cs = q.cs;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         float *chan = lds, *rows = chan + 2 * cs;
         const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
@@ -736,7 +728,9 @@ __global__ __launch_bounds__(256) void norm_backward_totals_kernel(Args a) {
 template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_backward_apply_kernel(Args a) {
     const Plan &q = a.q;
-    for (uint32_t tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < 8 * q.per_xcd; b += gridDim.x) {
+        const uint32_t tile = b % 8 * q.per_xcd + b / 8;
+        if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
         if (!t.mine) continue;
         const float *mean = a.mean + t.i * q.groups + t.g0, *rstd = a.rstd + t.i * q.groups + t.g0;
@@ -792,13 +786,13 @@ unsigned grid_of(int64_t tiles) { return (unsigned)(tiles < kMaxGrid ? tiles : k
 // rows of threads that leave an entry in LDS
 size_t lds_rows(const Plan &q) { return q.tx < 64 && (q.tx & (q.tx - 1)) == 0 ? q.threads / 64 : q.ty; }
 
-size_t stat_bytes(const Plan &q) { return sizeof(float) * (3 * q.head + lds_rows(q) * 3 * (q.cs / q.unit)); }
+size_t stat_bytes(const Plan &q) { return sizeof(Stat) * (q.head + lds_rows(q) * (q.cs / q.unit)); }
 
 size_t sum_bytes(const Plan &q, int head) { return sizeof(float) * q.cs * (head + 2 * lds_rows(q)); }
 
 template <typename T, int V>
 int launch_forward(const Args &a, hipStream_t s) {
-    const unsigned grid = grid_of(a.q.tiles);
+    const unsigned grid = grid_of((int64_t)8 * a.q.per_xcd);
     const int threads = a.q.threads;
     const size_t lds = stat_bytes(a.q);
     switch (a.q.r) {
@@ -819,7 +813,7 @@ int launch_forward(const Args &a, hipStream_t s) {
 
 template <typename T, int V>
 int launch_backward(const Args &a, hipStream_t s) {
-    const unsigned grid = grid_of(a.q.tiles);
+    const unsigned grid = grid_of((int64_t)8 * a.q.per_xcd);
     const int threads = a.q.threads;
     switch (a.q.r) {
         case 1: norm_backward_whole_kernel<T, V, 1><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
@@ -877,9 +871,7 @@ size_t most_bytes(int64_t n, int64_t p, int64_t c, int groups, int elem, bool fo
     return most;
 }
 
-size_t first_at(const Plan &q) { return round_up(sizeof(float2) * q.n * q.groups * q.chunks * q.parts); }
-
-size_t forward_bytes(const Plan &q) { return whole(q) ? 0 : first_at(q) + round_up(sizeof(float) * q.n * q.groups); }
+size_t forward_bytes(const Plan &q) { return whole(q) ? 0 : round_up(sizeof(Stat) * q.n * q.groups * q.chunks * q.parts); }
 
 struct BackwardLayout {
     size_t total, sums, part, bytes;
@@ -925,8 +917,7 @@ extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, 
     a.x = x, a.xs = x_sample, a.xp = x_pixel;
     a.out = y, a.os = y_sample, a.op = y_pixel;
     a.gamma = gamma, a.beta = beta, a.mean = mean, a.rstd = rstd, a.eps = eps, a.act = act;
-    a.part = (float2 *)workspace;
-    a.first = (float *)((char *)workspace + (whole(a.q) ? 0 : first_at(a.q)));
+    a.stat = (Stat *)workspace;
     return launch<true>(a, dtype, s);
 }
 

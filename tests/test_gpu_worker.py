@@ -301,9 +301,11 @@ def _distill_check(logits, teacher, index, dloss, tau, out=None):
     _near(loss, want, tol, "loss")
     _near(loss2, want, tol, "loss of the step")
     _near(lse, wlse, 2.0 ** -23 * wlse.abs() + 16 * E * sl / tau ** 2, "lse")
-    _near(d, wd, u * wd.abs() + 32 * E * sd + 2.0 ** -149, "dlogits") if logits.dtype != F16 else \
-        _near(d, wd, u * wd.abs() + 32 * E * sd + 2.0 ** -25, "dlogits")  # half a step of fp16's smallest
-    _near(d2, wd, u * wd.abs() + 32 * E * sd + (2.0 ** -149 if logits.dtype != F16 else 2.0 ** -25), "dlogits of the step")
+    # and half a step of the type's smallest values: bf16's step there is 2^-133, fp16's 2^-24, fp32's 2^-149 (a whole
+    # one allowed)
+    tiny = {F32: 2.0 ** -149, BF16: 2.0 ** -134, F16: 2.0 ** -25}[logits.dtype]
+    for got, what in ((d, "dlogits"), (d2, "dlogits of the step")):
+        _near(got, wd, u * wd.abs() + 32 * E * sd + tiny, what)
     assert not bool(d[~some].any()) and not bool(loss[~some].any())
     return loss, lse, d, loss2, d2
 
@@ -316,6 +318,58 @@ def _distill_check(logits, teacher, index, dloss, tau, out=None):
 def test_distill_sizes(rows, vocab, k, dtype):
     case = _distill_case(rows, vocab, k, dtype, rows + vocab + k)
     _distill_check(*case, 2.0)
+
+
+# rows enough for every compute unit and long enough for its registers: the kernel that holds them there
+RESIDENT = [(130, 33000, 7), (129, 40001, 20), (257, 65533, 5), (140, 131072, 64), (300, 70001, 1024)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("rows,vocab,k", RESIDENT)
+def test_distill_rows_held_in_registers(rows, vocab, k, dtype):
+    logits, teacher, index, dloss = _distill_case(rows, vocab, k, dtype, rows + k)
+    _, _, d, _, d2 = _distill_check(logits, teacher, index, dloss, 2.0)
+    _, d3 = B.byz_distill_loss_step(logits.clone(), teacher, index, dloss, 2.0)
+    assert _same_bits(d2, d3)
+    held = logits.clone()  # the gradient over the logits: the next row is loaded while this one is written
+    loss, d4 = B.byz_distill_loss_step(held, teacher, index, dloss, 2.0, out=held)
+    assert _same_bits(d4, d2)
+    wide = torch.full((rows, vocab + 11), 1.0e4, dtype=dtype, device=DEV)  # other alignments, row by row
+    part = wide[:, 3:vocab + 3]
+    part.copy_(logits)
+    out = torch.zeros((rows, vocab + 11), dtype=dtype, device=DEV)
+    _, d5 = B.byz_distill_loss_step(part, teacher, index, dloss, 2.0, out=out[:, 3:vocab + 3])
+    assert not bool(out[:, :3].any()) and not bool(out[:, vocab + 3:].any())
+    _distill_check(part, teacher, index, dloss, 2.0, out=out[:, 3:vocab + 3])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_distill_rows_held_in_registers_special_values(dtype):
+    rows, vocab, k = 140, 40000, 6
+    logits, teacher, index, dloss = _distill_case(rows, vocab, k, dtype, 41)
+    index = torch.where(index >= 0, index % 20000 + 15000, index)
+    clean = B.byz_distill_loss_step(logits, teacher, index, dloss, 1.0)
+    # values far above the first ones of every thread, and first values that are all banned
+    logits[3, :10000] = -1000.0
+    logits[4, :12000] = -math.inf
+    logits[5, ::2] = -math.inf
+    logits[5].scatter_(0, index[5].clamp_min(0).long(), 1.0)
+    logits[6] = (logits[6] + 3.0e4 if dtype == F32 else logits[6] * 64).round()
+    _distill_check(logits, teacher, index, dloss, 1.0)
+    logits[7, 39999] = math.nan
+    logits[8] = -math.inf
+    logits[1] = math.nan  # a row without entries
+    index[9, 0] = vocab
+    logits[10, 17] = math.inf
+    loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, 1.0)
+    for row in (7, 8, 9, 10):
+        assert bool(loss[row].isnan()) and bool(d[row].isnan().any())
+    assert bool(d[[7, 8, 9]].isnan().all())
+    assert float(loss[1]) == 0.0 and not bool(d[1].any())
+    assert torch.equal(loss[11:], clean[0][11:]) and torch.equal(d[11:], clean[1][11:])
+    logits[12, index[12, 0]] = -math.inf  # weight on a banned place
+    loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, 1.0)
+    assert float(loss[12]) == math.inf and bool(d[12].isfinite().all())
 
 
 @pytest.mark.parametrize("tau", [0.1, 1.0, 3.0, 20.0])
