@@ -114,19 +114,26 @@ struct Side {
         return (uint32_t)((std::min<int64_t>(row, outer - 1) * ld + piece * 8) * sizeof(T));
     }
 
-    // One 16-byte piece through registers, zeros from `ks` values of k on.  `at`: the step's corner.
-    static __device__ __forceinline__ void copy_piece(const T *at, int64_t ld, int64_t outer, int64_t ks, int number, char *lds) {
+    // The number-th 16-byte piece of a step, zeros from `ks` values of k on, and its byte in LDS.  `at`: the step's corner.
+    static __device__ __forceinline__ frag piece(const T *at, int64_t ld, int64_t outer, int64_t ks, int number) {
         frag v = {};
         if constexpr (COLUMNS) {
             constexpr int pieces = WIDTH / 8;
             const int row = number / pieces, piece = number % pieces;
             if (row < ks) v = *(const frag *)(at + row * ld + std::min<int64_t>(piece * 8, outer - 8));
-            *(frag *)(lds + row * WIDTH * 2 + (((piece >> 2) ^ column_turn<WIDTH>(row)) << 6) + (piece & 3) * 16) = v;
         } else {
             const int row = number / 8, piece = number % 8;
             if (piece * 8 < ks) v = *(const frag *)(at + std::min<int64_t>(row, outer - 1) * ld + piece * 8);
-            *(frag *)(lds + row_piece(row, piece)) = v;
         }
+        return v;
+    }
+    static __device__ __forceinline__ int place(int number) {
+        if constexpr (COLUMNS) {
+            constexpr int pieces = WIDTH / 8;
+            const int row = number / pieces, piece = number % pieces;
+            return row * WIDTH * 2 + (((piece >> 2) ^ column_turn<WIDTH>(row)) << 6) + (piece & 3) * 16;
+        }
+        return row_piece(number / 8, number % 8);
     }
 
     // Byte of this lane's first piece of the fragment of 32 outer indices that starts at `first`.
@@ -205,7 +212,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     extern __shared__ char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN, wn = wave % WN;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    char *const scratch = lds + STAGES * kBytes + wave * 4096;  // this wave's, for turning results
+    // this wave's, for turning results: in the stages' place, which nobody reads behind the last step's barrier
+    char *const scratch = lds + wave * 4096;
+    static_assert(kWaves * 4096 <= STAGES * kBytes, "");
     const int64_t move_a = KIND == kWeight ? kStep * p.a_ld : kStep, move_b = KIND == kForward ? kStep : kStep * p.b_ld;
     // kInput: steps of w_gate, then of w_up; `turn` is a multiple of the step
     const int steps = (int)((p.k + kStep - 1) / kStep), turn = KIND == kInput ? (int)(p.turn / kStep) : steps;
@@ -252,13 +261,28 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
             char *to = lds + t % STAGES * kBytes;
             const int64_t ks = values(t);
             const int thread = afresh(threadIdx.x);
-#pragma unroll 1
-            for (int i = thread; i < BM * 8; i += kWaves * 64) A::copy_piece(at_a, p.a_ld, at.outer_a, ks, i, to);
-#pragma unroll 1
-            for (int i = thread; i < BN * 8; i += kWaves * 64) {
-                const bool second = KIND == kForward && i >= BN * 4;
-                B::copy_piece(second ? at.corner_b2 + t * move_b : at_b, p.b_ld, at.outer_b, ks, second ? i - BN * 4 : i,
-                              to + BM * 128 + (second ? BN * 64 : 0));
+            // a thread's kLoads pieces, up to four at a time
+            constexpr int kBatch = BM == 256 ? 2 : kLoads % 4 == 0 ? 4 : 3, kPiecesA = BM * 8, kPiecesB = B::kChunks * 64;
+            static_assert(kLoads % kBatch == 0 && kPiecesA % (kWaves * 64) == 0 && kPiecesB % (kWaves * 64) == 0, "");
+#pragma unroll
+            for (int i0 = 0; i0 < kLoads; i0 += kBatch) {
+                frag v[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; u++) {
+                    const int first = (i0 + u) * kWaves * 64;
+                    if (first < kPiecesA)
+                        v[u] = A::piece(at_a, p.a_ld, at.outer_a, ks, first + thread);
+                    else
+                        v[u] = B::piece(first < kPiecesA + kPiecesB ? at_b : at.corner_b2 + t * move_b, p.b_ld, at.outer_b, ks,
+                                        (first - kPiecesA) % kPiecesB + thread);
+                }
+#pragma unroll
+                for (int u = 0; u < kBatch; u++) {
+                    const int first = (i0 + u) * kWaves * 64;
+                    char *side = to + (first < kPiecesA ? 0 : first < kPiecesA + kPiecesB ? kPiecesA * 16 : (kPiecesA + kPiecesB) * 16);
+                    const int number = first < kPiecesA ? first : (first - kPiecesA) % kPiecesB;
+                    *(frag *)(side + (first < kPiecesA ? A::place(number + thread) : B::place(number + thread))) = v[u];
+                }
             }
         }
     };
@@ -409,18 +433,35 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     });
 }
 
-// Up to 16 tokens.  Block: 16 outputs, kSkinnyWaves shares of k.
-constexpr int kSkinnyWaves = 8;
+// Up to 16 tokens.  A block has 8 outputs: a matrix instruction's 16 columns are their gate rows and their up rows.  Its waves
+// share k, 64 values (a cache line of a row) at a time.  Blocks of 16 outputs, with an instruction for each weight, are half as
+// many: 344 of them on 256 compute units took 11.3 us for a token of 2048 -> 5504.
+constexpr int kSkinnyWaves = 8, kSkinnyOut = 8;
 template <typename T>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(Product p) {
     using frag = typename Frag<T>::type;
-    __shared__ f32x4 part[2][kSkinnyWaves][64];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, n = std::min<int64_t>(n0 + lane % 16, p.n - 1);
-    const T *g = (const T *)p.b + n * p.b_ld, *u = (const T *)p.b2 + n * p.b_ld;
-    const bool token = lane % 16 < p.m;
-    const T *x = (const T *)p.a + (token ? lane % 16 : 0) * p.a_ld;
-    f32x4 accg = {}, accu = {};
+    __shared__ f32x4 part[kSkinnyWaves][64];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, col = lane % 16;
+    const int64_t n0 = (int64_t)blockIdx.x * kSkinnyOut, n = std::min<int64_t>(n0 + col % 8, p.n - 1);
+    const T *w = (const T *)(col < 8 ? p.b : p.b2) + n * p.b_ld;
+    const bool token = col < p.m;
+    const T *x = (const T *)p.a + (token ? col : 0) * p.a_ld;
+    f32x4 acc = {};
+    constexpr int kAhead = 4, kApart = kSkinnyWaves * 64;
+    int64_t k0 = wave * 64;
+    if (p.direct)
+        for (; k0 + (kAhead - 1) * kApart + 64 <= p.k; k0 += kAhead * kApart) {
+            frag a[2 * kAhead], b[2 * kAhead];
+#pragma unroll
+            for (int u = 0; u < 2 * kAhead; u++) {
+                const int64_t k = k0 + u / 2 * kApart + u % 2 * 32 + lane / 16 * 8;
+                b[u] = *(const frag *)(w + k);
+                a[u] = frag{};
+                if (token) a[u] = *(const frag *)(x + k);
+            }
+#pragma unroll
+            for (int u = 0; u < 2 * kAhead; u++) acc = mma16(a[u], b[u], acc);
+        }
     auto piece = [&](const T *src, int64_t k) {
         frag v;
         if (p.direct && k + 8 <= p.k) {
@@ -431,28 +472,27 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(Product p) {
         }
         return v;
     };
-    // steps of 32 values, dealt to the waves in turn
-    for (int64_t k0 = wave * 32; k0 < p.k; k0 += kSkinnyWaves * 32) {
-        const int64_t k = k0 + lane / 16 * 8;
-        frag a = piece(x, k), bg = piece(g, k), bu = piece(u, k);
-        if (!token) a = frag{};
-        accg = mma16(a, bg, accg);
-        accu = mma16(a, bu, accu);
-    }
-    part[0][wave][lane] = accg, part[1][wave][lane] = accu;
+    for (; k0 < p.k; k0 += kApart)
+        for (int half = 0; half < 2; half++) {
+            const int64_t k = k0 + half * 32 + lane / 16 * 8;
+            frag a = piece(x, k), b = piece(w, k);
+            if (!token) a = frag{};
+            acc = mma16(a, b, acc);
+        }
+    part[wave][lane] = acc;
     __syncthreads();
     if (wave == 0) {
-        for (int w = 1; w < kSkinnyWaves; w++) accg += part[0][w][lane], accu += part[1][w][lane];
-        const int64_t col = n0 + lane % 16;
+        for (int v = 1; v < kSkinnyWaves; v++) acc += part[v][lane];
         with_act(p.act, [&](auto act) {
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-                const int64_t row = lane / 16 * 4 + r;
-                if (row >= p.m || col >= p.n) continue;
-                ((T *)p.out)[row * p.out_ld + col] = round_to<T>(act_value<act.value>(accg[r]) * accu[r]);
+                const float up = __shfl_xor(acc[r], 8);  // of lanes with a gate
+                const int64_t row = lane / 16 * 4 + r, at = n0 + col;
+                if (col >= 8 || row >= p.m || at >= p.n) continue;
+                ((T *)p.out)[row * p.out_ld + at] = round_to<T>(act_value<act.value>(acc[r]) * up);
                 if (p.gate) {
-                    p.gate[row * p.gate_ld + col] = accg[r];
-                    p.up[row * p.gate_ld + col] = accu[r];
+                    p.gate[row * p.gate_ld + at] = acc[r];
+                    p.up[row * p.gate_ld + at] = up;
                 }
             }
         });
@@ -521,8 +561,7 @@ unsigned grid_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads 
 
 template <typename T, int BM, int BN, int WM, int WN, Kind KIND, int STAGES>
 int launch_tile(Product p, hipStream_t s) {
-    constexpr int kOut = KIND == kForward ? BN / 2 : BN, kThreads = WM * WN * 64;
-    constexpr int kLds = STAGES * (BM + BN) * 128 + WM * WN * 4096;
+    constexpr int kOut = KIND == kForward ? BN / 2 : BN, kThreads = WM * WN * 64, kLds = STAGES * (BM + BN) * 128;
     const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + kOut - 1) / kOut, tiles = tm * tn * (KIND == kWeight ? 2 : 1);
     if (tiles > INT32_MAX / kThreads) return BYZ_EUNSUPPORTED;
     p.tiles_m = (int)tm, p.tiles_n = (int)tn;
@@ -538,15 +577,46 @@ int launch_tile(Product p, hipStream_t s) {
     return BYZ_OK;
 }
 
+// The tiles that a product can be cut into: how many blocks of them a compute unit holds, and what a step takes of
+// its time (us, measured on products that fill the card).  Fewer than two blocks leave room for more stages.
+struct Shape {
+    int bm, bn, stages, resident;
+    double step;
+};
+constexpr Shape kShapes[] = {{256, 256, 2, 1, 1.85}, {128, 128, 2, 2, 0.6}, {128, 128, 4, 1, 0.6}, {64, 128, 3, 2, 0.35},
+                             {64, 128, 6, 1, 0.35},  {64, 64, 4, 2, 0.22},  {64, 64, 8, 1, 0.22}};
+
+// The shape of the shortest estimated time: rounds of blocks, each so many steps and 3 us for its first loads and its stores; a step
+// takes the blocks' products on a compute unit or, where those are shorter, the way from memory (1 us) over the stages ahead.
+int best_shape(int64_t m, int64_t across, int64_t k, int copies, bool square64) {
+    int best = 0;
+    double best_time = 0.0;
+    for (int i = 0; i < (square64 ? 7 : 5); i++) {
+        const Shape &c = kShapes[i];
+        const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((across + c.bn - 1) / c.bn) * copies;
+        const int64_t rounds = (tiles + 256 * c.resident - 1) / (256 * c.resident), together = std::min<int64_t>(c.resident, (tiles + 255) / 256);
+        const double step = std::max(together * c.step, 1.0 / (c.stages - 1));
+        const double time = rounds * ((k + kStep - 1) / kStep * step + 3.0);
+        if (i == 0 || time < best_time) best = i, best_time = time;
+    }
+    return best;
+}
+
 // Operands' rows start at 16-byte boundaries and have whole 16-byte pieces.
 template <typename T, Kind KIND>
 int launch_product(const Product &p, hipStream_t s) {
-    const int64_t across = KIND == kInput ? p.n : 2 * p.n;
-    auto tiles = [&](int bm, int bn) { return ((p.m + bm - 1) / bm) * ((across + bn - 1) / bn); };
-    if (tiles(256, 256) >= 192) return launch_tile<T, 256, 256, 2, 4, KIND, 2>(p, s);
-    if (tiles(128, 128) >= 192) return launch_tile<T, 128, 128, 2, 2, KIND, 2>(p, s);
-    if (KIND == kForward || tiles(64, 128) >= 192) return launch_tile<T, 64, 128, 2, 2, KIND, 2>(p, s);
-    if constexpr (KIND != kForward) return launch_tile<T, 64, 64, 2, 2, KIND, 4>(p, s);
+    switch (best_shape(p.m, KIND == kForward ? 2 * p.n : p.n, p.k, KIND == kWeight ? 2 : 1, KIND != kForward)) {
+        case 0: return launch_tile<T, 256, 256, 2, 4, KIND, 2>(p, s);
+        case 1: return launch_tile<T, 128, 128, 2, 2, KIND, 2>(p, s);
+        case 2: return launch_tile<T, 128, 128, 2, 2, KIND, 4>(p, s);
+        case 3: return launch_tile<T, 64, 128, 2, 2, KIND, 3>(p, s);
+        case 4: return launch_tile<T, 64, 128, 2, 2, KIND, 6>(p, s);
+        default: break;
+    }
+    if constexpr (KIND != kForward)
+        return best_shape(p.m, p.n, p.k, KIND == kWeight ? 2 : 1, true) == 5 ? launch_tile<T, 64, 64, 2, 2, KIND, 4>(p, s)
+                                                                             : launch_tile<T, 64, 64, 2, 2, KIND, 8>(p, s);
+    return BYZ_EINTERNAL;
 }
 
 int64_t padded(int64_t v) { return (v + 63) / 64 * 64; }
@@ -623,7 +693,7 @@ int forward(Call c, Product p, hipStream_t s) {
         return launch_product<T, kForward>(p, s);
     }
     p.direct = pieces(c.x, 8, c.x_ld) && pieces(c.w_gate, 8, c.w_ld) && pieces(c.w_up, 8, c.w_ld);
-    skinny_kernel<T><<<(unsigned)((p.n + 15) / 16), kSkinnyWaves * 64, 0, s>>>(p);
+    skinny_kernel<T><<<(unsigned)((p.n + kSkinnyOut - 1) / kSkinnyOut), kSkinnyWaves * 64, 0, s>>>(p);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
