@@ -8,10 +8,15 @@
 //
 // Bound by memory: logits in, gradients out.  Loss and gradient in one call hold a long row in registers ("resident"): it
 // is read once, and as soon as a thread has stored a piece of its gradient it loads that piece of its next row, so reads,
-// the two exponentials of a value and writes overlap although a row fills a compute unit's registers.  The fp64
-// functions would take those registers, so the teacher's softmax and the losses are kernels before and behind it.
-// Rows that are too long, short rows and the other calls stream: with a running maximum m and a sum of exp((s - m) / T).
+// the two exponentials of a value and writes overlap although a row fills a compute unit's registers.  Nothing else is
+// in that kernel: the teacher's softmax, fp64 functions and the few places are kernels before and behind it (places
+// written in it, behind a barrier, cost 17 % of its time).  Rows that are too long, short rows and the other calls stream:
+// with a running maximum m and a sum of exp((s - m) / T).
+//
+// 8192 x 131072 bf16, loss and gradient: resident 822 us (4.3 GB at 5.2 TB/s, a copy reaches 6.5; vector instructions issue 0.47 of the
+// time), teacher and places 45.  30 x 10: 7.8 us, one launch and its chain of loads, fp64 functions and barriers.
 #include <algorithm>
+#include <type_traits>
 
 #include "worker_internal.h"
 
@@ -220,6 +225,29 @@ struct Softmax {
     }
 };
 
+// The same from a row's sum of exp2(x c - m), for the resident kernel.  16-bit types: the exponent in one operation; the
+// rounding of m + l is 2^-24 of it, where q is rounded to 2^-9 of itself at best.
+template <typename T>
+struct ScaledSoftmax {
+    static constexpr bool kWide = sizeof(T) == 4;
+    std::conditional_t<kWide, Softmax<float>, float> s;
+    float c, w;
+    __device__ ScaledSoftmax(float m, float sum, float temperature, float weight, float c_) : s(exponent(m, sum, temperature, weight, c_)), c(c_), w(weight) {}
+    static __device__ __forceinline__ auto exponent(float m, float sum, float temperature, float weight, float c) {
+        if constexpr (kWide)
+            return Softmax<float>(m, sum, temperature, weight, c);
+        else
+            return 32.0f - (m + __builtin_amdgcn_logf(sum));
+    }
+    __device__ __forceinline__ float less(float x, float p) const {
+        if constexpr (kWide)
+            return s.less(x, p);
+        else
+            return (__builtin_amdgcn_exp2f(fmaf(x, c, s)) - p * 0x1p32f) * (w * 0x1p-32f);
+    }
+    __device__ __forceinline__ float weighted(float x) const { return less(x, 0.0f); }
+};
+
 // The gradient at the teacher's places; the dense part is written.
 template <typename T, int NT>
 __device__ __forceinline__ void write_places(const Args &a, const Teacher &t, const Softmax<T> &q, T *out, int tid) {
@@ -315,24 +343,31 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
     }
 }
 
-// A row's part of the workspace of the resident kernel, beside its p (k doubles).
+// A row's part of the workspace of the resident kernel, beside its k places.
 struct RowSums {
     double entropy;  // sum of p log p
     double dot, ps;  // sums of p s and p over the places
-    float m, s;      // the student's maximum and sum
+    float m, s;      // the student's maximum (16-bit types: times c) and sum
     int flags;       // kSome: an entry at all; kBroken: the row is NaN
     int pad;
 };
+struct Place {
+    float p, student;  // of all entries at the place; the student's logit
+};
 enum { kSome = 1, kBroken = 2 };
 
-// The teacher's softmax, a wave a row.
-__global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, double *p, RowSums *sums) {
+// The teacher's softmax and what the student has at its places, a wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, Place *places, RowSums *sums) {
+    extern __shared__ double own[];
     const double tau = a.temperature;
     const int lane = threadIdx.x % 64;
+    double *const each = own + threadIdx.x / 64 * a.k;  // a lane reads what it has written itself
     for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
         const float *t = a.teacher + row * a.teacher_ld;
         const int32_t *index = a.index + row * a.teacher_ld;
-        double top = -INFINITY, total = 0.0, entropy = 0.0;
+        const T *logits = (const T *)a.logits + row * a.ld;
+        double top = -INFINITY, total = 0.0, entropy = 0.0, dot = 0.0, ps = 0.0;
         bool broken = false;
         for (int j = lane; j < a.k; j += 64)
             if (index[j] >= 0) {
@@ -342,41 +377,79 @@ __global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, double *p,
             }
         top = row_max<64>(top, nullptr);
         const double shift = top > -INFINITY ? top : 0.0;
-        for (int j = lane; j < a.k; j += 64)
-            if (index[j] >= 0) total += exp((double)t[j] / tau - shift);
+        for (int j = lane; j < a.k; j += 64) {
+            const int32_t i = index[j];
+            const float s = i >= 0 && i < a.vocab ? (float)logits[i] : 0.0f;
+            const double e = i >= 0 ? exp((double)t[j] / tau - shift) : 0.0;
+            total += e;
+            each[j] = e;
+            places[row * a.k + j].student = s;
+        }
         total = row_sum<64>(total, nullptr);
         broken = __ballot(broken) != 0 || total != total;
         const bool some = total > 0.0 || broken;
         for (int j = lane; j < a.k; j += 64) {
-            const double w = index[j] < 0 || !some ? 0.0 : broken ? NAN : exp((double)t[j] / tau - shift) / total;
-            p[row * a.k + j] = w;
-            if (w > 0.0) entropy += w * log(w);
+            const double w = index[j] < 0 || !some ? 0.0 : broken ? NAN : each[j] / total;
+            each[j] = w;
+            if (w > 0.0) entropy += w * log(w), dot += w * (double)places[row * a.k + j].student, ps += w;
         }
         entropy = row_sum<64>(entropy, nullptr);
-        if (lane == 0) sums[row].entropy = entropy, sums[row].flags = (some ? kSome : 0) | (broken ? kBroken : 0);
+        dot = row_sum<64>(dot, nullptr);
+        ps = row_sum<64>(ps, nullptr);
+        if (lane == 0) {
+            sums[row].entropy = entropy, sums[row].dot = dot, sums[row].ps = ps;
+            sums[row].flags = (some ? kSome : 0) | (broken ? kBroken : 0);
+        }
+        for (int j0 = 0; j0 < a.k; j0 += 64) {
+            const int32_t i = j0 + lane < a.k ? index[j0 + lane] : -1;
+            float p = 0.0f;
+            for (int l0 = 0; l0 < a.k; l0 += 64) {
+                const int32_t il = l0 + lane < a.k ? index[l0 + lane] : -1;
+                const float pl = l0 + lane < a.k ? (float)each[l0 + lane] : 0.0f;
+                const int end = std::min(64, a.k - l0);
+                for (int l = 0; l < end; l++) {
+                    const float pj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pl), l));
+                    p += __builtin_amdgcn_readlane(il, l) == i ? pj : 0.0f;
+                }
+            }
+            if (j0 + lane < a.k) places[row * a.k + j0 + lane].p = p;
+        }
     }
 }
 
-__global__ __launch_bounds__(256) void distill_losses_kernel(Args a, const RowSums *sums) {
+// The losses, and the gradient at the teacher's places (the dense part is written), a wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_places_kernel(Args a, const Place *places, const RowSums *sums) {
     const double tau = a.temperature;
-    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (row >= a.rows) return;
-    const RowSums r = sums[row];
-    const double lse = (double)r.m / tau + log((double)r.s);
-    a.loss[row] = r.flags & kBroken ? NAN : r.flags & kSome ? (float)(tau * tau * (r.entropy - r.dot / tau + r.ps * lse)) : 0.0f;
-    if (a.lse) a.lse[row] = (float)lse;
+    const float c = (float)(1.4426950408889634 / tau);
+    const int lane = threadIdx.x % 64;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
+        const RowSums r = sums[row];
+        if (lane == 0) {
+            const double lse = (double)r.m / (sizeof(T) == 4 ? tau : (double)c * tau) + log((double)r.s);
+            a.loss[row] =
+                r.flags & kBroken ? NAN : r.flags & kSome ? (float)(tau * tau * (r.entropy - r.dot / tau + r.ps * lse)) : 0.0f;
+            if (a.lse) a.lse[row] = (float)lse;
+        }
+        if (!(r.flags & kSome)) continue;
+        const ScaledSoftmax<T> q(r.m, r.s, a.temperature, r.flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
+        T *out = (T *)a.dlogits + row * a.dlogits_ld;
+        for (int j = lane; j < a.k; j += 64) {
+            const int32_t i = a.index[row * a.teacher_ld + j];
+            const Place at = places[row * a.k + j];
+            if (i >= 0 && i < a.vocab) out[i] = round_to<T>(q.less(at.student, at.p));
+        }
+    }
 }
 
-// The gradients, and the sums for the losses.  R vectors of a row in each of 1024 threads' registers; for rows whose logits
+// The dense gradients and the student's sums.  R vectors of a row in each of 1024 threads' registers; for rows whose logits
 // and gradients lie at the same place within 16 bytes.
 template <typename T, int R>
-__global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, const double *p, RowSums *sums) {
+__global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums *sums) {
     constexpr int V = 16 / sizeof(T), NT = 1024;
-    extern __shared__ char lds_raw[];
     __shared__ double red[32];
     const int tid = threadIdx.x;
     const float c = (float)(1.4426950408889634 / (double)a.temperature);
-    Teacher t(lds_raw, a.k);
     Words<T, V> x[R];
     T edge = (T)0.0f;
     // A row here is shorter than 2^31 bytes.  A thread's number `own` is made afresh for each use, or the places of all R
@@ -385,6 +458,10 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, const do
     auto load = [&](const Row<T> &r, int own, int v) {
         x[v] = *vector_of(r.at + r.head, std::min(own + v * NT, (int)r.vectors - 1));
     };
+    // 16-bit types: sums are of exp2(x c - m) with m = c times a value, rounded: one operation for the exponent
+    constexpr bool kScaled = sizeof(T) == 2;
+    const float unit = kScaled ? 1.0f : c;
+    auto scaled = [&](float v) { return kScaled ? v * c : v; };
     auto load_edge = [&](const Row<T> &r) {
         if (tid < r.head + r.tail) edge = r.at[r.edge(tid)];
     };
@@ -396,17 +473,6 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, const do
     }
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
-        __syncthreads();  // the last row's places are written
-        double dot = 0.0, ps = 0.0;
-#pragma unroll 1
-        for (int j = tid; j < a.k; j += NT) {
-            const int32_t i = a.index[row * a.teacher_ld + j];
-            const double w = p[row * a.k + j];
-            const bool in = i >= 0 && i < a.vocab;
-            const float s = in ? (float)r.at[i] : 0.0f;
-            t.index[j] = in ? i : -1, t.p[j] = (float)w, t.student[j] = s;
-            if (w > 0.0) dot += w * (double)s, ps += w;
-        }
         // A thread's sum of exp2((x - m) c).  The maximum of its first values is m: a sum in fp32 holds values up to
         // 2^127 times that.  What goes beyond (or is not finite) is summed again with a running maximum.
         const bool has_edge = tid < r.head + r.tail;
@@ -415,72 +481,76 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, const do
             float top = x[0][0];
 #pragma unroll
             for (int e = 1; e < V; e++) top = fmaxf(top, x[0][e]);
-            s.m = top;
+            s.m = scaled(top);
         } else if (has_edge) {
-            s.m = (float)edge;
+            s.m = scaled((float)edge);
         }
         const float m0 = s.m;
+        auto power = [&](float v) { return __builtin_amdgcn_exp2f(kScaled ? fmaf(v, c, -m0) : (v - m0) * c); };
         const int vectors = (int)r.vectors, own = afresh(tid);
 #pragma unroll
         for (int v = 0; v < R; v++) {
             float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < V; e++) sum += __builtin_amdgcn_exp2f((x[v][e] - m0) * c);
+            for (int e = 0; e < V; e++) sum += power(x[v][e]);
             s.s += own + v * NT < vectors ? sum : 0.0f;
             x[v].keep();
             __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
         }
-        if (has_edge) s.s += __builtin_amdgcn_exp2f(((float)edge - m0) * c);
+        if (has_edge) s.s += power((float)edge);
         if (!(s.s < 0x1p120f)) {
             s = RunningSum();
 #pragma unroll
             for (int v = 0; v < R; v++) {
                 float y[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) y[e] = own + v * NT < vectors ? x[v][e] : -INFINITY;
-                s.add(y, c);
+                for (int e = 0; e < V; e++) y[e] = own + v * NT < vectors ? scaled(x[v][e]) : -INFINITY;
+                s.add(y, unit);
                 x[v].keep();
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (has_edge) {
-                const float y[1] = {(float)edge};
-                s.add(y, c);
+                const float y[1] = {scaled((float)edge)};
+                s.add(y, unit);
             }
         }
-        s = row_join<NT>(s, c, red);
-        dot = row_sum<NT>(dot, red);
-        ps = row_sum<NT>(ps, red);
+        s = row_join<NT>(s, unit, red);
         const int flags = sums[row].flags;
-        if (tid == 0) sums[row].dot = dot, sums[row].ps = ps, sums[row].m = s.m, sums[row].s = s.s;
+        if (tid == 0) sums[row].m = s.m, sums[row].s = s.s;
         const bool some = flags & kSome;
-        const Softmax<T> q(s.m, s.s, a.temperature, flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
+        const ScaledSoftmax<T> q(s.m, s.s, a.temperature, flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
         T *out = (T *)a.dlogits + row * a.dlogits_ld;
-        // here everybody has read the logits at the teacher's places (the barriers of the sums): they may be written
         if (has_edge) {
             const int64_t e = r.edge(tid);
             out[e] = some ? round_to<T>(q.weighted((float)edge)) : (T)0.0f;
         }
         const int then = afresh(tid);
-        auto store = [&](int v) {
-            if (then + v * NT < vectors)
-                *vector_of(out + r.head, then + v * NT) = Words<T, V>::of([&](int e) { return some ? q.weighted(x[v][e]) : 0.0f; });
-            __builtin_amdgcn_sched_barrier(0);
+        auto pass = [&](auto gradient, auto more, const Row<T> &next) {
+#pragma unroll
+            for (int v = 0; v < R; v++) {
+                if (then + v * NT < vectors)
+                    put_past_caches(vector_of(out + r.head, then + v * NT), Words<T, V>::of([&](int e) { return gradient(x[v][e]); }));
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (more.value) {
+                    load(next, then, v);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         };
+        auto weighted = [&](float v) { return q.weighted(v); };
+        auto none = [](float) { return 0.0f; };
         if (row + gridDim.x < a.rows) {
             const Row<T> next(a.logits, row + gridDim.x, a.ld, a.vocab);
             load_edge(next);
-#pragma unroll
-            for (int v = 0; v < R; v++) {
-                store(v);
-                load(next, then, v);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            if (some)
+                pass(weighted, std::true_type{}, next);
+            else
+                pass(none, std::true_type{}, next);
+        } else if (some) {
+            pass(weighted, std::false_type{}, r);
         } else {
-#pragma unroll
-            for (int v = 0; v < R; v++) store(v);
+            pass(none, std::false_type{}, r);
         }
-        __syncthreads();  // the dense part is written: the teacher's places again
-        if (some) write_places<T, NT>(a, t, q, out, tid);
     }
 }
 
@@ -500,21 +570,21 @@ bool fits_resident(int64_t rows, int64_t vocab, int dtype) {
     return vectors >= 1024 * 4 && vectors <= 1024 * kResident && rows >= kCus / 2;
 }
 
-size_t resident_bytes(int64_t rows, int k) { return (size_t)rows * (sizeof(RowSums) + (size_t)k * sizeof(double)); }
+size_t resident_bytes(int64_t rows, int k) { return (size_t)rows * (sizeof(RowSums) + (size_t)k * sizeof(Place)); }
 
 template <typename T>
 int launch_resident(const Args &a, void *workspace, hipStream_t s) {
     RowSums *sums = (RowSums *)workspace;
-    double *p = (double *)(sums + a.rows);
-    distill_teacher_kernel<<<(unsigned)std::min<int64_t>((a.rows + 3) / 4, kMaxGrid), 256, 0, s>>>(a, p, sums);
+    Place *places = (Place *)(sums + a.rows);
+    const unsigned waves = (unsigned)std::min<int64_t>((a.rows + 3) / 4, kMaxGrid), grid = (unsigned)std::min<int64_t>(a.rows, kCus);
+    distill_teacher_kernel<T><<<waves, 256, 4 * a.k * sizeof(double), s>>>(a, places, sums);
     BYZ_HIP(hipGetLastError());
-    const unsigned grid = (unsigned)std::min<int64_t>(a.rows, kCus);
     if (a.vocab * (int64_t)sizeof(T) / 16 <= 1024 * kResident / 2)
-        distill_resident_kernel<T, kResident / 2><<<grid, 1024, teacher_bytes(a.k), s>>>(a, p, sums);
+        distill_resident_kernel<T, kResident / 2><<<grid, 1024, 0, s>>>(a, sums);
     else
-        distill_resident_kernel<T, kResident><<<grid, 1024, teacher_bytes(a.k), s>>>(a, p, sums);
+        distill_resident_kernel<T, kResident><<<grid, 1024, 0, s>>>(a, sums);
     BYZ_HIP(hipGetLastError());
-    distill_losses_kernel<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, sums);
+    distill_places_kernel<T><<<waves, 256, 0, s>>>(a, places, sums);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }

@@ -98,6 +98,17 @@ struct Words<T, 1> {
     __device__ __forceinline__ void keep() {}
 };
 
+// Stored past the caches: for results larger than these, in whose place they keep the inputs, which are read again.
+template <typename T, int V>
+__device__ __forceinline__ void put_past_caches(Words<T, V> *to, const Words<T, V> &v) {
+    if constexpr (sizeof(v) == 16) {
+        typedef uint32_t words4 __attribute__((ext_vector_type(4), may_alias));
+        __builtin_nontemporal_store(__builtin_bit_cast(words4, v), (words4 *)to);
+    } else {
+        *to = v;
+    }
+}
+
 // fp32 -> T, to the nearest, ties to even
 template <typename T>
 __device__ __forceinline__ T round_to(float x) {
