@@ -16,8 +16,15 @@
 //
 // Bound by memory: 2 values moved per value forward, 3 backward, a dozen operations each.  Where a slice
 // of a sample fits the registers of one block ("whole") everything is read once.  Larger samples are cut into
-// chunks: a first kernel writes their statistics, a second joins them in chunk order, a third reads the chunks again.
+// chunks: a first kernel writes their statistics, a second joins them in chunk order, a third reads the chunks again and
+// stores past the caches, which then still hold inputs for the next pass (backward sums behind the forward pass 46.6 / 38.4 us,
+// gradients 54.9 / 48.8, without / with that).  Registers for 200 KB slices, 16 vectors a thread, spill and were slower (64 us
+// for 58 in three kernels on 64 x 56 x 56 x 256 bf16).
 // No atomics.
+//
+// us, traced: 64 x 112 x 112 x 64 fp16 forward: statistics 22.5 (103 MB, 4.6 TB/s), join 4.7, pass 36.4 (206 MB, 5.6 TB/s).
+// 64 x 56 x 56 x 256 bf16: forward 20.4 + 4.8 + 33.3; backward sums 38.4 (206 MB, 5.4 TB/s), totals 5.4, pass 48.8 (309 MB, 6.3 TB/s),
+// parameters 4.9.  30 x 32 x 32 x 64 bf16: 12.1 forward, 16.0 backward, one block's chain of loads, joins and stores.
 #include <algorithm>
 #include <type_traits>
 
@@ -66,6 +73,16 @@ int widest_vec(int elem, int64_t c, std::initializer_list<View> views) {
         if (ok) return vec;
     }
     return 1;
+}
+
+// Positions of a chunk of a large sample: as many as leave `blocks` of them.  Blocks that sum end in joins, which cost less
+// over long chunks; those that only pass over the data again are better short.  us on 64 x 56 x 56 x 256 bf16, 512 / 2048 blocks and
+// more: sums of the backward pass 46.5 / 51.6, forward's 21.1 / 25.1; gradients 63.2 / 55.6.
+constexpr int64_t kSumBlocks = 700, kPassBlocks = 2048;
+int64_t chunk_of(const Plan &q, int64_t slices, int64_t blocks) {
+    int depth = kDepth;
+    while (depth > 8 && q.n * slices * ((q.p + (int64_t)q.ty * depth - 1) / ((int64_t)q.ty * depth)) < blocks) depth /= 2;
+    return (int64_t)q.ty * depth;
 }
 
 // False: more tiles than can be counted.
@@ -128,14 +145,11 @@ bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int ele
     if (!q.r) {
         q.threads = 256;
         q.ty = q.threads / q.tx;
-        // long chunks, as long as every compute unit gets eight
-        int depth = kDepth;
-        while (depth > 8 && n * slices * ((p + (int64_t)q.ty * depth - 1) / ((int64_t)q.ty * depth)) < 2048) depth /= 2;
-        q.chunk = (int64_t)q.ty * depth;
+        q.chunk = chunk_of(q, slices, kSumBlocks);
         chunks = (p + q.chunk - 1) / q.chunk;
     }
     int64_t tiles;
-    if (__builtin_mul_overflow(n, slices, &tiles) || __builtin_mul_overflow(tiles, chunks, &tiles) || tiles > INT32_MAX ||
+    if (__builtin_mul_overflow(n, slices, &tiles) || __builtin_mul_overflow(tiles, chunks, &tiles) || tiles > (q.r ? INT32_MAX : INT32_MAX / 4) ||
         n * groups > INT32_MAX)
         return false;
     q.slices = (uint32_t)slices, q.chunks = (uint32_t)chunks, q.tiles = (uint32_t)tiles;
@@ -144,6 +158,17 @@ bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int ele
 }
 
 bool whole(const Plan &q) { return q.r > 0; }
+
+// The call for the kernel that passes over a large sample again.  Its chunks are shorter by 32 / 8 at most: a tile's number still fits.
+template <typename A>
+A pass_again(A a) {
+    Plan &q = a.q;
+    q.chunk = chunk_of(q, q.slices, kPassBlocks);
+    q.chunks = (uint32_t)((q.p + q.chunk - 1) / q.chunk);
+    q.tiles = (uint32_t)q.n * q.slices * q.chunks;
+    q.per_xcd = (q.tiles + 7) / 8;
+    return a;
+}
 
 // Mean, count, squared distances from it.
 struct Stat {
@@ -557,7 +582,7 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(Args a) {
         const int64_t pixel[1] = {a.xp};
         with_act(a.act, [&](auto act) {
             each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Words<T, V>(&x)[1]) {
-                *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[0]);
+                put_past_caches((Words<T, V> *)(to + (int64_t)r * q.ty * a.op), normalised<act.value>(f, x[0]));
             });
         });
     }
@@ -750,7 +775,7 @@ __global__ __launch_bounds__(256) void norm_backward_apply_kernel(Args a) {
         const int64_t pixel[2] = {a.xp, a.dp};
         with_act(a.act, [&](auto act) {
             each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Words<T, V>(&v)[2]) {
-                *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, v[0], v[1]);
+                put_past_caches((Words<T, V> *)(to + (int64_t)r * q.ty * a.op), gradient<act.value>(f, k1, k0, v[0], v[1]));
             });
         });
     }
@@ -800,12 +825,14 @@ int launch_forward(const Args &a, hipStream_t s) {
         case 2: norm_whole_kernel<T, V, 2><<<grid, threads, lds, s>>>(a); break;
         case 4: norm_whole_kernel<T, V, 4><<<grid, threads, lds, s>>>(a); break;
         case 8: norm_whole_kernel<T, V, 8><<<grid, threads, lds, s>>>(a); break;
-        default:
+        default: {
             norm_stats_kernel<T, V><<<grid, threads, lds, s>>>(a);
             BYZ_HIP(hipGetLastError());
             norm_join_kernel<<<grid_of((a.q.n * a.q.groups + 3) / 4), 256, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
-            norm_apply_kernel<T, V><<<grid, threads, 0, s>>>(a);
+            const Args again = pass_again(a);
+            norm_apply_kernel<T, V><<<grid_of((int64_t)8 * again.q.per_xcd), threads, 0, s>>>(again);
+        }
     }
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
@@ -820,12 +847,14 @@ int launch_backward(const Args &a, hipStream_t s) {
         case 2: norm_backward_whole_kernel<T, V, 2><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
         case 4: norm_backward_whole_kernel<T, V, 4><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
         case 8: norm_backward_whole_kernel<T, V, 8><<<grid, threads, sum_bytes(a.q, 4), s>>>(a); break;
-        default:
+        default: {
             norm_backward_sums_kernel<T, V><<<grid, threads, sum_bytes(a.q, 2), s>>>(a);
             BYZ_HIP(hipGetLastError());
             norm_backward_totals_kernel<<<grid_of(a.q.n * a.q.groups), 256, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
-            norm_backward_apply_kernel<T, V><<<grid, threads, 0, s>>>(a);
+            const Args again = pass_again(a);
+            norm_backward_apply_kernel<T, V><<<grid_of((int64_t)8 * again.q.per_xcd), threads, 0, s>>>(again);
+        }
     }
     BYZ_HIP(hipGetLastError());
     if (a.dgamma) {
