@@ -1,4 +1,4 @@
-"""Builds libbyzshield.so (HIP kernels + host library + C-ABI) for gfx950, in-tree."""
+"""Builds libbyzshield.so (HIP kernels + host library + C-ABI) for gfx950, and _worker_calls.so, in-tree."""
 import concurrent.futures
 import os
 import subprocess
@@ -16,6 +16,26 @@ KERNELS = os.path.join(CSRC, "kernels.hip")
 KERNEL_PARTS = (2, 1, 18, 7, 4, 22, 25, 14, 24, 15, 17, 6, 5, 23, 20, 21, 8, 10, 16, 9, 11, 19, 3, 13, 12, 0)
 OTHER_SOURCES = [os.path.join(CSRC, name) for name in
                  ("group_norm.hip", "gated_ffn.hip", "distill.hip", "krum.hip", "host.cpp")]
+
+
+CALLS = os.path.join(PKG, "_worker_calls.so")
+
+
+def build_calls(verbose=False):
+    """Compiles the Python module of the worker operators' common calls against torch's headers (ten seconds)."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           os.path.join(CSRC, "worker_calls.cpp"), "-o", CALLS, "-L", PKG, "-lbyzshield",
+           "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return CALLS
 
 
 def build(verbose=False):
@@ -56,6 +76,7 @@ def build(verbose=False):
     if verbose:
         print(" ".join(link), flush=True)
     subprocess.run(link, check=True)
+    build_calls(verbose)
     return LIB
 
 
