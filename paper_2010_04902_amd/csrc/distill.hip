@@ -10,11 +10,12 @@
 // is read once, and as soon as a thread has stored a piece of its gradient it loads that piece of its next row, so reads,
 // the two exponentials of a value and writes overlap although a row fills a compute unit's registers.  Nothing else is
 // in that kernel: the teacher's softmax, fp64 functions and the few places are kernels before and behind it (places
-// written in it, behind a barrier, cost 17 % of its time).  Rows that are too long, short rows and the other calls stream:
+// written in it, behind a barrier, cost 17 % of its time).  Short rows are a wave's.  Rows between, too long ones and the other calls stream:
 // with a running maximum m and a sum of exp((s - m) / T).
 //
 // 8192 x 131072 bf16, loss and gradient: resident 822 us (4.3 GB at 5.2 TB/s, a copy reaches 6.5; vector instructions issue 0.47 of the
-// time), teacher and places 45.  30 x 10: 7.8 us, one launch and its chain of loads, fp64 functions and barriers.
+// time), teacher and places 45.
+// 30 x 10 and 750 x 1000: 5.8 us a call, one launch, bound by the host; through LDS and barriers 7.2 and 8.1.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,6 +27,7 @@ namespace {
 
 constexpr int64_t kMaxGrid = 1 << 20;
 constexpr int kCus = 256;  // compute units
+constexpr int kShortBytes = 4096;  // of a row that a wave holds
 
 enum Mode { kLoss, kGradient, kStep };
 
@@ -68,56 +70,52 @@ struct RunningSum {
     }
 };
 
-// Reductions over the NT threads of a row: a butterfly in the wave, then every wave does one over the waves' results.
+// Reductions over the NT threads of a row: in the wave, then every wave does one over the waves' results.
 // `lds` has room for NT / 64 doubles.  Every thread gets the result.
-__device__ __forceinline__ RunningSum butterfly_join(RunningSum r, float c, int end) {
-    for (int off = 1; off < end; off *= 2) {
-        // both sides of a pair join the lower lane first and get the same bits
-        RunningSum other;
-        other.m = __shfl_xor(r.m, off), other.s = __shfl_xor(r.s, off);
-        const bool upper = threadIdx.x & off;
-        RunningSum lo = upper ? other : r;
-        const RunningSum hi = upper ? r : other;
-        lo.join(hi.m, hi.s, c);
-        r = lo;
-    }
-    return r;
+__device__ __forceinline__ RunningSum wave_join(RunningSum r, float c) {
+    return wave_reduce(r, [&](RunningSum a, const RunningSum &b) {
+        a.join(b.m, b.s, c);
+        return a;
+    });
 }
 
 template <int NT>
 __device__ __forceinline__ RunningSum row_join(RunningSum r, float c, double *lds) {
-    r = butterfly_join(r, c, 64);
-    if constexpr (NT > 64) {
+    constexpr int waves = NT / 64;
+    r = wave_join(r, c);
+    if constexpr (waves > 1) {
         float *f = reinterpret_cast<float *>(lds);
-        const int from = threadIdx.x % (NT / 64);
         __syncthreads();
         if (threadIdx.x % 64 == 0) f[threadIdx.x / 64 * 2] = r.m, f[threadIdx.x / 64 * 2 + 1] = r.s;
         __syncthreads();
-        r.m = f[2 * from], r.s = f[2 * from + 1];
-        r = butterfly_join(r, c, NT / 64);
+        const int from = threadIdx.x % 64;
+        r = RunningSum();
+        if (from < waves) r.m = f[2 * from], r.s = f[2 * from + 1];
+        r = wave_join(r, c);
     }
     return r;
 }
 
 template <int NT, typename F>
-__device__ __forceinline__ double row_reduce(double v, double *lds, F join) {
-    for (int off = 32; off; off >>= 1) v = join(v, __shfl_xor(v, off));
-    if constexpr (NT > 64) {
+__device__ __forceinline__ double row_reduce(double v, double nothing, double *lds, F join) {
+    constexpr int waves = NT / 64;
+    v = wave_reduce(v, join);
+    if constexpr (waves > 1) {
         __syncthreads();
         if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
         __syncthreads();
-        v = lds[threadIdx.x % (NT / 64)];
-        for (int off = NT / 128; off; off >>= 1) v = join(v, __shfl_xor(v, off));
+        const int from = threadIdx.x % 64;
+        v = wave_reduce(from < waves ? lds[from] : nothing, join);
     }
     return v;
 }
 template <int NT>
 __device__ __forceinline__ double row_sum(double v, double *lds) {
-    return row_reduce<NT>(v, lds, [](double a, double b) { return a + b; });
+    return row_reduce<NT>(v, 0.0, lds, [](double a, double b) { return a + b; });
 }
 template <int NT>
 __device__ __forceinline__ double row_max(double v, double *lds) {
-    return row_reduce<NT>(v, lds, [](double a, double b) { return fmax(a, b); });
+    return row_reduce<NT>(v, -INFINITY, lds, [](double a, double b) { return fmax(a, b); });
 }
 
 // A row's vocabulary as 16-byte vectors between a few single elements on either side.
@@ -263,18 +261,15 @@ __device__ __forceinline__ void write_places(const Args &a, const Teacher &t, co
 }
 
 template <typename T, int NT, Mode MODE>
-__global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
+__global__ __launch_bounds__(NT) void distill_kernel(Args a) {
     extern __shared__ char lds_raw[];
     __shared__ double red[32];
-    constexpr int V = 16 / sizeof(T), kRows = NT == 64 ? 4 : 1, kUnroll = 4;
-    const int tid = threadIdx.x % NT, sub = threadIdx.x / NT;
+    constexpr int V = 16 / sizeof(T), kUnroll = 4;
+    const int tid = threadIdx.x;
     const double tau = a.temperature;
     const float c = (float)(1.4426950408889634 / tau);
-    Teacher t(lds_raw + sub * teacher_bytes(a.k), a.k);
-    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
-        // a wave whose row lies behind the last works on the last one again and writes nothing
-        const bool there = row0 + sub < a.rows;
-        const int64_t row = there ? row0 + sub : a.rows - 1;
+    Teacher t(lds_raw, a.k);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
         read_teacher<T, NT>(a, row, r.at, t, tid, red);
         double m, log_sum;  // the student's log-sum-exp is m / tau + log_sum
@@ -308,26 +303,26 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
             s = row_join<NT>(s, c, red);
             m = s.m, log_sum = log((double)s.s);
             const double loss = loss_of<NT>(a, t, m / tau + log_sum, tid, red);
-            if (there && tid == 0) {
+            if (tid == 0) {
                 a.loss[row] = (float)loss;
                 if (a.lse) a.lse[row] = (float)(m / tau + log_sum);
             }
         } else {
             m = 0.0, log_sum = a.lse[row];
-        #pragma unroll 1
-    for (int j = tid; j < a.k; j += NT) t.p[j] = t.index[j] < 0 ? 0.0f : (float)(t.weight[j] / t.total);
+#pragma unroll 1
+            for (int j = tid; j < a.k; j += NT) t.p[j] = t.index[j] < 0 ? 0.0f : (float)(t.weight[j] / t.total);
         }
         if constexpr (MODE != kLoss) {
             const Softmax<T> q(m, log_sum, tau, t.total != t.total ? NAN : a.temperature * a.dloss[row]);
             T *out = (T *)a.dlogits + row * a.dlogits_ld;
             const bool pieces = (((uintptr_t)out ^ (uintptr_t)r.at) & 15) == 0;
             __syncthreads();  // the logits at the teacher's places are read: they may be written now
-            if (there && tid < r.head + r.tail) {
+            if (tid < r.head + r.tail) {
                 const int64_t e = r.edge(tid);
                 out[e] = t.some ? round_to<T>(q.weighted((float)r.at[e])) : (T)0.0f;
             }
             const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
-            for (int64_t i = tid; there && i < r.vectors; i += NT) {
+            for (int64_t i = tid; i < r.vectors; i += NT) {
                 const Words<T, V> v = at[i];
                 const Words<T, V> d = Words<T, V>::of([&](int e) { return t.some ? q.weighted(v[e]) : 0.0f; });
                 if (pieces) {
@@ -338,7 +333,124 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(Args a) {
                 }
             }
             __syncthreads();  // the dense part is written: the teacher's places again
-            if (there && t.some) write_places<T, NT>(a, t, q, out, tid);
+            if (t.some) write_places<T, NT>(a, t, q, out, tid);
+        }
+    }
+}
+
+// Short rows, at most 4096 bytes and 64 E entries of the teacher: a wave a row, everything in its registers, all loads sent
+// first.  Bound by one chain: places, the student there, fp64 functions and four reductions.
+template <typename T, Mode MODE, int E>
+__global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
+    constexpr int V = 16 / sizeof(T), R = kShortBytes / 1024;
+    const int lane = threadIdx.x % 64;
+    const double tau = a.temperature, inv = 1.0 / tau;
+    const float c = (float)(1.4426950408889634 / tau);
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
+        const Row<T> r(a.logits, row, a.ld, a.vocab);
+        int32_t index[E];
+        float t[E], student[E];
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const int j = e * 64 + lane;
+            index[e] = -1, t[e] = 0.0f;
+            if (j < a.k) index[e] = a.index[row * a.teacher_ld + j], t[e] = a.teacher[row * a.teacher_ld + j];
+        }
+        Words<T, V> x[R];
+        const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
+#pragma unroll
+        for (int v = 0; v < R; v++)
+            if (v * 64 + lane < r.vectors) x[v] = at[v * 64 + lane];
+        const bool has_edge = lane < r.head + r.tail;
+        T edge = (T)0.0f;
+        if (has_edge) edge = r.at[r.edge(lane)];
+        const float given = MODE == kGradient ? a.lse[row] : 0.0f, dloss = MODE == kLoss ? 0.0f : a.dloss[row];
+        float first = -INFINITY;
+        bool broken = false;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const bool in = index[e] >= 0 && index[e] < a.vocab;
+            student[e] = in ? (float)r.at[index[e]] : 0.0f;
+            if (in) first = fmaxf(first, t[e]);
+            broken = broken || index[e] >= a.vocab || (in && t[e] != t[e]);
+        }
+        first = wave_reduce(first, [](float p, float q) { return fmaxf(p, q); });
+        const double top = first > -INFINITY ? (double)first : 0.0;
+        double weight[E], total = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            weight[e] = index[e] >= 0 ? exp(((double)t[e] - top) * inv) : 0.0;
+            total += weight[e];
+        }
+        total = row_sum<64>(total, nullptr);
+        if (__ballot(broken) != 0) total = NAN;
+        const bool some = total > 0.0 || total != total;
+#pragma unroll
+        for (int e = 0; e < E; e++) weight[e] = index[e] < 0 ? 0.0 : weight[e] / total;
+        double m, log_sum;
+        if constexpr (MODE != kGradient) {
+            RunningSum s;
+            if (has_edge) {
+                const float y[1] = {(float)edge};
+                s.add(y, c);
+            }
+#pragma unroll
+            for (int v = 0; v < R; v++)
+                if (v * 64 + lane < r.vectors) {
+                    float y[V];
+#pragma unroll
+                    for (int i = 0; i < V; i++) y[i] = x[v][i];
+                    s.add(y, c);
+                }
+            s = wave_join(s, c);
+            m = s.m, log_sum = log((double)s.s);
+            const double lse = m * inv + log_sum, log_total = log(total);
+            double part = 0.0;
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (weight[e] > 0.0) part += weight[e] * ((((double)t[e] - top) - (double)student[e]) * inv - log_total + lse);
+            part = row_sum<64>(part, nullptr);
+            if (lane == 0) {
+                a.loss[row] = !some ? 0.0f : total != total ? NAN : (float)(tau * tau * part);
+                if (a.lse) a.lse[row] = (float)lse;
+            }
+        } else {
+            m = 0.0, log_sum = given;
+        }
+        if constexpr (MODE != kLoss) {
+            float p[E] = {};
+#pragma unroll
+            for (int f = 0; f < E; f++) {
+                const int end = std::min(64, a.k - f * 64), own = __builtin_bit_cast(int, (float)weight[f]);
+                for (int l = 0; l < end; l++) {
+                    const int il = __builtin_amdgcn_readlane(index[f], l);
+                    const float pl = __builtin_bit_cast(float, __builtin_amdgcn_readlane(own, l));
+#pragma unroll
+                    for (int e = 0; e < E; e++) p[e] += il == index[e] ? pl : 0.0f;
+                }
+            }
+            const Softmax<T> q(m, log_sum, tau, total != total ? NAN : a.temperature * dloss);
+            T *out = (T *)a.dlogits + row * a.dlogits_ld;
+            const bool pieces = (((uintptr_t)out ^ (uintptr_t)r.at) & 15) == 0;
+            if (has_edge) out[r.edge(lane)] = some ? round_to<T>(q.weighted((float)edge)) : (T)0.0f;
+#pragma unroll
+            for (int v = 0; v < R; v++)
+                if (v * 64 + lane < r.vectors) {
+                    const Words<T, V> d = Words<T, V>::of([&](int i) { return some ? q.weighted(x[v][i]) : 0.0f; });
+                    T *to = out + r.head + (v * 64 + lane) * V;
+                    if (pieces) {
+                        *(Words<T, V> *)to = d;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < V; i++) to[i] = round_to<T>(d[i]);
+                    }
+                }
+            // the dense part is written, in the wave's order: the teacher's places again
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (some && index[e] >= 0 && index[e] < a.vocab) out[index[e]] = round_to<T>(q.less(student[e], p[e]));
         }
     }
 }
@@ -556,9 +668,14 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
 
 template <typename T, int NT, Mode MODE>
 int launch_threads(const Args &a, hipStream_t s) {
-    constexpr int rows = NT == 64 ? 4 : 1;
-    const int64_t blocks = (a.rows + rows - 1) / rows;
-    distill_kernel<T, NT, MODE><<<(unsigned)std::min(blocks, kMaxGrid), NT == 64 ? 256 : NT, rows * teacher_bytes(a.k), s>>>(a);
+    distill_kernel<T, NT, MODE><<<(unsigned)std::min(a.rows, kMaxGrid), NT, teacher_bytes(a.k), s>>>(a);
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+template <typename T, Mode MODE, int E>
+int launch_short(const Args &a, hipStream_t s) {
+    distill_short_kernel<T, MODE, E><<<(unsigned)std::min((a.rows + 3) / 4, kMaxGrid), 256, 0, s>>>(a);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -591,7 +708,8 @@ int launch_resident(const Args &a, void *workspace, hipStream_t s) {
 
 template <typename T, Mode MODE>
 int launch_mode(const Args &a, hipStream_t s) {
-    if (a.vocab * (int64_t)sizeof(T) <= 4096 && a.k <= 256) return launch_threads<T, 64, MODE>(a, s);
+    if (a.vocab * (int64_t)sizeof(T) <= kShortBytes && a.k <= 256)
+        return a.k <= 64 ? launch_short<T, MODE, 1>(a, s) : launch_short<T, MODE, 4>(a, s);
     if (a.vocab * (int64_t)sizeof(T) <= 32768) return launch_threads<T, 256, MODE>(a, s);
     return launch_threads<T, 1024, MODE>(a, s);
 }

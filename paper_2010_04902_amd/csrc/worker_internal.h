@@ -173,6 +173,44 @@ __device__ __forceinline__ void with_act(int act, F fn) {
     }
 }
 
+// What a lane and its partner of step STEP hold, for reductions over a wave: steps 0 to 3 join lanes of 16 by moves within
+// a row of lanes (where the steps before have made 4 or 8 neighbours equal, a mirrored row serves as well as the partner's),
+// steps 4 and 5 exchange rows and halves.  A tenth of the latency of a shuffle through LDS.
+template <int STEP, typename V>
+__device__ __forceinline__ void wave_pair(const V &v, V &a, V &b) {
+    static_assert(sizeof(V) % 4 == 0, "");
+    struct Bits {
+        uint32_t w[sizeof(V) / 4];
+    };
+    const Bits in = __builtin_bit_cast(Bits, v);
+    Bits x = in, y;
+#pragma unroll
+    for (size_t i = 0; i < sizeof(V) / 4; i++) {
+        if constexpr (STEP < 4) {
+            constexpr int control[4] = {0xB1, 0x4E, 0x141, 0x140};  // lanes 1 0 3 2, 2 3 0 1, half rows and rows mirrored
+            y.w[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)in.w[i], control[STEP], 0xf, 0xf, true);
+        } else {
+            const auto r = STEP == 4 ? __builtin_amdgcn_permlane16_swap(in.w[i], in.w[i], false, false)
+                                     : __builtin_amdgcn_permlane32_swap(in.w[i], in.w[i], false, false);
+            x.w[i] = r[0], y.w[i] = r[1];
+        }
+    }
+    a = __builtin_bit_cast(V, x), b = __builtin_bit_cast(V, y);
+}
+
+// join(a, b) over the wave's lanes, for a join whose operands can be exchanged; every lane gets the same bits.
+template <typename V, typename F>
+__device__ __forceinline__ V wave_reduce(V v, F join) {
+    V a, b;
+    wave_pair<0>(v, a, b), v = join(a, b);
+    wave_pair<1>(v, a, b), v = join(a, b);
+    wave_pair<2>(v, a, b), v = join(a, b);
+    wave_pair<3>(v, a, b), v = join(a, b);
+    wave_pair<4>(v, a, b), v = join(a, b);
+    wave_pair<5>(v, a, b), v = join(a, b);
+    return v;
+}
+
 inline bool aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 // first + (rows - 1) * pitch + width elements can be counted, and addressed with 64 bits
