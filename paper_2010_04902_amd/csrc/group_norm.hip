@@ -22,9 +22,10 @@
 // for 58 in three kernels on 64 x 56 x 56 x 256 bf16).
 // No atomics.
 //
-// us, traced: 64 x 112 x 112 x 64 fp16 forward: statistics 22.5 (103 MB, 4.6 TB/s), join 4.7, pass 36.4 (206 MB, 5.6 TB/s).
-// 64 x 56 x 56 x 256 bf16: forward 20.4 + 4.8 + 33.3; backward sums 38.4 (206 MB, 5.4 TB/s), totals 5.4, pass 48.8 (309 MB, 6.3 TB/s),
-// parameters 4.9.  30 x 32 x 32 x 64 bf16: 12.1 forward, 16.0 backward, one block's chain of loads, joins and stores.
+// us, traced: 64 x 112 x 112 x 64 fp16 forward: statistics 21.5 (103 MB, 4.8 TB/s), join 4.8, pass 36.2 (206 MB, 5.7 TB/s).
+// 64 x 56 x 56 x 256 bf16: forward 20.5 + 5.0 + 33.3; backward sums 37.5 (206 MB, 5.5 TB/s), totals 5.0, pass 48.6 (309 MB, 6.3 TB/s),
+// parameters 4.8.  30 x 32 x 32 x 64 bf16: 10.9 forward, 11.4 backward (12.1 and 16.0 with joins through LDS), 3.5
+// parameters: a block's chain of loads, joins and stores.
 #include <algorithm>
 #include <type_traits>
 
@@ -251,24 +252,27 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
     return Stat{a.n > 0.0f ? a.m + e * (double)f : b.m, n, a.d + b.d + (a.n > 0.0f ? e1 * e1 * (a.n * f) : 0.0f)};
 }
 
-__device__ __forceinline__ Stat from(Stat s, int off) { return Stat{__shfl_xor(s.m, off), __shfl_xor(s.n, off), __shfl_xor(s.d, off)}; }
-
-// Joins the statistics of the wave's lanes; each gets the same bits.
-__device__ __forceinline__ Stat join_wave(Stat s, int first, int end) {
-    for (int off = first; off < end; off *= 2) {
-        const Stat o = from(s, off);
-        s = threadIdx.x & off ? join(o, s) : join(s, o);
-    }
+// Joins the statistics of lanes that are `first` and more apart; each gets the same bits.
+__device__ __forceinline__ Stat join_wave(Stat s, int first) {
+    wave_steps(first, [&](auto step) {
+        Stat lower, upper;
+        wave_pair<step.value>(s, lower, upper);
+        if (step.value < 4 && (threadIdx.x & (1 << step.value))) {
+            const Stat own = lower;
+            lower = upper, upper = own;
+        }
+        s = join(lower, upper);
+    });
     return s;
 }
 
 constexpr int kStatRows = 16;
 constexpr int kSerial = 16;  // entries of a group that one thread joins
 
-// Joins the threads' statistics (n values each of V channels, mean m, distances d) into the groups': grp[g].
-// Ends with a barrier.  `entries`: LDS for one Stat a thread and unit, or a wave's column and unit.
-template <int V>
-__device__ void group_stats(const Plan &q, const Tile &t, float n, double (&m)[V], float (&d)[V], Stat *entry, Stat *grp) {
+// Joins the threads' statistics (n values each of V channels, mean m, distances d) into the groups', one thread calls
+// done(g, statistics) for each.  Ends with a barrier.  `entry`: LDS for one Stat a thread and unit, or a wave's column and unit.
+template <int V, typename F>
+__device__ void group_stats(const Plan &q, const Tile &t, float n, double (&m)[V], float (&d)[V], Stat *entry, F done) {
     // channels of a unit first: equal counts
     float count = n;
 #pragma unroll
@@ -296,16 +300,19 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, double (&m)[V
         if (v % q.unit == 0) {
             Stat s{m[v], t.mine ? count : 0.0f, d[v]};
             if (joined && even) {
-                for (int off = q.tx; off < 64; off *= 2) {
+                wave_steps(q.tx, [&](auto step) {
                     // the pair's lanes get the same bits: their sum, and the square of their difference
-                    const double m2 = __shfl_xor(s.m, off);
-                    const float d2 = __shfl_xor(s.d, off), e = (float)(m2 - s.m);
-                    s.m = 0.5 * (s.m + m2);
-                    s.d = (s.d + d2) + e * e * (0.5f * s.n);
+                    double ma, mb;
+                    float da, db;
+                    wave_pair<step.value>(s.m, ma, mb);
+                    wave_pair<step.value>(s.d, da, db);
+                    const float e = (float)(mb - ma);
+                    s.m = 0.5 * (ma + mb);
+                    s.d = (da + db) + e * e * (0.5f * s.n);
                     s.n *= 2.0f;
-                }
+                });
             } else if (joined) {
-                s = join_wave(s, q.tx, 64);
+                s = join_wave(s, q.tx);
             }
             if (writes) entry[row * units + (t.tx * V + v) / q.unit] = s;
         }
@@ -316,15 +323,15 @@ __device__ void group_stats(const Plan &q, const Tile &t, float n, double (&m)[V
             Stat s = entry[g * per];
             for (int y = 0; y < rows; y++)
                 for (int e = y == 0; e < per; e++) s = join(s, entry[y * units + g * per + e]);
-            grp[g] = s;
+            done(g, s);
         }
     } else {  // a wave a group
         const int lane = threadIdx.x % 64;
         for (int g = threadIdx.x / 64; g < ng; g += q.threads / 64) {
             Stat s{0.0, 0.0f, 0.0f};
             for (int e = lane; e < rows * per; e += 64) s = join(s, entry[e / per * units + g * per + e % per]);
-            s = join_wave(s, 1, 64);
-            if (lane == 0) grp[g] = s;
+            s = join_wave(s, 1);
+            if (lane == 0) done(g, s);
         }
     }
     __syncthreads();
@@ -338,11 +345,16 @@ __device__ void channel_sums(const Plan &q, const Tile &t, float (&acc)[K][V], f
     int rows = q.ty, row = t.ty;
     bool writes = t.ty < q.ty;
     if (q.tx < 64 && (q.tx & (q.tx - 1)) == 0) {  // a wave holds whole rows: join them in registers first
+        wave_steps(q.tx, [&](auto step) {
 #pragma unroll
-        for (int k = 0; k < K; k++)
+            for (int k = 0; k < K; k++)
 #pragma unroll
-            for (int v = 0; v < V; v++)
-                for (int off = q.tx; off < 64; off *= 2) acc[k][v] += __shfl_xor(acc[k][v], off);
+                for (int v = 0; v < V; v++) {
+                    float a, b;
+                    wave_pair<step.value>(acc[k][v], a, b);
+                    acc[k][v] = a + b;
+                }
+        });
         rows = q.threads / 64;
         row = threadIdx.x / 64;
         writes = (int)(threadIdx.x % 64) < q.tx;
@@ -389,8 +401,7 @@ __device__ void group_sums(const Plan &q, const Tile &t, const float *chan, int 
             for (int k = 0; k < K; k++) s[k] += w * chan[k * cs + g * gw + j];
         }
 #pragma unroll
-        for (int k = 0; k < K; k++)
-            for (int off = 32; off; off >>= 1) s[k] += __shfl_xor(s[k], off);
+        for (int k = 0; k < K; k++) s[k] = wave_reduce(s[k], [](float a, float b) { return a + b; });
         if (lane == 0)
 #pragma unroll
             for (int k = 0; k < K; k++) grp[k * stride + g] = s[k];
@@ -452,7 +463,7 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
         const uint32_t tile = b % 8 * q.per_xcd + b / 8;
         if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
-        Stat *grp = (Stat *)lds;
+        float2 *grp = (float2 *)lds;  // means and rstd, in the room of as many Stats
         Words<T, V> x[R];
         const T *at = t.in<T>(a.x, a.xs, a.xp, V);
         int count = 0;
@@ -485,14 +496,15 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
             for (int v = 0; v < V; v++) centre[v] = (double)x[0][v] + (double)m[v];
 #pragma unroll
         for (int r = 0; r < R; r++) x[r].keep();
-        group_stats<V>(q, t, (float)count, centre, d, grp + q.head, grp);
         const float m1 = 1.0f / ((float)q.p * (float)q.gc);
-        auto mean = [&](int g) { return (float)grp[g].m; };
-        auto rstd = [&](int g) { return 1.0f / sqrtf(grp[g].d * m1 + a.eps); };
-        for (int g = threadIdx.x; g < t.groups(q); g += q.threads) {
-            a.mean[t.i * q.groups + t.g0 + g] = mean(g);
-            a.rstd[t.i * q.groups + t.g0 + g] = rstd(g);
-        }
+        group_stats<V>(q, t, (float)count, centre, d, (Stat *)lds + q.head, [&](int g, const Stat &s) {
+            const float mean = (float)s.m, rstd = 1.0f / sqrtf(s.d * m1 + a.eps);
+            grp[g] = make_float2(mean, rstd);
+            a.mean[t.i * q.groups + t.g0 + g] = mean;
+            a.rstd[t.i * q.groups + t.g0 + g] = rstd;
+        });
+        auto mean = [&](int g) { return grp[g].x; };
+        auto rstd = [&](int g) { return grp[g].y; };
         if (t.mine) {
             const Affine<V> f(a, t, mean, rstd);
             T *to = t.out<T>(a, V);
@@ -518,7 +530,6 @@ __global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
         const uint32_t tile = b % 8 * q.per_xcd + b / 8;
         if (tile >= q.tiles) continue;
         const Tile t(q, tile, V);
-        Stat *grp = (Stat *)lds;
         float pivot[V] = {}, s[V] = {}, d[V] = {};
         int count = 0;
         const T *const at[1] = {t.in<T>(a.x, a.xs, a.xp, V)};
@@ -543,10 +554,9 @@ __global__ __launch_bounds__(256) void norm_stats_kernel(Args a) {
             d[v] = e < 0.0f ? 0.0f : e;
             centre[v] = (double)pivot[v] + (double)(s[v] * inv);
         }
-        group_stats<V>(q, t, (float)count, centre, d, grp + q.head, grp);
-        for (int g = threadIdx.x; g < t.groups(q); g += q.threads)
-            a.stat[((t.i * q.groups + t.g0 + g) * q.chunks + t.chunk) * q.parts + t.part] = grp[g];
-        __syncthreads();
+        group_stats<V>(q, t, (float)count, centre, d, (Stat *)lds, [&](int g, const Stat &s) {
+            a.stat[((t.i * q.groups + t.g0 + g) * q.chunks + t.chunk) * q.parts + t.part] = s;
+        });
     }
 }
 
@@ -558,7 +568,7 @@ __global__ __launch_bounds__(256) void norm_join_kernel(Args a) {
     for (uint32_t group = blockIdx.x * 4 + threadIdx.x / 64; group < all; group += gridDim.x * 4) {
         Stat s{0.0, 0.0f, 0.0f};
         for (uint32_t e = lane; e < entries; e += 64) s = join(s, a.stat[(int64_t)group * entries + e]);
-        s = join_wave(s, 1, 64);
+        s = join_wave(s, 1);
         if (lane == 0) {
             a.mean[group] = (float)s.m;
             a.rstd[group] = 1.0f / sqrtf(s.d / ((float)q.p * (float)q.gc) + a.eps);
@@ -738,7 +748,7 @@ __global__ __launch_bounds__(256) void norm_backward_totals_kernel(Args a) {
             }
             __syncthreads();
         }
-        for (int off = 32; off; off >>= 1) s1 += __shfl_xor(s1, off), s2 += __shfl_xor(s2, off);
+        s1 = wave_reduce(s1, [](float a, float b) { return a + b; }), s2 = wave_reduce(s2, [](float a, float b) { return a + b; });
         if (threadIdx.x % 64 == 0) sums[0][threadIdx.x / 64] = s1, sums[1][threadIdx.x / 64] = s2;
         __syncthreads();
         if (threadIdx.x == 0) {

@@ -173,9 +173,9 @@ __device__ __forceinline__ void with_act(int act, F fn) {
     }
 }
 
-// What a lane and its partner of step STEP hold, for reductions over a wave: steps 0 to 3 join lanes of 16 by moves within
-// a row of lanes (where the steps before have made 4 or 8 neighbours equal, a mirrored row serves as well as the partner's),
-// steps 4 and 5 exchange rows and halves.  A tenth of the latency of a shuffle through LDS.
+// What a lane and the lane 2^STEP away (in the exclusive-or of their numbers) hold: a row of 16 lanes is turned by DPP, rows and
+// halves are exchanged; a tenth of the latency of a shuffle through LDS.  Steps 2 and 3 turn the row by 4 and 8, which is the
+// partner's value where the steps above have been taken.  Steps 4 and 5 give the lower lane's value first, others the lane's own.
 template <int STEP, typename V>
 __device__ __forceinline__ void wave_pair(const V &v, V &a, V &b) {
     static_assert(sizeof(V) % 4 == 0, "");
@@ -187,7 +187,7 @@ __device__ __forceinline__ void wave_pair(const V &v, V &a, V &b) {
 #pragma unroll
     for (size_t i = 0; i < sizeof(V) / 4; i++) {
         if constexpr (STEP < 4) {
-            constexpr int control[4] = {0xB1, 0x4E, 0x141, 0x140};  // lanes 1 0 3 2, 2 3 0 1, half rows and rows mirrored
+            constexpr int control[4] = {0xB1, 0x4E, 0x124, 0x128};  // lanes 1 0 3 2; 2 3 0 1; row turned by 4; by 8
             y.w[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)in.w[i], control[STEP], 0xf, 0xf, true);
         } else {
             const auto r = STEP == 4 ? __builtin_amdgcn_permlane16_swap(in.w[i], in.w[i], false, false)
@@ -198,16 +198,25 @@ __device__ __forceinline__ void wave_pair(const V &v, V &a, V &b) {
     a = __builtin_bit_cast(V, x), b = __builtin_bit_cast(V, y);
 }
 
+// fn(step) for the steps that join lanes `first` and more apart, first a power of two
+template <typename F>
+__device__ __forceinline__ void wave_steps(int first, F fn) {
+    if (first <= 32) fn(std::integral_constant<int, 5>{});
+    if (first <= 16) fn(std::integral_constant<int, 4>{});
+    if (first <= 8) fn(std::integral_constant<int, 3>{});
+    if (first <= 4) fn(std::integral_constant<int, 2>{});
+    if (first <= 2) fn(std::integral_constant<int, 1>{});
+    if (first <= 1) fn(std::integral_constant<int, 0>{});
+}
+
 // join(a, b) over the wave's lanes, for a join whose operands can be exchanged; every lane gets the same bits.
 template <typename V, typename F>
 __device__ __forceinline__ V wave_reduce(V v, F join) {
-    V a, b;
-    wave_pair<0>(v, a, b), v = join(a, b);
-    wave_pair<1>(v, a, b), v = join(a, b);
-    wave_pair<2>(v, a, b), v = join(a, b);
-    wave_pair<3>(v, a, b), v = join(a, b);
-    wave_pair<4>(v, a, b), v = join(a, b);
-    wave_pair<5>(v, a, b), v = join(a, b);
+    wave_steps(1, [&](auto step) {
+        V a, b;
+        wave_pair<step.value>(v, a, b);
+        v = join(a, b);
+    });
     return v;
 }
 
