@@ -5,12 +5,18 @@
 // outputs, laid out so that a wave holds both sums of an output in the same lane and register: the epilogue needs no
 // exchange.  Backward, one pass over dh and the saved sums writes dgate | dup, and
 //     dx = dgate w_gate + dup w_up  is one product summed over 2n,   dw_gate = dgate^T x and dw_up = dup^T x  one launch.
+// dx of few tokens has few tiles and a long sum: blocks share it and a kernel adds their sums in order (us of the backward pass
+// without / with that: 40 x 4096 x 10944 198 / 111, 64 x 1024 x 2752 36 / 23, 333 x 1000 x 2731 59 / 48).
 // Operands whose summed index is not contiguous are turned by the loads from LDS, nothing is transposed in memory.
 // The saved sums are fp32: rounded to bf16 they would be a third rounding on the way to a weight's gradient (2.9e-3
 // off its 64-bit value instead of 2.35e-3; dgate's and the result's own are the others).
 //
 // Few tokens: the weights' bytes bound the call; a wave multiplies 16 rows of each weight with up to 16 tokens,
 // straight from memory into the matrix instruction's registers, the waves of a block split k and join in LDS.
+//
+// us, traced (TFLOP/s; a large library product reaches 1161 in bf16): 8192 x 4096 x 10944 bf16 forward with saved sums 1391 (1056),
+// dgate | dup 258, dx 1233 (1191), both dw 1388 (1058).  1920 x 512 x 1376: 17.7, 8.2, 18.9, 15.0, short products on less than
+// two blocks a compute unit.  333 x 1000 x 2731 fp16 forward 18.  One token of 2048 -> 5504: 9.3 (45 MB, 4.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -66,6 +72,9 @@ struct Product {
     int64_t gate_ld;
     int act;
     int tiles_m, tiles_n;
+    int splits, split_steps;  // kInput: blocks that share a tile's sum, and steps of each; their sums go to
+    float *partial;           // [splits][m][partial_ld]
+    int64_t partial_ld;
     bool direct;             // whole steps go from memory to LDS without registers
     bool out_wide, gate_wide;  // rows of results start at 16-byte boundaries
 };
@@ -217,7 +226,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     static_assert(kWaves * 4096 <= STAGES * kBytes, "");
     const int64_t move_a = KIND == kWeight ? kStep * p.a_ld : kStep, move_b = KIND == kForward ? kStep : kStep * p.b_ld;
     // kInput: steps of w_gate, then of w_up; `turn` is a multiple of the step
-    const int steps = (int)((p.k + kStep - 1) / kStep), turn = KIND == kInput ? (int)(p.turn / kStep) : steps;
+    const int all = (int)((p.k + kStep - 1) / kStep), turn = KIND == kInput ? (int)(p.turn / kStep) : all;
+    // this block's: all, or its share of them
+    const bool split = KIND == kInput && p.splits > 1;
+    const int share = split ? (int)blockIdx.x / (p.tiles_m * p.tiles_n) : 0, first = share * p.split_steps;
+    const int steps = split ? std::min(all, first + p.split_steps) : all;
     // whole steps go from memory to LDS without registers
     const int whole = !p.direct ? 0 : (int)((KIND == kInput ? p.k - p.turn : p.k) / kStep);
     auto is_direct = [&](int t) { return t < steps && (t >= turn ? t - turn : t) < whole; };
@@ -233,7 +246,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     for (int j = 0; j < FN; j++)
         place_b[j] = BM * 128 + (KIND == kForward ? j % 2 * (BN * 64) + B::fragment((wn * (FN / 2) + j / 2) * 32, lane)
                                                   : B::fragment((wn * FN + j) * 32, lane));
-    const Pl at(p, blockIdx.x, wave, lane);
+    const Pl at(p, split ? (int)blockIdx.x - share * p.tiles_m * p.tiles_n : (int)blockIdx.x, wave, lane);
     // Addresses of this thread's loads of a step; which operand a load is of goes by its number, for all waves.
     const T *from[kLoads];
     auto address = [&](int t) {
@@ -342,19 +355,20 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     // end of the fast steps that t is among: those behind t that are counted off are direct, too, and their loads
     // move on in one operand
     auto fast_end = [&](int t) {
-        if (KIND != kInput || t + STAGES < turn) return whole - STAGES;
-        return whole == turn || t + 2 >= turn ? turn + whole - STAGES : t;
+        if (KIND != kInput || t + STAGES < turn) return std::min(whole, steps) - STAGES;
+        return whole == turn || t + 2 >= turn ? std::min(turn + whole, steps) - STAGES : t;
     };
-    if (steps > 0) {
-        for (int t = 0; t < STAGES; t++) load(t);
+    if (steps > first) {
+        bool ahead = true;  // the first steps are all there and direct
+        for (int t = first; t < first + STAGES; t++) ahead = ahead && is_direct(t), load(t);
         done_reading();
-        if (whole >= STAGES)
+        if (ahead)
             asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 1) * kLoads) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         barrier();
-        read(a0, b0, 0, 0);
-        for (int t = 0; t < steps;) {
+        read(a0, b0, first, 0);
+        for (int t = first; t < steps;) {
             const int end = fast_end(t);
             if (t < end) address(t + STAGES);
             for (; t < end; t++) step(t, std::true_type{});
@@ -368,7 +382,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
     const bool full = m0 + FM * 32 <= p.m && n0 + kWide <= p.n;
     const int own = afresh(lane), row = own % 32, high = own / 32;
     auto exchange = [&](int bytes) { return bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
-    auto flush = [&](auto type, int i, auto bytes_, auto *to, int64_t ld, bool wide) {
+    auto flush = [&](auto type, int i, auto bytes_, int from, auto *to, int64_t ld, bool wide) {
         // rows of bytes_ bytes from the scratch to memory
         asm volatile("" ::: "memory");
         using U = decltype(type);
@@ -378,13 +392,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
             const int r = c * (64 / pieces) + own / pieces, piece = own % pieces;
             const int turned = piece ^ (bytes == 128 ? (r >> 1) & 7 : (r >> 2) & 3);
             const Pack<U, per> v = *(const Pack<U, per> *)(scratch + r * bytes + turned * 16);
-            U *at_row = to + (m0 + i * 32 + r) * ld + n0 + piece * per;
+            U *at_row = to + (m0 + i * 32 + r) * ld + n0 + from + piece * per;
             if (full && wide) {
-                *(Pack<U, per> *)at_row = v;
+                put(at_row, v);
             } else if (m0 + i * 32 + r < p.m) {
-                const int64_t left = p.n - n0 - piece * per;
+                const int64_t left = p.n - n0 - from - piece * per;
                 if (wide && left >= per) {
-                    *(Pack<U, per> *)at_row = v;
+                    put(at_row, v);
                 } else {
 #pragma unroll
                     for (int e = 0; e < per; e++)
@@ -394,6 +408,24 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
         }
         asm volatile("" ::: "memory");
     };
+    if constexpr (KIND == kInput)
+        if (split) {
+            float *const sums = p.partial + share * p.m * p.partial_ld;
+#pragma unroll
+            for (int i = 0; i < FM; i++)
+#pragma unroll
+                for (int j = 0; j < FN; j++) {
+#pragma unroll
+                    for (int g = 0; g < 4; g++) {
+                        Pack<float, 4> v;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) v.v[e] = acc[i][j][g * 4 + e];
+                        *(Pack<float, 4> *)(scratch + row * 128 + ((g * 2 + high) ^ exchange(128)) * 16) = v;
+                    }
+                    flush(0.0f, i, std::integral_constant<int, 128>{}, j * 32, sums, p.partial_ld, true);
+                }
+            return;
+        }
     constexpr std::integral_constant<int, kWide * 2> out_bytes{};
     with_act(KIND == kForward ? p.act : BYZ_ACT_NONE, [&](auto act) {
 #pragma unroll
@@ -414,7 +446,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
                     const int piece = (KIND == kForward ? j / 2 : j) * 4 + g;
                     *(Pack<T, 4> *)(scratch + row * out_bytes.value + (piece ^ exchange(out_bytes.value)) * 16 + high * 8) = v;
                 }
-            flush(T{}, i, out_bytes, out, p.out_ld, p.out_wide);
+            flush(T{}, i, out_bytes, 0, out, p.out_ld, p.out_wide);
             if constexpr (KIND == kForward)
                 if (p.gate) {
 #pragma unroll
@@ -426,7 +458,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p) {
                             for (int e = 0; e < 4; e++) v.v[e] = acc[i][j][g * 4 + e];
                             *(Pack<float, 4> *)(scratch + row * 128 + ((g * 2 + high) ^ exchange(128)) * 16) = v;
                         }
-                        flush(0.0f, i, std::integral_constant<int, 128>{}, (j % 2 ? p.up : p.gate) + j / 2 * 32, p.gate_ld, p.gate_wide);
+                        flush(0.0f, i, std::integral_constant<int, 128>{}, j / 2 * 32, j % 2 ? p.up : p.gate, p.gate_ld, p.gate_wide);
                     }
                 }
         }
@@ -508,13 +540,15 @@ struct Slopes {
     int act;
 };
 
-// Four values a thread, rows of np / 4 threads.
+// Four values a thread, rows of np / 4 threads.  Bound by memory: 258 us for 8192 x 10944 (1256 MB, 4.9 TB/s); eight values a
+// thread, whose loads are 32 bytes apart: 315.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void slopes_kernel(Slopes s) {
     const int64_t across = s.np / 4, all = s.m * across;
+    const bool small = all <= UINT32_MAX;
     with_act(s.act, [&](auto act) {
         for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
-            const int64_t i = at / across, j = (at - i * across) * 4;
+            const int64_t i = small ? (uint32_t)at / (uint32_t)across : at / across, j = (at - i * across) * 4;
             const T *dh = (const T *)s.dh + i * s.dh_ld + j;
             const float *gate = s.gate + i * s.gate_ld + j, *up = s.up + i * s.gate_ld + j;
             Pack<T, 4> h, dg, du;
@@ -557,12 +591,40 @@ __global__ __launch_bounds__(256) void align_kernel(const T *in, int64_t in_ld, 
     }
 }
 
+// Adds the sums of the blocks that share a tile, in their order, four values a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float *partial, int splits, int64_t m, int64_t n, int64_t ld, T *out, int64_t out_ld) {
+    const int64_t across = ld / 4, all = m * across, apart = m * ld;
+    const bool wide = ((uintptr_t)out & 7) == 0 && out_ld % 4 == 0;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        const int64_t i = at / across, j = (at - i * across) * 4;
+        const float *from = partial + i * ld + j;
+        Pack<float, 4> sum = *(const Pack<float, 4> *)from;
+        for (int k = 1; k < splits; k++) {
+            const Pack<float, 4> v = *(const Pack<float, 4> *)(from + k * apart);
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum.v[e] += v.v[e];
+        }
+        Pack<T, 4> r;
+#pragma unroll
+        for (int e = 0; e < 4; e++) r.v[e] = round_to<T>(sum.v[e]);
+        T *to = out + i * out_ld + j;
+        if (wide && j + 4 <= n) {
+            put(to, r);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (j + e < n) to[e] = r.v[e];
+        }
+    }
+}
+
 unsigned grid_of(int64_t threads) { return (unsigned)std::min<int64_t>((threads + 255) / 256, 8192); }
 
 template <typename T, int BM, int BN, int WM, int WN, Kind KIND, int STAGES>
 int launch_tile(Product p, hipStream_t s) {
     constexpr int kOut = KIND == kForward ? BN / 2 : BN, kThreads = WM * WN * 64, kLds = STAGES * (BM + BN) * 128;
-    const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + kOut - 1) / kOut, tiles = tm * tn * (KIND == kWeight ? 2 : 1);
+    const int64_t tm = (p.m + BM - 1) / BM, tn = (p.n + kOut - 1) / kOut, tiles = tm * tn * (KIND == kWeight ? 2 : KIND == kInput ? p.splits : 1);
     if (tiles > INT32_MAX / kThreads) return BYZ_EUNSUPPORTED;
     p.tiles_m = (int)tm, p.tiles_n = (int)tn;
     // a lane's place in a tile's side is a 32-bit offset
@@ -586,26 +648,35 @@ struct Shape {
 constexpr Shape kShapes[] = {{256, 256, 2, 1, 1.85}, {128, 128, 2, 2, 0.6}, {128, 128, 4, 1, 0.6}, {64, 128, 3, 2, 0.35},
                              {64, 128, 6, 1, 0.35},  {64, 64, 4, 2, 0.22},  {64, 64, 8, 1, 0.22}};
 
+struct Choice {
+    int shape, splits;
+};
+
 // The shape of the shortest estimated time: rounds of blocks, each so many steps and 3 us for its first loads and its stores; a step
 // takes the blocks' products on a compute unit or, where those are shorter, the way from memory (1 us) over the stages ahead.
-int best_shape(int64_t m, int64_t across, int64_t k, int copies, bool square64) {
-    int best = 0;
+// dx of few tokens has few tiles and a long sum, which up to 16 blocks of a tile share, 8 steps each at least; the kernel that
+// adds their sums takes 4 us and its bytes at 4 TB/s.
+Choice best_shape(int64_t m, int64_t across, int64_t k, Kind kind) {
+    Choice best{};
     double best_time = 0.0;
-    for (int i = 0; i < (square64 ? 7 : 5); i++) {
-        const Shape &c = kShapes[i];
-        const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((across + c.bn - 1) / c.bn) * copies;
-        const int64_t rounds = (tiles + 256 * c.resident - 1) / (256 * c.resident), together = std::min<int64_t>(c.resident, (tiles + 255) / 256);
-        const double step = std::max(together * c.step, 1.0 / (c.stages - 1));
-        const double time = rounds * ((k + kStep - 1) / kStep * step + 3.0);
-        if (i == 0 || time < best_time) best = i, best_time = time;
-    }
+    const int64_t steps = (k + kStep - 1) / kStep;
+    for (int splits = 1; splits <= (kind == kInput ? 16 : 1) && (splits == 1 || steps >= 8 * splits); splits *= 2)
+        for (int i = 0; i < (kind != kForward ? 7 : 5); i++) {
+            const Shape &c = kShapes[i];
+            const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((across + c.bn - 1) / c.bn) * (kind == kWeight ? 2 : splits);
+            const int64_t rounds = (tiles + 256 * c.resident - 1) / (256 * c.resident), together = std::min<int64_t>(c.resident, (tiles + 255) / 256);
+            const double step = std::max(together * c.step, 1.0 / (c.stages - 1));
+            double time = rounds * ((steps + splits - 1) / splits * step + 3.0);
+            if (splits > 1) time += 4.0 + (double)m * (double)across * (8 * splits + 2) / 4e6;
+            if (best_time == 0.0 || time < best_time) best = {i, splits}, best_time = time;
+        }
     return best;
 }
 
 // Operands' rows start at 16-byte boundaries and have whole 16-byte pieces.
 template <typename T, Kind KIND>
-int launch_product(const Product &p, hipStream_t s) {
-    switch (best_shape(p.m, KIND == kForward ? 2 * p.n : p.n, p.k, KIND == kWeight ? 2 : 1, KIND != kForward)) {
+int launch_shape(int shape, const Product &p, hipStream_t s) {
+    switch (shape) {
         case 0: return launch_tile<T, 256, 256, 2, 4, KIND, 2>(p, s);
         case 1: return launch_tile<T, 128, 128, 2, 2, KIND, 2>(p, s);
         case 2: return launch_tile<T, 128, 128, 2, 2, KIND, 4>(p, s);
@@ -614,9 +685,26 @@ int launch_product(const Product &p, hipStream_t s) {
         default: break;
     }
     if constexpr (KIND != kForward)
-        return best_shape(p.m, p.n, p.k, KIND == kWeight ? 2 : 1, true) == 5 ? launch_tile<T, 64, 64, 2, 2, KIND, 4>(p, s)
-                                                                             : launch_tile<T, 64, 64, 2, 2, KIND, 8>(p, s);
+        return shape == 5 ? launch_tile<T, 64, 64, 2, 2, KIND, 4>(p, s) : launch_tile<T, 64, 64, 2, 2, KIND, 8>(p, s);
     return BYZ_EINTERNAL;
+}
+
+// kInput: `partial` has room for the sums of the blocks that share a tile.
+template <typename T, Kind KIND>
+int launch_product(Product p, float *partial, hipStream_t s) {
+    const Choice c = best_shape(p.m, KIND == kForward ? 2 * p.n : p.n, p.k, KIND);
+    p.splits = c.splits;
+    if (c.splits > 1) {
+        const int64_t steps = (p.k + kStep - 1) / kStep;
+        p.split_steps = (int)((steps + c.splits - 1) / c.splits);
+        p.partial = partial, p.partial_ld = (p.n + 3) / 4 * 4;
+    }
+    int rc = launch_shape<T, KIND>(c.shape, p, s);
+    if (rc == BYZ_OK && c.splits > 1) {
+        join_kernel<T><<<grid_of(p.m * (p.partial_ld / 4)), 256, 0, s>>>(partial, c.splits, p.m, p.n, p.partial_ld, (T *)p.out, p.out_ld);
+        BYZ_HIP(hipGetLastError());
+    }
+    return rc;
 }
 
 int64_t padded(int64_t v) { return (v + 63) / 64 * 64; }
@@ -629,15 +717,20 @@ bool sizes_ok(int64_t m, int64_t k, int64_t n) {
 // Whether the tile kernel reads a matrix as it lies: pieces of 16 bytes, none of them beyond the columns.
 bool pieces(const void *at, int64_t cols, int64_t ld) { return aligned(at, 16) && cols % 8 == 0 && ld % 8 == 0; }
 
-// Workspace, in elements: matrices that have to be copied, and for the backward pass dgate | dup.
+// Workspace, in elements: matrices that have to be copied, and for the backward pass dgate | dup and the sums of blocks
+// that share a tile of dx.
 struct Layout {
     int64_t np, kp;
-    int64_t x, w, d, all;
+    int64_t x, w, d, partial, all;
     Layout(int64_t m, int64_t k, int64_t n, bool backward) : np(padded(n)), kp((k + 7) / 8 * 8) {
         x = 0;
         w = x + m * kp;
         d = w + 2 * n * kp;
-        all = d + (backward ? m * 2 * np : 0);
+        partial = all = d + (backward ? m * 2 * np : 0);
+        if (backward && m > 0 && k > 0) {
+            const int splits = best_shape(m, k, np + n, kInput).splits;
+            if (splits > 1) all += 2 * splits * m * ((k + 3) / 4 * 4);
+        }
     }
 };
 
@@ -690,7 +783,7 @@ int forward(Call c, Product p, hipStream_t s) {
     p.m = c.m, p.n = c.n, p.k = c.k, p.act = c.act;
     if (c.m > kSkinny) {
         p.k = (p.k + 7) / 8 * 8, p.a_outer = p.m, p.b_outer = p.n;
-        return launch_product<T, kForward>(p, s);
+        return launch_product<T, kForward>(p, nullptr, s);
     }
     p.direct = pieces(c.x, 8, c.x_ld) && pieces(c.w_gate, 8, c.w_ld) && pieces(c.w_up, 8, c.w_ld);
     skinny_kernel<T><<<(unsigned)((p.n + kSkinnyOut - 1) / kSkinnyOut), kSkinnyWaves * 64, 0, s>>>(p);
@@ -728,14 +821,14 @@ int backward(Call c, const Gradients &g, hipStream_t s) {
         p.a = d, p.a_ld = 2 * lay.np, p.b = c.w_gate, p.b2 = c.w_up, p.b_ld = c.w_ld;
         p.m = c.m, p.n = cols, p.turn = lay.np, p.k = lay.np + c.n, p.out = g.dx, p.out_ld = g.dx_ld;
         p.a_outer = c.m, p.b_outer = lay.kp;
-        rc = launch_product<T, kInput>(p, s);
+        rc = launch_product<T, kInput>(p, (float *)((T *)c.ws + lay.partial), s);
     }
     if (rc == BYZ_OK && dw) {
         Product p{};
         p.a = d, p.a_ld = 2 * lay.np, p.turn = lay.np, p.b = c.x, p.b_ld = c.x_ld;
         p.m = c.n, p.n = cols, p.k = c.m, p.out = g.dw_gate, p.out2 = g.dw_up, p.out_ld = g.dw_ld;
         p.a_outer = lay.np, p.b_outer = lay.kp;
-        rc = launch_product<T, kWeight>(p, s);
+        rc = launch_product<T, kWeight>(p, nullptr, s);
     }
     return rc;
 }

@@ -38,6 +38,14 @@ struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
+// Stores a pack as one vector.  Assigned as a struct beside a branch that stores single elements, the compiler (ROCm 7.2) joins a
+// store of each side to one and has lost the last element of packs in tiles that end early.
+template <typename T, int V>
+__device__ __forceinline__ void put(T *to, const Pack<T, V> &v) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) * V / 4), may_alias));
+    *(words *)to = __builtin_bit_cast(words, v);
+}
+
 // The same, held as 32-bit words: values of 16 bits that live over a loop or a barrier as such would take a register
 // each.
 typedef uint32_t __attribute__((may_alias)) word_t;
