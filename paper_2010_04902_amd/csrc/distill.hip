@@ -27,7 +27,8 @@ namespace {
 
 constexpr int64_t kMaxGrid = 1 << 20;
 constexpr int kCus = 256;  // compute units
-constexpr int kShortBytes = 4096;  // of a row that a wave holds
+constexpr int kManyRows = 4 * kCus;
+constexpr int kShortBytes = 16384;  // of a row that a wave holds at most
 
 enum Mode { kLoss, kGradient, kStep };
 
@@ -338,11 +339,11 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
     }
 }
 
-// Short rows, at most 4096 bytes and 64 E entries of the teacher: a wave a row, everything in its registers, all loads sent
+// Short rows, R KB and 64 E entries of the teacher at most: a wave a row, everything in its registers, all loads sent
 // first.  Bound by one chain: places, the student there, fp64 functions and four reductions.
-template <typename T, Mode MODE, int E>
+template <typename T, Mode MODE, int R, int E>
 __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
-    constexpr int V = 16 / sizeof(T), R = kShortBytes / 1024;
+    constexpr int V = 16 / sizeof(T);
     const int lane = threadIdx.x % 64;
     const double tau = a.temperature, inv = 1.0 / tau;
     const float c = (float)(1.4426950408889634 / tau);
@@ -673,9 +674,13 @@ int launch_threads(const Args &a, hipStream_t s) {
     return BYZ_OK;
 }
 
-template <typename T, Mode MODE, int E>
+template <typename T, Mode MODE, int R>
 int launch_short(const Args &a, hipStream_t s) {
-    distill_short_kernel<T, MODE, E><<<(unsigned)std::min((a.rows + 3) / 4, kMaxGrid), 256, 0, s>>>(a);
+    const unsigned grid = (unsigned)std::min((a.rows + 3) / 4, kMaxGrid);
+    if (a.k <= 64)
+        distill_short_kernel<T, MODE, R, 1><<<grid, 256, 0, s>>>(a);
+    else
+        distill_short_kernel<T, MODE, R, 4><<<grid, 256, 0, s>>>(a);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -708,9 +713,12 @@ int launch_resident(const Args &a, void *workspace, hipStream_t s) {
 
 template <typename T, Mode MODE>
 int launch_mode(const Args &a, hipStream_t s) {
-    if (a.vocab * (int64_t)sizeof(T) <= kShortBytes && a.k <= 256)
-        return a.k <= 64 ? launch_short<T, MODE, 1>(a, s) : launch_short<T, MODE, 4>(a, s);
-    if (a.vocab * (int64_t)sizeof(T) <= 32768) return launch_threads<T, 256, MODE>(a, s);
+    const int64_t bytes = a.vocab * (int64_t)sizeof(T);
+    if (bytes <= kShortBytes && a.k <= 256) return bytes <= 4096 ? launch_short<T, MODE, 4>(a, s) : launch_short<T, MODE, 16>(a, s);
+    // Blocks of 256 threads where every compute unit has rows for several, whose chains then overlap, or where a row is short.
+    // us, blocks of 1024 / 256: loss of 8192 x 20000 bf16 261 / 80, of 8192 x 50000 322 / 152, step on 8192 x 20000 342 / 184.
+    // A wave a row against a block of 256: step on 8192 x 3000 bf16 33.6 / 66.2, loss of 8192 x 5000 22.4 / 49.3.
+    if (bytes <= 32768 || a.rows >= kManyRows) return launch_threads<T, 256, MODE>(a, s);
     return launch_threads<T, 1024, MODE>(a, s);
 }
 
