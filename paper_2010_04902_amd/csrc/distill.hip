@@ -586,8 +586,8 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
     }
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
-        // A thread's sum of exp2((x - m) c).  The maximum of its first values is m: a sum in fp32 holds values up to
-        // 2^127 times that.  What goes beyond (or is not finite) is summed again with a running maximum.
+        // A thread's sum of exp2((x - m) c).  The maximum of its first values is m.  The row's sum of 1024 such sums has to stay
+        // below fp32's 2^128, so what reaches 2^117 (or is not finite) is summed again with a running maximum.
         const bool has_edge = tid < r.head + r.tail;
         RunningSum s;
         if (tid < r.vectors) {
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
             __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
         }
         if (has_edge) s.s += power((float)edge);
-        if (!(s.s < 0x1p120f)) {
+        if (!(s.s < 0x1p117f)) {
             s = RunningSum();
 #pragma unroll
             for (int v = 0; v < R; v++) {

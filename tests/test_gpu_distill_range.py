@@ -1,0 +1,56 @@
+"""Distillation at the ends of the logits' range: sums next to the border of fp32, banned entries at any temperature, rows
+far from 0, rows of the types' extreme values.
+
+The reference is test_gpu_worker's, in 64 bits, on logits less their row's maximum (loss and gradient do not change by that).
+Its tolerances go by the values' distances from the maximum then, not by their size, and by 200 temperatures of them at
+most: what lies lower weighs nothing.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2010_04902_amd as B
+from test_gpu_worker import BF16, DEV, E, F16, F32, _distill_case, _distill_check, _distill_reference, _near, _same_bits, _u
+
+pytestmark = pytest.mark.gpu
+
+TINY = {F32: 2.0 ** -149, BF16: 2.0 ** -134, F16: 2.0 ** -25}
+
+
+def _shifted_reference(logits, teacher, index, tau, dloss):
+    z = logits.double()
+    z = z - z.amax(dim=1, keepdim=True)
+    loss, lse, d, _, _, some = _distill_reference(z, teacher, index, tau, dloss)
+    near = _distill_reference(z.clamp_min(-200.0 * tau), teacher, index, tau, dloss)
+    return loss, lse, d, near[3], near[4], some
+
+
+def _check_gradient(got, ref, dtype, what, more=0.0):
+    _, _, want, _, scale, _ = ref
+    _near(got, want, _u(dtype) * want.abs() + (32 + more) * E * scale + TINY[dtype], what)
+
+
+def _check_loss(got, ref, what):
+    want, _, _, scale, _, _ = ref
+    _near(got, want, 2.0 ** -23 * want.abs() + 16 * E * scale, what)
+
+
+# ------------------------------------------------------------------ sums of rows held in registers
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("vocab", [40000, 65536, 131072])
+def test_rows_that_start_far_below_their_rest(vocab, dtype):
+    # the first 16 KB of a row, every thread's first values, lie so far below the others that a thread's sum in fp32, or the
+    # row's of 1024 such sums, reaches fp32's end
+    if dtype == F32 and vocab > 65536:
+        vocab = 61440
+    gaps = [0.0, 60.0, 69.0, 70.0, 76.0, 77.0, 77.5, 78.0, 78.5, 79.0, 83.0, 88.0, 100.0]
+    logits, teacher, index, dloss = _distill_case(130, vocab, 7, dtype, vocab)
+    logits.zero_()
+    first = 16384 // logits.element_size()
+    for i, gap in enumerate(gaps):
+        logits[i::len(gaps), first:] = gap
+    loss, lse, _, loss2, d2 = _distill_check(logits, teacher, index, dloss, 1.0)
+    assert bool(loss2.isfinite().all()) and bool(d2.isfinite().all())
