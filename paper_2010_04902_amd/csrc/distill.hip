@@ -63,11 +63,12 @@ struct RunningSum {
         for (int i = 0; i < N; i++) sum += __builtin_amdgcn_exp2f((x[i] - top) * c);
         s = sum, m = top;
     }
+    // The power is taken in halves: a sum of the resident kernel can be 2^117 of its m and weigh something where the power itself is
+    // less than fp32 has.
     __device__ __forceinline__ void join(float m2, float s2, float c) {
-        const float top = fmaxf(m, m2);
-        const float a = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * c);
-        const float b = m2 == -INFINITY ? s2 : s2 * __builtin_amdgcn_exp2f((m2 - top) * c);
-        s = a + b, m = top;
+        const float top = fmaxf(m, m2), half = 0.5f * c;
+        const float a = __builtin_amdgcn_exp2f((m - top) * half), b = __builtin_amdgcn_exp2f((m2 - top) * half);
+        s = (m == -INFINITY ? s : s * a * a) + (m2 == -INFINITY ? s2 : s2 * b * b), m = top;
     }
 };
 

@@ -54,3 +54,19 @@ def test_rows_that_start_far_below_their_rest(vocab, dtype):
         logits[i::len(gaps), first:] = gap
     loss, lse, _, loss2, d2 = _distill_check(logits, teacher, index, dloss, 1.0)
     assert bool(loss2.isfinite().all()) and bool(d2.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("vocab", [40000, 65536, 131072])
+def test_threads_whose_first_values_lie_far_apart(vocab, dtype):
+    # all threads but one start at 0 and have 78 next: their sums of e^78 count beside the one that starts at 84 to 90, although
+    # e^-87.4, what lies between their references, is 0 in fp32
+    if dtype == F32 and vocab > 65536:
+        vocab = 61440
+    logits, teacher, index, dloss = _distill_case(130, vocab, 7, dtype, vocab)
+    logits.zero_()
+    first = 16384 // logits.element_size()
+    logits[:, first:2 * first] = 78.0
+    for i, high in enumerate((84.0, 86.0, 87.0, 87.5, 88.0, 90.0)):
+        logits[i::6, first // 2] = high
+    _distill_check(logits, teacher, index, dloss, 1.0)
