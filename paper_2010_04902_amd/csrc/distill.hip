@@ -215,7 +215,8 @@ struct Softmax {
     __device__ __forceinline__ float less(float x, float p) const {
         const float d = x - m;
         if constexpr (sizeof(T) == 4) {
-            const float e = fmaf(d, c, fmaf(d, c_low, -l));
+            // c_low can be 0 or less: the small term of a banned entry, d = -inf, is that of a finite d, or the sum would be NaN
+            const float e = fmaf(d, c, fmaf(fmaxf(d, -0x1p64f), c_low, -l));
             const bool low = e < -100.0f;
             const float q = __builtin_amdgcn_exp2f(low ? e + 32.0f : e);
             return low ? (q - p * 0x1p32f) * (w * 0x1p-32f) : (q - p) * w;

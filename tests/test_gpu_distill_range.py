@@ -70,3 +70,19 @@ def test_threads_whose_first_values_lie_far_apart(vocab, dtype):
     for i, high in enumerate((84.0, 86.0, 87.0, 87.5, 88.0, 90.0)):
         logits[i::6, first // 2] = high
     _distill_check(logits, teacher, index, dloss, 1.0)
+
+
+# ------------------------------------------------------------------ banned entries
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("tau", [0.1, 0.7, 1.0, 3.0, 10.0])
+@pytest.mark.parametrize("rows,vocab", [(6, 40), (5, 3000), (4, 9000), (3, 70000), (1030, 20011), (130, 40000)])
+def test_banned_entries_at_any_temperature(rows, vocab, tau, dtype):
+    # log2(e) / temperature is rounded to fp32 upwards for some of these temperatures and downwards for others
+    logits, teacher, index, dloss = _distill_case(rows, vocab, 6, dtype, vocab + rows)
+    banned = torch.rand(rows, vocab, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV) < 0.4
+    banned.scatter_(1, index.clamp_min(0).long(), False)
+    logits.masked_fill_(banned, -math.inf)
+    _, _, d, _, d2 = _distill_check(logits, teacher, index, dloss, tau)
+    assert not bool(d[banned].any()) and not bool(d2[banned].any())
