@@ -226,27 +226,29 @@ struct Softmax {
     }
 };
 
-// The same from a row's sum of exp2(x c - m), for the resident kernel.  16-bit types: the exponent in one operation; the
-// rounding of m + l is 2^-24 of it, where q is rounded to 2^-9 of itself at best.
+// The same from a row's sum of exp2(x c - m), for the resident kernel.
+template <typename T>
+struct ScaledSoftmax;
+template <>
+struct ScaledSoftmax<float> : Softmax<float> {
+    using Softmax<float>::Softmax;
+};
+// 16-bit types: the exponent in one operation, x c - high.  m can be large (fp16 logits reach 65504) where q has 11 bits, so
+// only what is exact or accounted for is added to it: the sum's whole powers of two; what the addition's rounding took and
+// the sum's mantissa make a factor.  With m + log2(sum) rounded to fp32 instead q was 0.27 % off at logits of 60000.
 template <typename T>
 struct ScaledSoftmax {
-    static constexpr bool kWide = sizeof(T) == 4;
-    std::conditional_t<kWide, Softmax<float>, float> s;
-    float c, w;
-    __device__ ScaledSoftmax(float m, float sum, float temperature, float weight, float c_) : s(exponent(m, sum, temperature, weight, c_)), c(c_), w(weight) {}
-    static __device__ __forceinline__ auto exponent(float m, float sum, float temperature, float weight, float c) {
-        if constexpr (kWide)
-            return Softmax<float>(m, sum, temperature, weight, c);
-        else
-            return 32.0f - (m + __builtin_amdgcn_logf(sum));
+    float c, high, share, w;
+    __device__ ScaledSoftmax(float m, float sum, float, float weight, float c_) {
+        const float t = (float)(__builtin_amdgcn_frexp_expf(sum) - 32);
+        c = c_, high = m + t;
+        const float back = high - m, lost = (m - (high - back)) + (t - back);
+        share = __builtin_amdgcn_exp2f(-lost) / __builtin_amdgcn_frexp_mantf(sum), w = weight * 0x1p-32f;
     }
     __device__ __forceinline__ float less(float x, float p) const {
-        if constexpr (kWide)
-            return s.less(x, p);
-        else
-            return (__builtin_amdgcn_exp2f(fmaf(x, c, s)) - p * 0x1p32f) * (w * 0x1p-32f);
+        return (__builtin_amdgcn_exp2f(fmaf(x, c, -high)) * share - p * 0x1p32f) * w;
     }
-    __device__ __forceinline__ float weighted(float x) const { return less(x, 0.0f); }
+    __device__ __forceinline__ float weighted(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, c, -high)) * (share * w); }
 };
 
 // The gradient at the teacher's places; the dense part is written.
@@ -589,7 +591,7 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
         // A thread's sum of exp2((x - m) c).  The maximum of its first values is m.  The row's sum of 1024 such sums has to stay
-        // below fp32's 2^128, so what reaches 2^117 (or is not finite) is summed again with a running maximum.
+        // below fp32's 2^128, so what reaches 2^117 (or is not finite) is summed again from the maximum of all.
         const bool has_edge = tid < r.head + r.tail;
         RunningSum s;
         if (tid < r.vectors) {
@@ -600,34 +602,34 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
         } else if (has_edge) {
             s.m = scaled((float)edge);
         }
-        const float m0 = s.m;
-        auto power = [&](float v) { return __builtin_amdgcn_exp2f(kScaled ? fmaf(v, c, -m0) : (v - m0) * c); };
+        // of 16-bit values to a rounded product m: the product's rounding is in the sum, which the gradient takes into account
+        auto power = [&](float v, float m) { return __builtin_amdgcn_exp2f(kScaled ? fmaf(v, c, -m) : (v - m) * c); };
         const int vectors = (int)r.vectors, own = afresh(tid);
-#pragma unroll
-        for (int v = 0; v < R; v++) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < V; e++) sum += power(x[v][e]);
-            s.s += own + v * NT < vectors ? sum : 0.0f;
-            x[v].keep();
-            __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
-        }
-        if (has_edge) s.s += power((float)edge);
-        if (!(s.s < 0x1p117f)) {
-            s = RunningSum();
+        auto add_up = [&](float m) {
+            float all = 0.0f;
 #pragma unroll
             for (int v = 0; v < R; v++) {
-                float y[V];
+                float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < V; e++) y[e] = own + v * NT < vectors ? scaled(x[v][e]) : -INFINITY;
-                s.add(y, unit);
+                for (int e = 0; e < V; e++) sum += power(x[v][e], m);
+                all += own + v * NT < vectors ? sum : 0.0f;
+                x[v].keep();
+                __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
+            }
+            return has_edge ? all + power((float)edge, m) : all;
+        };
+        s.s = add_up(s.m);
+        if (!(s.s < 0x1p117f)) {
+            float top = has_edge ? fmaxf((float)edge, -INFINITY) : -INFINITY;
+#pragma unroll
+            for (int v = 0; v < R; v++) {
+#pragma unroll
+                for (int e = 0; e < V; e++) top = own + v * NT < vectors ? fmaxf(top, x[v][e]) : top;
                 x[v].keep();
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (has_edge) {
-                const float y[1] = {scaled((float)edge)};
-                s.add(y, unit);
-            }
+            s.m = scaled(top);
+            s.s = add_up(top == -INFINITY ? 0.0f : s.m);  // nothing but -inf, or NaN, which has to stay
         }
         s = row_join<NT>(s, unit, red);
         const int flags = sums[row].flags;

@@ -86,3 +86,45 @@ def test_banned_entries_at_any_temperature(rows, vocab, tau, dtype):
     logits.masked_fill_(banned, -math.inf)
     _, _, d, _, d2 = _distill_check(logits, teacher, index, dloss, tau)
     assert not bool(d[banned].any()) and not bool(d2[banned].any())
+
+
+# ------------------------------------------------------------------ rows far from 0
+
+
+def _far_case(rows, vocab, dtype, seed):
+    """Rows around many values, those of 16 bits with the few different ones that the type has there."""
+    logits, teacher, index, dloss = _distill_case(rows, vocab, 6, dtype, seed)
+    most = 6.0e4 if dtype == F16 else 3.0e5
+    shift = torch.tensor([0.0, 300.0, -300.0, 4.0e3, -4.0e3, 3.0e4, -3.0e4, most, -most], device=DEV)
+    shift = shift[torch.arange(rows, device=DEV) % 9].unsqueeze(1)
+    return (logits.float() + shift).to(dtype), teacher, index, dloss
+
+
+FAR = [(9, 40), (9, 3000), (9, 9000), (9, 70000), (1030, 20011), (130, 40000), (130, 65536)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("rows,vocab", FAR)
+def test_rows_far_from_zero(rows, vocab, tau, dtype):
+    logits, teacher, index, dloss = _far_case(rows, vocab, dtype, vocab)
+    ref = _shifted_reference(logits, teacher, index, tau, dloss)
+    loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, tau)
+    _check_loss(loss, ref, "loss of the step")
+    _check_gradient(d, ref, dtype, "dlogits of the step")
+    loss, lse = B.byz_distill_loss(logits, teacher, index, tau)
+    _check_loss(loss, ref, "loss")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("base", [0.0, 2.0e4, -6.0e4])
+def test_rows_held_in_registers_that_are_far_from_zero_and_start_below_their_rest(base, dtype):
+    # sums taken again with a maximum, next to ones that were not, with rounded products of either
+    logits, teacher, index, dloss = _distill_case(130, 40000, 6, dtype, 51)
+    logits = (logits.float() + base).to(dtype)
+    logits[:, :8192] -= 1024.0
+    logits[5:20, ::3] = base
+    ref = _shifted_reference(logits, teacher, index, 1.0, dloss)
+    loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, 1.0)
+    _check_loss(loss, ref, "loss")
+    _check_gradient(d, ref, dtype, "dlogits")
