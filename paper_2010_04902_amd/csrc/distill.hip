@@ -178,16 +178,17 @@ __device__ __forceinline__ void read_teacher(const Args &a, int64_t row, const T
     t.some = t.total > 0.0 || t.total != t.total;
 }
 
-// p, and the loss with the student's log-sum-exp lse
+// p, and the loss with the student's log-sum-exp m / tau + log_sum.  Logits are taken less m first: next to an m of 10^30 no
+// other term has a bit.
 template <int NT>
-__device__ __forceinline__ double loss_of(const Args &a, Teacher &t, double lse, int tid, double *red) {
+__device__ __forceinline__ double loss_of(const Args &a, Teacher &t, double m, double log_sum, int tid, double *red) {
     const double tau = a.temperature;
     double part = 0.0;
 #pragma unroll 1
     for (int j = tid; j < a.k; j += NT) {
         const double p = t.index[j] < 0 ? 0.0 : t.weight[j] / t.total;
         t.p[j] = (float)p;
-        if (p > 0.0) part += p * (log(p) - ((double)t.student[j] / tau - lse));
+        if (p > 0.0) part += p * (log(p) - (((double)t.student[j] - m) / tau - log_sum));
         if (p != p) part = NAN;
     }
     part = row_sum<NT>(part, red);
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
             }
             s = row_join<NT>(s, c, red);
             m = s.m, log_sum = log((double)s.s);
-            const double loss = loss_of<NT>(a, t, m / tau + log_sum, tid, red);
+            const double loss = loss_of<NT>(a, t, m, log_sum, tid, red);
             if (tid == 0) {
                 a.loss[row] = (float)loss;
                 if (a.lse) a.lse[row] = (float)(m / tau + log_sum);
@@ -409,15 +410,15 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
                 }
             s = wave_join(s, c);
             m = s.m, log_sum = log((double)s.s);
-            const double lse = m * inv + log_sum, log_total = log(total);
+            const double log_total = log(total);
             double part = 0.0;
 #pragma unroll
             for (int e = 0; e < E; e++)
-                if (weight[e] > 0.0) part += weight[e] * ((((double)t[e] - top) - (double)student[e]) * inv - log_total + lse);
+                if (weight[e] > 0.0) part += weight[e] * ((((double)t[e] - top) - ((double)student[e] - m)) * inv - log_total + log_sum);
             part = row_sum<64>(part, nullptr);
             if (lane == 0) {
                 a.loss[row] = !some ? 0.0f : total != total ? NAN : (float)(tau * tau * part);
-                if (a.lse) a.lse[row] = (float)lse;
+                if (a.lse) a.lse[row] = (float)(m * inv + log_sum);
             }
         } else {
             m = 0.0, log_sum = given;
@@ -463,10 +464,10 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
 // A row's part of the workspace of the resident kernel, beside its k places.
 struct RowSums {
     double entropy;  // sum of p log p
-    double dot, ps;  // sums of p s and p over the places
+    double dot, ps;  // sums of p (s - at) and p over the places
     float m, s;      // the student's maximum (16-bit types: times c) and sum
     int flags;       // kSome: an entry at all; kBroken: the row is NaN
-    int pad;
+    float at;        // the largest s of the places with weight: differences of logits keep what a sum of large ones loses
 };
 struct Place {
     float p, student;  // of all entries at the place; the student's logit
@@ -505,17 +506,24 @@ __global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, Place *pla
         total = row_sum<64>(total, nullptr);
         broken = __ballot(broken) != 0 || total != total;
         const bool some = total > 0.0 || broken;
+        float at = -INFINITY;
         for (int j = lane; j < a.k; j += 64) {
             const double w = index[j] < 0 || !some ? 0.0 : broken ? NAN : each[j] / total;
             each[j] = w;
-            if (w > 0.0) entropy += w * log(w), dot += w * (double)places[row * a.k + j].student, ps += w;
+            if (w > 0.0) at = fmaxf(at, places[row * a.k + j].student);
+        }
+        at = wave_reduce(at, [](float p, float q) { return fmaxf(p, q); });
+        if (at == -INFINITY) at = 0.0f;
+        for (int j = lane; j < a.k; j += 64) {
+            const double w = each[j];
+            if (w > 0.0) entropy += w * log(w), dot += w * ((double)places[row * a.k + j].student - (double)at), ps += w;
         }
         entropy = row_sum<64>(entropy, nullptr);
         dot = row_sum<64>(dot, nullptr);
         ps = row_sum<64>(ps, nullptr);
         if (lane == 0) {
             sums[row].entropy = entropy, sums[row].dot = dot, sums[row].ps = ps;
-            sums[row].flags = (some ? kSome : 0) | (broken ? kBroken : 0);
+            sums[row].flags = (some ? kSome : 0) | (broken ? kBroken : 0), sums[row].at = at;
         }
         for (int j0 = 0; j0 < a.k; j0 += 64) {
             const int32_t i = j0 + lane < a.k ? index[j0 + lane] : -1;
@@ -534,6 +542,49 @@ __global__ __launch_bounds__(256) void distill_teacher_kernel(Args a, Place *pla
     }
 }
 
+// Rows whose maximum in c times a value is not small beside 2^31: the rounding of such a product is no small power of two, and
+// past 2^128 there is no product (16-bit types; a row that is all banned, or masked with the type's lowest value).
+template <typename T>
+__device__ __forceinline__ bool is_far(float m) {
+    return sizeof(T) == 2 && !(fabsf(m) < 0x1p28f);
+}
+
+// A far row, of which the resident kernel has written nothing: its sum about its maximum and, where the teacher has an entry, its
+// dense gradient, by a wave.
+template <typename T>
+__device__ __forceinline__ Softmax<T> far_row(const Args &a, int64_t row, bool some, float weight, float c, RunningSum &s, int lane) {
+    constexpr int V = 16 / sizeof(T);
+    const Row<T> r(a.logits, row, a.ld, a.vocab);
+    const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
+    const bool has_edge = lane < r.head + r.tail;
+    s = RunningSum();
+    if (has_edge) {
+        const float x[1] = {(float)r.at[r.edge(lane)]};
+        s.add(x, c);
+    }
+    for (int64_t i = lane; i < r.vectors; i += 64) {
+        const Words<T, V> v = at[i];
+        float x[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) x[e] = v[e];
+        s.add(x, c);
+    }
+    s = wave_join(s, c);
+    const Softmax<T> q(s.m, log((double)s.s), a.temperature, weight);
+    if (some) {
+        T *out = (T *)a.dlogits + row * a.dlogits_ld;
+        if (has_edge) out[r.edge(lane)] = round_to<T>(q.weighted((float)r.at[r.edge(lane)]));
+        for (int64_t i = lane; i < r.vectors; i += 64) {
+            const Words<T, V> v = at[i];
+            ((Words<T, V> *)(out + r.head))[i] = Words<T, V>::of([&](int e) { return q.weighted(v[e]); });
+        }
+        // written, in the wave's order, before the teacher's places
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        __builtin_amdgcn_wave_barrier();
+    }
+    return q;
+}
+
 // The losses, and the gradient at the teacher's places (the dense part is written), a wave a row.
 template <typename T>
 __global__ __launch_bounds__(256) void distill_places_kernel(Args a, const Place *places, const RowSums *sums) {
@@ -542,19 +593,30 @@ __global__ __launch_bounds__(256) void distill_places_kernel(Args a, const Place
     const int lane = threadIdx.x % 64;
     for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
         const RowSums r = sums[row];
-        if (lane == 0) {
-            const double lse = (double)r.m / (sizeof(T) == 4 ? tau : (double)c * tau) + log((double)r.s);
-            a.loss[row] =
-                r.flags & kBroken ? NAN : r.flags & kSome ? (float)(tau * tau * (r.entropy - r.dot / tau + r.ps * lse)) : 0.0f;
-            if (a.lse) a.lse[row] = (float)lse;
-        }
-        if (!(r.flags & kSome)) continue;
-        const ScaledSoftmax<T> q(r.m, r.s, a.temperature, r.flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
-        T *out = (T *)a.dlogits + row * a.dlogits_ld;
-        for (int j = lane; j < a.k; j += 64) {
-            const int32_t i = a.index[row * a.teacher_ld + j];
-            const Place at = places[row * a.k + j];
-            if (i >= 0 && i < a.vocab) out[i] = round_to<T>(q.less(at.student, at.p));
+        const bool some = r.flags & kSome;
+        const float weight = r.flags & kBroken ? NAN : a.temperature * a.dloss[row];
+        auto finish = [&](double m, float s, const auto &q) {
+            if (lane == 0) {
+                const double log_sum = log((double)s);
+                a.loss[row] = r.flags & kBroken ? NAN
+                              : some            ? (float)(tau * tau * (r.entropy - (r.dot + r.ps * ((double)r.at - m)) / tau + r.ps * log_sum))
+                                                : 0.0f;
+                if (a.lse) a.lse[row] = (float)(m / tau + log_sum);
+            }
+            if (!some) return;
+            T *out = (T *)a.dlogits + row * a.dlogits_ld;
+            for (int j = lane; j < a.k; j += 64) {
+                const int32_t i = a.index[row * a.teacher_ld + j];
+                const Place at = places[row * a.k + j];
+                if (i >= 0 && i < a.vocab) out[i] = round_to<T>(q.less(at.student, at.p));
+            }
+        };
+        if (is_far<T>(r.m)) {
+            RunningSum s;
+            const Softmax<T> q = far_row<T>(a, row, some, weight, c, s, lane);
+            finish(s.m, s.s, q);
+        } else {
+            finish(sizeof(T) == 4 ? (double)r.m : (double)r.m / (double)c, r.s, ScaledSoftmax<T>(r.m, r.s, a.temperature, weight, c));
         }
     }
 }
@@ -629,7 +691,8 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
                 __builtin_amdgcn_sched_barrier(0);
             }
             s.m = scaled(top);
-            s.s = add_up(top == -INFINITY ? 0.0f : s.m);  // nothing but -inf, or NaN, which has to stay
+            // nothing but -inf (or NaN, which has to stay) adds up to 0, and so does what is far below: the row is far itself or has more
+            s.s = add_up(s.m == -INFINITY || is_far<T>(s.m) ? 0.0f : s.m);
         }
         s = row_join<NT>(s, unit, red);
         const int flags = sums[row].flags;
@@ -637,15 +700,16 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
         const bool some = flags & kSome;
         const ScaledSoftmax<T> q(s.m, s.s, a.temperature, flags & kBroken ? NAN : a.temperature * a.dloss[row], c);
         T *out = (T *)a.dlogits + row * a.dlogits_ld;
-        if (has_edge) {
+        const bool left = some && __builtin_amdgcn_readfirstlane((int)is_far<T>(s.m));  // to the places' kernel
+        if (has_edge && !left) {
             const int64_t e = r.edge(tid);
             out[e] = some ? round_to<T>(q.weighted((float)edge)) : (T)0.0f;
         }
         const int then = afresh(tid);
-        auto pass = [&](auto gradient, auto more, const Row<T> &next) {
+        auto pass = [&](auto gradient, auto store, auto more, const Row<T> &next) {
 #pragma unroll
             for (int v = 0; v < R; v++) {
-                if (then + v * NT < vectors)
+                if (store.value && then + v * NT < vectors)
                     put_past_caches(vector_of(out + r.head, then + v * NT), Words<T, V>::of([&](int e) { return gradient(x[v][e]); }));
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (more.value) {
@@ -659,14 +723,17 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
         if (row + gridDim.x < a.rows) {
             const Row<T> next(a.logits, row + gridDim.x, a.ld, a.vocab);
             load_edge(next);
-            if (some)
-                pass(weighted, std::true_type{}, next);
+            if (left)
+                pass(none, std::false_type{}, std::true_type{}, next);
+            else if (some)
+                pass(weighted, std::true_type{}, std::true_type{}, next);
             else
-                pass(none, std::true_type{}, next);
+                pass(none, std::true_type{}, std::true_type{}, next);
+        } else if (left) {
         } else if (some) {
-            pass(weighted, std::false_type{}, r);
+            pass(weighted, std::true_type{}, std::false_type{}, r);
         } else {
-            pass(none, std::false_type{}, r);
+            pass(none, std::true_type{}, std::false_type{}, r);
         }
     }
 }

@@ -128,3 +128,54 @@ def test_rows_held_in_registers_that_are_far_from_zero_and_start_below_their_res
     loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, 1.0)
     _check_loss(loss, ref, "loss")
     _check_gradient(d, ref, dtype, "dlogits")
+
+
+# ------------------------------------------------------------------ rows of extreme values
+
+
+def _extreme_case(rows, vocab, dtype):
+    """Rows that a mask has filled with a value far below all others, or with the type's lowest, wholly or but for a few."""
+    logits, teacher, index, dloss = _distill_case(rows, vocab, 6, dtype, 61)
+    index = torch.where(index >= 0, index % vocab, index)
+    info = torch.finfo(dtype)
+    values = [info.min, info.max, info.min / 2] + ([-6.0e4] if dtype == F16 else [-1.0e9, -3.0e9, -1.0e30, 1.0e20, -1.0e38])
+    at = 3
+    for value in values:
+        if at + 3 > rows:
+            break
+        logits[at] = value                      # nothing is left: all entries alike
+        logits[at + 1, ::2] = value             # half of it
+        logits[at + 2] = value                  # all but the teacher's places
+        logits[at + 2].scatter_(0, index[at + 2].clamp_min(0).long(), 2.0)
+        at += 3
+    return logits, teacher, index, dloss
+
+
+EXTREME = [(30, 40), (30, 3000), (30, 9000), (30, 70000), (1030, 20011), (130, 40000), (130, 65536)]
+
+
+def _extreme_rows(logits, index):
+    """Rows whose teacher's places are no further than 200 from the row's maximum, as far as the reference goes."""
+    z = logits.double()
+    near = z.gather(1, index.clamp_min(0).long()) >= z.amax(dim=1, keepdim=True) - 200.0
+    return (near | (index < 0)).all(dim=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("rows,vocab", EXTREME)
+def test_rows_of_extreme_values(rows, vocab, dtype):
+    logits, teacher, index, dloss = _extreme_case(rows, vocab, dtype)
+    keep = _extreme_rows(logits, index)
+    assert int(keep.sum()) > 8
+    for tau in (1.0, 2.0):
+        ref = [r[keep] for r in _shifted_reference(logits, teacher, index, tau, dloss)]
+        loss, lse = B.byz_distill_loss(logits, teacher, index, tau)
+        _check_loss(loss[keep], ref, "loss")
+        assert not bool(lse.isnan().any())
+        loss, d = B.byz_distill_loss_step(logits, teacher, index, dloss, tau)
+        _check_loss(loss[keep], ref, "loss of the step")
+        _check_gradient(d[keep], ref, dtype, "dlogits of the step")
+        assert bool(d.isfinite().all())  # of the others the gradient, too, is less than the weight
+        held = logits.clone()
+        loss3, d3 = B.byz_distill_loss_step(held, teacher, index, dloss, tau, out=held)
+        assert _same_bits(loss3, loss) and _same_bits(d3, d)
