@@ -86,6 +86,8 @@ int byz_distill_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld
 /*
  * The gradient for dloss (one value a row), from the call's lse:
  *     dlogits[i, v] = dloss[i] * temperature * (q_v - sum of p_j with index[j] = v).
+ * q has the rounding of lse to fp32 (2^-19 of it at most: a row with |lse| > 64 is summed again, at the price of a second
+ * pass over it).
  * dlogits (pitch dlogits_ld, type dtype) may be the logits themselves with the same pitch.
  */
 int byz_distill_loss_backward(const float *dloss, const void *logits, int64_t rows, int64_t vocab,
@@ -94,7 +96,8 @@ int byz_distill_loss_backward(const float *dloss, const void *logits, int64_t ro
                               int64_t dlogits_ld, void *stream);
 
 /* Loss and gradient in one call, for a dloss that is known beforehand (the weight of a row in a mean): the logits
- * are read once where a row fits a compute unit.  Same outputs as the two calls; lse may be NULL. */
+ * are read once where a row fits a compute unit.  The outputs of the two calls but for rounding (the gradient without that of
+ * lse); lse may be NULL. */
 size_t byz_distill_loss_step_workspace_bytes(int64_t rows, int64_t vocab, int k, int dtype);
 int byz_distill_loss_step(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
                           const float *teacher, const int32_t *index, int k, int64_t teacher_ld,

@@ -252,6 +252,10 @@ struct ScaledSoftmax {
     __device__ __forceinline__ float weighted(float x) const { return __builtin_amdgcn_exp2f(fmaf(x, c, -high)) * (share * w); }
 };
 
+// The gradient by its own call has a row's log-sum-exp in fp32, half a step of which is a share of q.  Up to here that is
+// 2^-19 of q, as much as the other terms' rounding; a row beyond (logits far from 0, or all of a mask's value) is summed again.
+__device__ __forceinline__ bool lse_is_good(float lse) { return fabsf(lse) <= 64.0f; }
+
 // The gradient at the teacher's places; the dense part is written.
 template <typename T, int NT>
 __device__ __forceinline__ void write_places(const Args &a, const Teacher &t, const Softmax<T> &q, T *out, int tid) {
@@ -279,7 +283,8 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
         read_teacher<T, NT>(a, row, r.at, t, tid, red);
         double m, log_sum;  // the student's log-sum-exp is m / tau + log_sum
-        if constexpr (MODE != kGradient) {
+        const float given = MODE == kGradient ? a.lse[row] : 0.0f;
+        if (MODE != kGradient || !lse_is_good(given)) {
             RunningSum s;
             if (tid < r.head + r.tail) {
                 const float x[1] = {(float)r.at[r.edge(tid)]};
@@ -308,13 +313,16 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
             }
             s = row_join<NT>(s, c, red);
             m = s.m, log_sum = log((double)s.s);
+        } else {
+            m = (float)(given * tau), log_sum = given - m / tau;
+        }
+        if constexpr (MODE != kGradient) {
             const double loss = loss_of<NT>(a, t, m, log_sum, tid, red);
             if (tid == 0) {
                 a.loss[row] = (float)loss;
                 if (a.lse) a.lse[row] = (float)(m / tau + log_sum);
             }
         } else {
-            m = 0.0, log_sum = a.lse[row];
 #pragma unroll 1
             for (int j = tid; j < a.k; j += NT) t.p[j] = t.index[j] < 0 ? 0.0f : (float)(t.weight[j] / t.total);
         }
@@ -394,7 +402,7 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < E; e++) weight[e] = index[e] < 0 ? 0.0 : weight[e] / total;
         double m, log_sum;
-        if constexpr (MODE != kGradient) {
+        if (MODE != kGradient || !lse_is_good(given)) {
             RunningSum s;
             if (has_edge) {
                 const float y[1] = {(float)edge};
@@ -410,6 +418,10 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
                 }
             s = wave_join(s, c);
             m = s.m, log_sum = log((double)s.s);
+        } else {
+            m = (float)(given * tau), log_sum = given - m * inv;
+        }
+        if constexpr (MODE != kGradient) {
             const double log_total = log(total);
             double part = 0.0;
 #pragma unroll
@@ -420,8 +432,6 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
                 a.loss[row] = !some ? 0.0f : total != total ? NAN : (float)(tau * tau * part);
                 if (a.lse) a.lse[row] = (float)(m * inv + log_sum);
             }
-        } else {
-            m = 0.0, log_sum = given;
         }
         if constexpr (MODE != kLoss) {
             float p[E] = {};

@@ -179,3 +179,35 @@ def test_rows_of_extreme_values(rows, vocab, dtype):
         held = logits.clone()
         loss3, d3 = B.byz_distill_loss_step(held, teacher, index, dloss, tau, out=held)
         assert _same_bits(loss3, loss) and _same_bits(d3, d)
+
+
+# ------------------------------------------------------------------ the gradient by its own call
+
+# It has the row's log-sum-exp in fp32: half a step of that is 2^-24 of 64 at most where it is used, 64 E of q.  Larger ones are
+# not used.
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("rows,vocab", FAR)
+def test_gradient_of_rows_far_from_zero(rows, vocab, tau, dtype):
+    logits, teacher, index, dloss = _far_case(rows, vocab, dtype, vocab)
+    ref = _shifted_reference(logits, teacher, index, tau, dloss)
+    _, lse = B.byz_distill_loss(logits, teacher, index, tau)
+    d = B.byz_distill_loss_backward(dloss, logits, teacher, index, lse, tau)
+    _check_gradient(d, ref, dtype, "dlogits", more=64)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("rows,vocab", EXTREME)
+def test_gradient_of_rows_of_extreme_values(rows, vocab, dtype):
+    logits, teacher, index, dloss = _extreme_case(rows, vocab, dtype)
+    keep = _extreme_rows(logits, index)
+    for tau in (0.5, 2.0):
+        ref = [r[keep] for r in _shifted_reference(logits, teacher, index, tau, dloss)]
+        _, lse = B.byz_distill_loss(logits, teacher, index, tau)
+        d = B.byz_distill_loss_backward(dloss, logits, teacher, index, lse, tau)
+        _check_gradient(d[keep], ref, dtype, "dlogits", more=64)
+        assert bool(d.isfinite().all())
+        held = logits.clone()
+        assert _same_bits(B.byz_distill_loss_backward(dloss, held, teacher, index, lse, tau, out=held), d)
