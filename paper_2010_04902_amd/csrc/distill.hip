@@ -120,21 +120,40 @@ __device__ __forceinline__ double row_max(double v, double *lds) {
     return row_reduce<NT>(v, -INFINITY, lds, [](double a, double b) { return fmax(a, b); });
 }
 
-// A row's vocabulary as 16-byte vectors between a few single elements on either side.
+// The values that start in the middle of v's first word and end in that of `next`.
+template <typename T, int V>
+__device__ __forceinline__ Words<T, V> shifted(Words<T, V> v, word_t next) {
+#pragma unroll
+    for (int w = 0; w < v.N; w++) v.w[w] = __builtin_amdgcn_alignbit(w + 1 < v.N ? v.w[w + 1] : next, v.w[w], 16);
+    return v;
+}
+
+// A row's vocabulary as vectors of 16 bytes from its start on, wherever that lies, and a few single elements behind them.
 template <typename T>
 struct Row {
     static constexpr int V = 16 / sizeof(T);
     const T *at;
-    int head, tail;
+    int tail;
     int64_t vectors;
     __device__ Row(const void *base, int64_t row, int64_t ld, int64_t vocab) {
         at = (const T *)base + row * ld;
-        const int off = (int)((16 - ((uintptr_t)at & 15)) & 15) / (int)sizeof(T);
-        head = vocab < off ? (int)vocab : off;
-        vectors = (vocab - head) / V;
-        tail = (int)(vocab - head - vectors * V);
+        vectors = vocab / V;
+        tail = (int)(vocab - vectors * V);
     }
-    __device__ int64_t edge(int t) const { return t < head ? t : vectors * V + t; }  // the t-th single element
+    __device__ __forceinline__ Words<T, V> vector(int64_t i) const { return get_words<T, V>(at + i * V); }
+    // A row that starts at an odd multiple of two bytes: the hardware is slower to load vectors there than at whole words, so the
+    // words that hold their values are loaded and shifted.  us on 8192 x 50016 bf16 as it comes / shifted: loss 176 / 149
+    // (aligned 152), step 418 / 385 (354).  The half words beside the row that are loaded too are in one word with its values.
+    __device__ __forceinline__ bool odd() const { return sizeof(T) == 2 && ((uintptr_t)at & 2) != 0; }
+    template <bool ODD>
+    __device__ __forceinline__ Words<T, V> vector_of(int64_t i) const {
+        if constexpr (ODD && sizeof(T) == 2) {
+            return shifted(get_words<T, V>(at + i * V - 1), *(const word_t *)(at + i * V + V - 1));
+        } else {
+            return vector(i);
+        }
+    }
+    __device__ int64_t edge(int t) const { return vectors * V + t; }  // the t-th single element
 };
 
 // A row's teacher in LDS: places (-1: no entry), exp(z - top), p, and the student's logits there.
@@ -274,7 +293,7 @@ template <typename T, int NT, Mode MODE>
 __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
     extern __shared__ char lds_raw[];
     __shared__ double red[32];
-    constexpr int V = 16 / sizeof(T), kUnroll = 4;
+    constexpr int V = 16 / sizeof(T);
     const int tid = threadIdx.x;
     const double tau = a.temperature;
     const float c = (float)(1.4426950408889634 / tau);
@@ -286,31 +305,37 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
         const float given = MODE == kGradient ? a.lse[row] : 0.0f;
         if (MODE != kGradient || !lse_is_good(given)) {
             RunningSum s;
-            if (tid < r.head + r.tail) {
+            if (tid < r.tail) {
                 const float x[1] = {(float)r.at[r.edge(tid)]};
                 s.add(x, c);
             }
-            const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
-            int64_t i = tid;
-            for (; i + (kUnroll - 1) * NT < r.vectors; i += kUnroll * NT) {
-                Words<T, V> v[kUnroll];
+            auto add_up = [&](auto odd) {
+                constexpr int kUnroll = MODE == kGradient ? 1 : odd.value ? 3 : 4;
+                int64_t i = tid;
+                for (; i + (kUnroll - 1) * NT < r.vectors; i += kUnroll * NT) {
+                    Words<T, V> v[kUnroll];
 #pragma unroll
-                for (int u = 0; u < kUnroll; u++) v[u] = at[i + u * NT];
+                    for (int u = 0; u < kUnroll; u++) v[u] = r.template vector_of<odd.value>(i + u * NT);
 #pragma unroll
-                for (int u = 0; u < kUnroll; u++) {
+                    for (int u = 0; u < kUnroll; u++) {
+                        float x[V];
+#pragma unroll
+                        for (int e = 0; e < V; e++) x[e] = v[u][e];
+                        s.add(x, c);
+                    }
+                }
+                for (; i < r.vectors; i += NT) {
+                    const Words<T, V> v = r.template vector_of<odd.value>(i);
                     float x[V];
 #pragma unroll
-                    for (int e = 0; e < V; e++) x[e] = v[u][e];
+                    for (int e = 0; e < V; e++) x[e] = v[e];
                     s.add(x, c);
                 }
-            }
-            for (; i < r.vectors; i += NT) {
-                const Words<T, V> v = at[i];
-                float x[V];
-#pragma unroll
-                for (int e = 0; e < V; e++) x[e] = v[e];
-                s.add(x, c);
-            }
+            };
+            if (r.odd())
+                add_up(std::true_type{});
+            else
+                add_up(std::false_type{});
             s = row_join<NT>(s, c, red);
             m = s.m, log_sum = log((double)s.s);
         } else {
@@ -329,23 +354,21 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
         if constexpr (MODE != kLoss) {
             const Softmax<T> q(m, log_sum, tau, t.total != t.total ? NAN : a.temperature * a.dloss[row]);
             T *out = (T *)a.dlogits + row * a.dlogits_ld;
-            const bool pieces = (((uintptr_t)out ^ (uintptr_t)r.at) & 15) == 0;
             __syncthreads();  // the logits at the teacher's places are read: they may be written now
-            if (tid < r.head + r.tail) {
+            if (tid < r.tail) {
                 const int64_t e = r.edge(tid);
                 out[e] = t.some ? round_to<T>(q.weighted((float)r.at[e])) : (T)0.0f;
             }
-            const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
-            for (int64_t i = tid; i < r.vectors; i += NT) {
-                const Words<T, V> v = at[i];
-                const Words<T, V> d = Words<T, V>::of([&](int e) { return t.some ? q.weighted(v[e]) : 0.0f; });
-                if (pieces) {
-                    ((Words<T, V> *)(out + r.head))[i] = d;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; e++) out[r.head + i * V + e] = round_to<T>(d[e]);
+            auto write = [&](auto odd) {
+                for (int64_t i = tid; i < r.vectors; i += NT) {
+                    const Words<T, V> v = r.template vector_of<odd.value>(i);
+                    put_words(out + i * V, Words<T, V>::of([&](int e) { return t.some ? q.weighted(v[e]) : 0.0f; }));
                 }
-            }
+            };
+            if (r.odd())
+                write(std::true_type{});
+            else
+                write(std::false_type{});
             __syncthreads();  // the dense part is written: the teacher's places again
             if (t.some) write_places<T, NT>(a, t, q, out, tid);
         }
@@ -357,10 +380,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
 template <typename T, Mode MODE, int R, int E>
 __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
     constexpr int V = 16 / sizeof(T);
-    const int lane = threadIdx.x % 64;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const double tau = a.temperature, inv = 1.0 / tau;
     const float c = (float)(1.4426950408889634 / tau);
-    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < a.rows; row += (int64_t)gridDim.x * 4) {
+    for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < a.rows; row += (int64_t)gridDim.x * 4) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
         int32_t index[E];
         float t[E], student[E];
@@ -371,11 +394,10 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
             if (j < a.k) index[e] = a.index[row * a.teacher_ld + j], t[e] = a.teacher[row * a.teacher_ld + j];
         }
         Words<T, V> x[R];
-        const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
 #pragma unroll
         for (int v = 0; v < R; v++)
-            if (v * 64 + lane < r.vectors) x[v] = at[v * 64 + lane];
-        const bool has_edge = lane < r.head + r.tail;
+            if (v * 64 + lane < r.vectors) x[v] = get_words<T, V>(r.at + (uint32_t)(v * 64 + lane) * V);
+        const bool has_edge = lane < r.tail;
         T edge = (T)0.0f;
         if (has_edge) edge = r.at[r.edge(lane)];
         const float given = MODE == kGradient ? a.lse[row] : 0.0f, dloss = MODE == kLoss ? 0.0f : a.dloss[row];
@@ -447,20 +469,11 @@ __global__ __launch_bounds__(256) void distill_short_kernel(Args a) {
             }
             const Softmax<T> q(m, log_sum, tau, total != total ? NAN : a.temperature * dloss);
             T *out = (T *)a.dlogits + row * a.dlogits_ld;
-            const bool pieces = (((uintptr_t)out ^ (uintptr_t)r.at) & 15) == 0;
             if (has_edge) out[r.edge(lane)] = some ? round_to<T>(q.weighted((float)edge)) : (T)0.0f;
 #pragma unroll
             for (int v = 0; v < R; v++)
-                if (v * 64 + lane < r.vectors) {
-                    const Words<T, V> d = Words<T, V>::of([&](int i) { return some ? q.weighted(x[v][i]) : 0.0f; });
-                    T *to = out + r.head + (v * 64 + lane) * V;
-                    if (pieces) {
-                        *(Words<T, V> *)to = d;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < V; i++) to[i] = round_to<T>(d[i]);
-                    }
-                }
+                if (v * 64 + lane < r.vectors)
+                    put_words(out + (uint32_t)(v * 64 + lane) * V, Words<T, V>::of([&](int i) { return some ? q.weighted(x[v][i]) : 0.0f; }));
             // the dense part is written, in the wave's order: the teacher's places again
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
             __builtin_amdgcn_wave_barrier();
@@ -565,15 +578,14 @@ template <typename T>
 __device__ __forceinline__ Softmax<T> far_row(const Args &a, int64_t row, bool some, float weight, float c, RunningSum &s, int lane) {
     constexpr int V = 16 / sizeof(T);
     const Row<T> r(a.logits, row, a.ld, a.vocab);
-    const Words<T, V> *at = (const Words<T, V> *)(r.at + r.head);
-    const bool has_edge = lane < r.head + r.tail;
+    const bool has_edge = lane < r.tail;
     s = RunningSum();
     if (has_edge) {
         const float x[1] = {(float)r.at[r.edge(lane)]};
         s.add(x, c);
     }
     for (int64_t i = lane; i < r.vectors; i += 64) {
-        const Words<T, V> v = at[i];
+        const Words<T, V> v = r.vector(i);
         float x[V];
 #pragma unroll
         for (int e = 0; e < V; e++) x[e] = v[e];
@@ -585,8 +597,8 @@ __device__ __forceinline__ Softmax<T> far_row(const Args &a, int64_t row, bool s
         T *out = (T *)a.dlogits + row * a.dlogits_ld;
         if (has_edge) out[r.edge(lane)] = round_to<T>(q.weighted((float)r.at[r.edge(lane)]));
         for (int64_t i = lane; i < r.vectors; i += 64) {
-            const Words<T, V> v = at[i];
-            ((Words<T, V> *)(out + r.head))[i] = Words<T, V>::of([&](int e) { return q.weighted(v[e]); });
+            const Words<T, V> v = r.vector(i);
+            put_words(out + i * V, Words<T, V>::of([&](int e) { return q.weighted(v[e]); }));
         }
         // written, in the wave's order, before the teacher's places
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
@@ -631,8 +643,7 @@ __global__ __launch_bounds__(256) void distill_places_kernel(Args a, const Place
     }
 }
 
-// The dense gradients and the student's sums.  R vectors of a row in each of 1024 threads' registers; for rows whose logits
-// and gradients lie at the same place within 16 bytes.
+// The dense gradients and the student's sums.  R vectors of a row in each of 1024 threads' registers.
 template <typename T, int R>
 __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums *sums) {
     constexpr int V = 16 / sizeof(T), NT = 1024;
@@ -643,16 +654,20 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
     T edge = (T)0.0f;
     // A row here is shorter than 2^31 bytes.  A thread's number `own` is made afresh for each use, or the places of all R
     // vectors would be kept in registers; threads without a v-th vector load the last, without a branch, and leave it.
-    auto vector_of = [](const T *base, int number) { return (Words<T, V> *)((char *)base + (uint32_t)number * 16u); };
+    auto vector_at = [](auto *base, int number) { return base + (uint32_t)number * (uint32_t)V; };
+    // Of an odd row x has the words that hold the values but for the last value's; shifted where the row is begun.
+    word_t next_word[R];
     auto load = [&](const Row<T> &r, int own, int v) {
-        x[v] = *vector_of(r.at + r.head, std::min(own + v * NT, (int)r.vectors - 1));
+        const T *from = vector_at(r.at - (r.odd() ? 1 : 0), std::min(own + v * NT, (int)r.vectors - 1));
+        x[v] = get_words<T, V>(from);
+        if (r.odd()) next_word[v] = *(const word_t *)(from + V);
     };
     // 16-bit types: sums are of exp2(x c - m) with m = c times a value, rounded: one operation for the exponent
     constexpr bool kScaled = sizeof(T) == 2;
     const float unit = kScaled ? 1.0f : c;
     auto scaled = [&](float v) { return kScaled ? v * c : v; };
     auto load_edge = [&](const Row<T> &r) {
-        if (tid < r.head + r.tail) edge = r.at[r.edge(tid)];
+        if (tid < r.tail) edge = r.at[r.edge(tid)];
     };
     {
         const Row<T> r(a.logits, blockIdx.x, a.ld, a.vocab);
@@ -662,9 +677,13 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
     }
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
+        if constexpr (sizeof(T) == 2)
+            if (r.odd())
+#pragma unroll
+                for (int v = 0; v < R; v++) x[v] = shifted(x[v], next_word[v]);
         // A thread's sum of exp2((x - m) c).  The maximum of its first values is m.  The row's sum of 1024 such sums has to stay
         // below fp32's 2^128, so what reaches 2^117 (or is not finite) is summed again from the maximum of all.
-        const bool has_edge = tid < r.head + r.tail;
+        const bool has_edge = tid < r.tail;
         RunningSum s;
         if (tid < r.vectors) {
             float top = x[0][0];
@@ -720,7 +739,7 @@ __global__ __launch_bounds__(1024) void distill_resident_kernel(Args a, RowSums 
 #pragma unroll
             for (int v = 0; v < R; v++) {
                 if (store.value && then + v * NT < vectors)
-                    put_past_caches(vector_of(out + r.head, then + v * NT), Words<T, V>::of([&](int e) { return gradient(x[v][e]); }));
+                    put_past_caches(vector_at(out, then + v * NT), Words<T, V>::of([&](int e) { return gradient(x[v][e]); }));
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (more.value) {
                     load(next, then, v);
@@ -868,14 +887,11 @@ extern "C" int byz_distill_loss_step(const void *logits, int64_t rows, int64_t v
     const int rc = check_gradient(a, dtype);
     if (rc != BYZ_OK || rows == 0) return rc;
     if (!loss) return BYZ_EINVAL;
-    const bool alike = ((((uintptr_t)logits ^ (uintptr_t)dlogits) | (uintptr_t)((ld - dlogits_ld) * dtype_size(dtype))) & 15) == 0;
     if (fits_resident(rows, vocab, dtype)) {
         if (workspace_bytes < resident_bytes(rows, k) || !workspace || !aligned(workspace, 16)) return BYZ_ENOMEM;
-        if (alike) {
-            const hipStream_t s = (hipStream_t)stream;
-            return dtype == BYZ_F32 ? launch_resident<float>(a, workspace, s)
-                   : dtype == BYZ_BF16 ? launch_resident<bf16>(a, workspace, s) : launch_resident<f16>(a, workspace, s);
-        }
+        const hipStream_t s = (hipStream_t)stream;
+        return dtype == BYZ_F32 ? launch_resident<float>(a, workspace, s)
+               : dtype == BYZ_BF16 ? launch_resident<bf16>(a, workspace, s) : launch_resident<f16>(a, workspace, s);
     }
     return launch<kStep>(a, dtype, (hipStream_t)stream);
 }

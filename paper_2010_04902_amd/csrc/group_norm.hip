@@ -592,7 +592,7 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(Args a) {
         const int64_t pixel[1] = {a.xp};
         with_act(a.act, [&](auto act) {
             each_position<T, V, 4, 1>(q, t, at, pixel, [&](int r, const Words<T, V>(&x)[1]) {
-                put_past_caches((Words<T, V> *)(to + (int64_t)r * q.ty * a.op), normalised<act.value>(f, x[0]));
+                put_past_caches(to + (int64_t)r * q.ty * a.op, normalised<act.value>(f, x[0]));
             });
         });
     }
@@ -785,7 +785,7 @@ __global__ __launch_bounds__(256) void norm_backward_apply_kernel(Args a) {
         const int64_t pixel[2] = {a.xp, a.dp};
         with_act(a.act, [&](auto act) {
             each_position<T, V, 2, 2>(q, t, at, pixel, [&](int r, const Words<T, V>(&v)[2]) {
-                put_past_caches((Words<T, V> *)(to + (int64_t)r * q.ty * a.op), gradient<act.value>(f, k1, k0, v[0], v[1]));
+                put_past_caches(to + (int64_t)r * q.ty * a.op, gradient<act.value>(f, k1, k0, v[0], v[1]));
             });
         });
     }

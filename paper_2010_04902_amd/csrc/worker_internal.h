@@ -106,14 +106,27 @@ struct Words<T, 1> {
     __device__ __forceinline__ void keep() {}
 };
 
+// Loaded and stored in one piece at any address of a T: the hardware takes vectors at an element's alignment, so which values
+// a thread holds, and with it the order of sums, need not depend on where a tensor lies.
+template <typename T, int V>
+__device__ __forceinline__ Words<T, V> get_words(const T *from) {
+    Words<T, V> v;
+    __builtin_memcpy(&v, from, sizeof(v));
+    return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ void put_words(T *to, const Words<T, V> &v) {
+    __builtin_memcpy(to, &v, sizeof(v));
+}
+
 // Stored past the caches: for results larger than these, in whose place they keep the inputs, which are read again.
 template <typename T, int V>
-__device__ __forceinline__ void put_past_caches(Words<T, V> *to, const Words<T, V> &v) {
+__device__ __forceinline__ void put_past_caches(T *to, const Words<T, V> &v) {
     if constexpr (sizeof(v) == 16) {
-        typedef uint32_t words4 __attribute__((ext_vector_type(4), may_alias));
+        typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(2), may_alias));
         __builtin_nontemporal_store(__builtin_bit_cast(words4, v), (words4 *)to);
     } else {
-        *to = v;
+        put_words(to, v);
     }
 }
 
