@@ -57,22 +57,13 @@ struct Plan {
     int64_t chunk;
 };
 
-struct View {
-    const void *at;
-    int64_t sample, pixel;
-};
-
 int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
 
-// Largest number of neighbouring elements that all views load in one piece.
-int widest_vec(int elem, int64_t c, std::initializer_list<View> views) {
-    for (int vec : {16 / elem, 4 / elem, 1}) {
-        if (vec < 1 || c % vec) continue;
-        bool ok = true;
-        for (const View &v : views)
-            ok = ok && aligned(v.at, (size_t)vec * elem) && v.sample % vec == 0 && v.pixel % vec == 0;
-        if (ok) return vec;
-    }
+// Neighbouring elements that are loaded in one piece, at any address of an element: a plan goes by sizes and type alone, or the
+// order of the sums would change with the place of a tensor.
+int widest_vec(int elem, int64_t c) {
+    for (int vec : {16 / elem, 4 / elem})
+        if (c % vec == 0) return vec;
     return 1;
 }
 
@@ -87,9 +78,9 @@ int64_t chunk_of(const Plan &q, int64_t slices, int64_t blocks) {
 }
 
 // False: more tiles than can be counted.
-bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int elem, int vec, bool forward) {
+bool make_plan(Plan &q, int64_t n, int64_t p, int64_t c, int64_t groups, int elem, bool forward) {
     const int max_r = forward ? kForwardR : kBackwardR;
-    int max_threads;
+    int max_threads, vec = widest_vec(elem, c);
     q = Plan{};
     const int64_t gc = c / groups;
     int64_t slices, step;
@@ -420,7 +411,7 @@ __device__ __forceinline__ void each_position(const Plan &q, const Tile &t, cons
         for (int u = 0; u < U; u++)
             if (all || t.ty + (r + u) * q.ty < t.np)
 #pragma unroll
-                for (int j = 0; j < N; j++) v[u][j] = *(const Words<T, V> *)(at[j] + (int64_t)(r + u) * q.ty * pixel[j]);
+                for (int j = 0; j < N; j++) v[u][j] = get_words<T, V>(at[j] + (int64_t)(r + u) * q.ty * pixel[j]);
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (all || t.ty + (r + u) * q.ty < t.np) {
@@ -469,7 +460,7 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
         int count = 0;
 #pragma unroll
         for (int r = 0; r < R; r++)
-            if (t.mine && t.ty + r * q.ty < t.np) x[r] = *(const Words<T, V> *)(at + (int64_t)r * q.ty * a.xp), count++;
+            if (t.mine && t.ty + r * q.ty < t.np) x[r] = get_words<T, V>(at + (int64_t)r * q.ty * a.xp), count++;
         // counted from the thread's first value, x[0]
         float m[V] = {}, d[V] = {};
 #pragma unroll
@@ -512,7 +503,7 @@ __global__ __launch_bounds__(kForwardThreads) void norm_whole_kernel(Args a) {
 #pragma unroll
                 for (int r = 0; r < R; r++)
                     if (r < count) {
-                        *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = normalised<act.value>(f, x[r]);
+                        put_words(to + (int64_t)r * q.ty * a.op, normalised<act.value>(f, x[r]));
                         __builtin_amdgcn_sched_barrier(0);
                     }
             });
@@ -626,9 +617,10 @@ __device__ __forceinline__ Words<T, V> gradient(const Affine<V> &f, const float 
     });
 }
 
-// Backward, a whole slice in registers: the channels' A and B, and dx.
+// Backward, a whole slice in registers: the channels' A and B, and dx.  Up to four vectors a thread in 128 registers, so that two
+// blocks share a compute unit: 64 x 14 x 14 x 1024 takes 33 (bf16) and 35 us (fp16, 7 values in memory) so, 42 with more.
 template <typename T, int V, int R>
-__global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(Args a) {
+__global__ __launch_bounds__(kBackwardThreads, R <= 4 ? 4 : 2) void norm_backward_whole_kernel(Args a) {
     extern __shared__ float lds[];
     const Plan &q = a.q;
     const int cs = q.cs;
@@ -644,8 +636,8 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
 #pragma unroll
         for (int r = 0; r < R; r++)
             if (t.mine && t.ty + r * q.ty < t.np) {
-                x[r] = *(const Words<T, V> *)(xat + (int64_t)r * q.ty * a.xp);
-                dy[r] = *(const Words<T, V> *)(dat + (int64_t)r * q.ty * a.dp);
+                x[r] = get_words<T, V>(xat + (int64_t)r * q.ty * a.xp);
+                dy[r] = get_words<T, V>(dat + (int64_t)r * q.ty * a.dp);
                 count++;
             }
         const Affine<V> f(a, t, [&](int g) { return mean[g]; }, [&](int g) { return rstd[g]; });
@@ -682,7 +674,7 @@ __global__ __launch_bounds__(kBackwardThreads) void norm_backward_whole_kernel(A
 #pragma unroll
                 for (int r = 0; r < R; r++)
                     if (r < count) {
-                        *(Words<T, V> *)(to + (int64_t)r * q.ty * a.op) = gradient<act.value>(f, k1, k0, x[r], dy[r]);
+                        put_words(to + (int64_t)r * q.ty * a.op, gradient<act.value>(f, k1, k0, x[r], dy[r]));
                         __builtin_amdgcn_sched_barrier(0);
                     }
             });
@@ -898,18 +890,6 @@ bool sizes_ok(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
            !__builtin_mul_overflow(n, p, &all) && !__builtin_mul_overflow(all, c, &all) && all <= (INT64_MAX >> 8);
 }
 
-// Workspace of either direction, for any alignment: the most that a plan takes of the widths that a call can have.
-template <typename F>
-size_t most_bytes(int64_t n, int64_t p, int64_t c, int groups, int elem, bool forward, F bytes) {
-    size_t most = 0;
-    for (int vec : {16 / elem, 4 / elem, 1}) {
-        Plan q;
-        if (vec < 1 || c % vec || !make_plan(q, n, p, c, groups, elem, vec, forward)) continue;
-        most = std::max(most, bytes(q));
-    }
-    return most;
-}
-
 size_t forward_bytes(const Plan &q) { return whole(q) ? 0 : round_up(sizeof(Stat) * q.n * q.groups * q.chunks * q.parts); }
 
 struct BackwardLayout {
@@ -926,8 +906,8 @@ struct BackwardLayout {
 
 extern "C" size_t byz_group_norm_workspace_bytes(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
     if (!sizes_ok(n, p, c, groups, dtype) || n == 0 || p == 0) return 0;
-    const int elem = (int)dtype_size(dtype);
-    return most_bytes(n, p, c, groups, elem, true, [](const Plan &q) { return forward_bytes(q); });
+    Plan q;
+    return make_plan(q, n, p, c, groups, (int)dtype_size(dtype), true) ? forward_bytes(q) : 0;
 }
 
 extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, int64_t n, int64_t p, int64_t c,
@@ -949,9 +929,8 @@ extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, 
         if (pixel < c || !extent_ok(p, pixel, c)) return BYZ_EINVAL;
     if (!extent_ok(n, x_sample, (p - 1) * x_pixel + c) || !extent_ok(n, y_sample, (p - 1) * y_pixel + c)) return BYZ_EINVAL;
     if (n > 1 && y_sample < (p - 1) * y_pixel + c) return BYZ_EINVAL;  // samples of the output may not overlap
-    const int vec = widest_vec(elem, c, {{x, x_sample, x_pixel}, {y, y_sample, y_pixel}});
     Args a{};
-    if (!make_plan(a.q, n, p, c, groups, elem, vec, true)) return BYZ_EUNSUPPORTED;
+    if (!make_plan(a.q, n, p, c, groups, elem, true)) return BYZ_EUNSUPPORTED;
     if (forward_bytes(a.q) > workspace_bytes || (forward_bytes(a.q) && (!workspace || !aligned(workspace, 16)))) return BYZ_ENOMEM;
     a.x = x, a.xs = x_sample, a.xp = x_pixel;
     a.out = y, a.os = y_sample, a.op = y_pixel;
@@ -962,8 +941,8 @@ extern "C" int byz_group_norm(const void *x, int64_t x_sample, int64_t x_pixel, 
 
 extern "C" size_t byz_group_norm_backward_workspace_bytes(int64_t n, int64_t p, int64_t c, int groups, int dtype) {
     if (!sizes_ok(n, p, c, groups, dtype) || n == 0 || p == 0) return 0;
-    const int elem = (int)dtype_size(dtype);
-    return most_bytes(n, p, c, groups, elem, false, [](const Plan &q) { return BackwardLayout(q).bytes; });
+    Plan q;
+    return make_plan(q, n, p, c, groups, (int)dtype_size(dtype), false) ? BackwardLayout(q).bytes : 0;
 }
 
 extern "C" int byz_group_norm_backward(const void *dy, int64_t dy_sample, int64_t dy_pixel, const void *x,
@@ -990,8 +969,7 @@ extern "C" int byz_group_norm_backward(const void *dy, int64_t dy_sample, int64_
         !extent_ok(n, dx_sample, (p - 1) * dx_pixel + c))
         return BYZ_EINVAL;
     if (n > 1 && dx_sample < (p - 1) * dx_pixel + c) return BYZ_EINVAL;
-    const int vec = widest_vec(elem, c, {{dy, dy_sample, dy_pixel}, {x, x_sample, x_pixel}, {dx, dx_sample, dx_pixel}});
-    if (!make_plan(a.q, n, p, c, groups, elem, vec, false)) return BYZ_EUNSUPPORTED;
+    if (!make_plan(a.q, n, p, c, groups, elem, false)) return BYZ_EUNSUPPORTED;
     const BackwardLayout lay(a.q);
     if (!workspace || lay.bytes > workspace_bytes || !aligned(workspace, 16)) return BYZ_ENOMEM;
     a.x = x, a.xs = x_sample, a.xp = x_pixel;

@@ -54,3 +54,31 @@ def test_distillation_of_a_file_in_a_batch():
         a = B.byz_distill_loss_step(logits[rows], teacher[rows], index[rows], dloss[rows], 2.0)
         b = B.byz_distill_loss_step(logits[rows].clone(), teacher[rows].clone(), index[rows].clone(), dloss[rows].clone(), 2.0)
         assert _same_bits(a[0], b[0]) and _same_bits(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("shape", [
+    (3, 1, 8, 2), (4, 49, 32, 8), (30, 16, 512, 32), (3, 77, 30, 6), (2, 100, 15, 5), (2, 31, 4096, 1), (1, 7, 2051, 1), (2, 9000, 32, 8),
+    (2, 12544, 64, 32), (1, 3001, 250, 10)], ids=str)
+def test_group_norm(shape, dtype):
+    groups, act = shape[3], B.BYZ_ACT_SILU
+    x, gamma, beta, dy = _norm_case(*shape, dtype, "silu", seed=sum(shape))
+    y, mean, rstd = B.byz_group_norm(x, groups, gamma, beta, act=act)
+    back = B.byz_group_norm_backward(dy, x, groups, mean, rstd, gamma, beta, act)
+    for offset, more, other in ((1, 0, 0), (0, 1, 3), (5, 11, 2), (3, 8, 16), (2, 6, 1)):
+        part, _ = _placed(x, offset, more)
+        dpart, _ = _placed(dy, other, more + 3)
+        out, wide = _placed(x, other, offset)
+        out.fill_(7.0)
+        beside = wide.isnan()
+        got = B.byz_group_norm(part, groups, gamma, beta, act=act, out=out)
+        assert all(_same_bits(a, b) for a, b in zip(got, (y, mean, rstd)))
+        assert torch.equal(wide.isnan(), beside)
+        out.fill_(7.0)
+        got = B.byz_group_norm_backward(dpart, part, groups, mean, rstd, gamma, beta, act, out=out)
+        assert all(_same_bits(a, b) for a, b in zip(got, back))
+        assert torch.equal(wide.isnan(), beside)
+        got = B.byz_group_norm_backward(dpart, part, groups, mean, rstd, gamma, beta, act, out=dpart)  # over dy
+        assert all(_same_bits(a, b) for a, b in zip(got, back))
+        got = B.byz_group_norm(part, groups, gamma, beta, act=act, out=part)  # in place
+        assert all(_same_bits(a, b) for a, b in zip(got, (y, mean, rstd)))
