@@ -125,9 +125,12 @@ int byz_gated_ffn(const void *x, int64_t x_ld, const void *w_gate, const void *w
  * Its gradients for dh (m x n, pitch dh_ld) from the saved gate and up (pitch gate_ld):
  *     dup = dh * act(gate),  dgate = dh * up * act'(gate)      (rounded to the type once)
  *     dx = dgate w_gate + dup w_up,  dw_gate = dgate^T x,  dw_up = dup^T x
- * dx has pitch dx_ld, dw_gate and dw_up pitch dw_ld; dx or both dw may be NULL.
+ * dx has pitch dx_ld, dw_gate and dw_up pitch dw_ld; dx or both dw may be NULL.  The workspace has room for copies of x and
+ * the weights, which a call whose k is a multiple of 8 and whose rows of x and weights all start at 16-byte boundaries does not
+ * need: it takes the aligned size.
  */
 size_t byz_gated_ffn_backward_workspace_bytes(int64_t m, int64_t k, int64_t n, int dtype);
+size_t byz_gated_ffn_backward_aligned_workspace_bytes(int64_t m, int64_t k, int64_t n, int dtype);
 int byz_gated_ffn_backward(const void *dh, int64_t dh_ld, const void *x, int64_t x_ld,
                            const void *w_gate, const void *w_up, int64_t w_ld, const float *gate,
                            const float *up, int64_t gate_ld, int64_t m, int64_t k, int64_t n, int dtype,

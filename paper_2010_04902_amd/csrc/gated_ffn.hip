@@ -717,20 +717,21 @@ bool sizes_ok(int64_t m, int64_t k, int64_t n) {
 // Whether the tile kernel reads a matrix as it lies: pieces of 16 bytes, none of them beyond the columns.
 bool pieces(const void *at, int64_t cols, int64_t ld) { return aligned(at, 16) && cols % 8 == 0 && ld % 8 == 0; }
 
-// Workspace, in elements: matrices that have to be copied, and for the backward pass dgate | dup and the sums of blocks
-// that share a tile of dx.
+// Workspace, in elements: for the backward pass dgate | dup and the sums of blocks that share a tile of dx; behind them
+// matrices that have to be copied, `aligned` without them.
 struct Layout {
     int64_t np, kp;
-    int64_t x, w, d, partial, all;
+    int64_t d, partial, x, w, aligned, all;
     Layout(int64_t m, int64_t k, int64_t n, bool backward) : np(padded(n)), kp((k + 7) / 8 * 8) {
-        x = 0;
-        w = x + m * kp;
-        d = w + 2 * n * kp;
-        partial = all = d + (backward ? m * 2 * np : 0);
+        d = 0;
+        partial = aligned = d + (backward ? m * 2 * np : 0);
         if (backward && m > 0 && k > 0) {
             const int splits = best_shape(m, k, np + n, kInput).splits;
-            if (splits > 1) all += 2 * splits * m * ((k + 3) / 4 * 4);
+            if (splits > 1) aligned += 2 * splits * m * ((k + 3) / 4 * 4);
         }
+        x = aligned;
+        w = x + m * kp;
+        all = w + 2 * n * kp;
     }
 };
 
@@ -751,16 +752,19 @@ int align(const void **at, int64_t *ld, int64_t rows, int64_t cols, T *to, int64
     return BYZ_OK;
 }
 
-// Copies x and the weights where the tile kernel cannot read them: rows of whole pieces, zeros behind k.
+// Whether the tile kernel reads x and the weights, where a call has use for them, as they lie.
+bool good_x(const Call &c, bool used) { return !used || c.m == 0 || c.k == 0 || pieces(c.x, c.k, c.x_ld); }
+bool good_w(const Call &c, bool used) {
+    return !used || c.n == 0 || c.k == 0 || (pieces(c.w_gate, c.k, c.w_ld) && pieces(c.w_up, c.k, c.w_ld));
+}
+
+// Copies those that it does not: rows of whole pieces, zeros behind k.
 template <typename T>
 int align_operands(Call &c, const Layout &lay, bool x, bool w, hipStream_t s) {
-    const bool good_x = !x || c.m == 0 || pieces(c.x, c.k, c.x_ld);
-    const bool good_w = !w || c.n == 0 || (pieces(c.w_gate, c.k, c.w_ld) && pieces(c.w_up, c.k, c.w_ld));
-    if (c.k == 0 || (good_x && good_w)) return BYZ_OK;
     T *ws = (T *)c.ws;
     int rc = BYZ_OK;
-    if (!good_x) rc = align<T>(&c.x, &c.x_ld, c.m, c.k, ws + lay.x, lay.kp, s);
-    if (rc == BYZ_OK && !good_w) {
+    if (!good_x(c, x)) rc = align<T>(&c.x, &c.x_ld, c.m, c.k, ws + lay.x, lay.kp, s);
+    if (rc == BYZ_OK && !good_w(c, w)) {
         int64_t ld = c.w_ld;
         rc = align<T>(&c.w_gate, &ld, c.n, c.k, ws + lay.w, lay.kp, s);
         if (rc == BYZ_OK) rc = align<T>(&c.w_up, &c.w_ld, c.n, c.k, ws + lay.w + c.n * lay.kp, lay.kp, s);
@@ -769,8 +773,7 @@ int align_operands(Call &c, const Layout &lay, bool x, bool w, hipStream_t s) {
 }
 
 size_t forward_bytes(const Call &c) {
-    const bool good = pieces(c.x, c.k, c.x_ld) && pieces(c.w_gate, c.k, c.w_ld) && pieces(c.w_up, c.k, c.w_ld);
-    return c.m <= kSkinny || good ? 0 : (size_t)Layout(c.m, c.k, c.n, false).all * 2;
+    return c.m <= kSkinny || (good_x(c, true) && good_w(c, true)) ? 0 : (size_t)Layout(c.m, c.k, c.n, false).all * 2;
 }
 
 template <typename T>
@@ -867,6 +870,11 @@ extern "C" size_t byz_gated_ffn_backward_workspace_bytes(int64_t m, int64_t k, i
     return (size_t)Layout(m, k, n, true).all * 2;
 }
 
+extern "C" size_t byz_gated_ffn_backward_aligned_workspace_bytes(int64_t m, int64_t k, int64_t n, int dtype) {
+    if (!sizes_ok(m, k, n) || (dtype != BYZ_BF16 && dtype != BYZ_F16)) return 0;
+    return (size_t)Layout(m, k, n, true).aligned * 2;
+}
+
 extern "C" int byz_gated_ffn_backward(const void *dh, int64_t dh_ld, const void *x, int64_t x_ld, const void *w_gate,
                                       const void *w_up, int64_t w_ld, const float *gate, const float *up,
                                       int64_t gate_ld, int64_t m, int64_t k, int64_t n, int dtype, int act, void *dx,
@@ -878,9 +886,10 @@ extern "C" int byz_gated_ffn_backward(const void *dh, int64_t dh_ld, const void 
         (dx && (!matrix_ok(w_gate, n, k, w_ld) || !matrix_ok(w_up, n, k, w_ld) || !matrix_ok(dx, m, k, dx_ld))) ||
         (dw_gate && (!matrix_ok(x, m, k, x_ld) || !matrix_ok(dw_gate, n, k, dw_ld) || !matrix_ok(dw_up, n, k, dw_ld))))
         return BYZ_EINVAL;
-    const size_t need = (size_t)Layout(m, k, n, true).all * 2;
-    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 16)))) return BYZ_ENOMEM;
     const Call c{x, w_gate, w_up, x_ld, w_ld, m, k, n, act, workspace};
+    const Layout lay(m, k, n, true);
+    const size_t need = (size_t)(good_x(c, dw_gate) && good_w(c, dx) ? lay.aligned : lay.all) * 2;
+    if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 16)))) return BYZ_ENOMEM;
     const Gradients g{dh, gate, up, dh_ld, gate_ld, dx, dw_gate, dw_up, dx_ld, dw_ld};
     return dtype == BYZ_BF16 ? backward<bf16>(c, g, (hipStream_t)stream) : backward<f16>(c, g, (hipStream_t)stream);
 }

@@ -247,16 +247,18 @@ PyObject *distill_loss_step(PyObject *, PyObject *const *o, Py_ssize_t count) {
     });
 }
 
-// A block's tokens and weights; 16-byte rows, so that a forward call needs no workspace.
+// A block's tokens and weights; aligned: 16-byte rows, so that a forward call needs no workspace and the backward none for copies.
 struct Block {
     const at::Tensor &x, &w_gate, &w_up;
     int dtype;
-    Block(Call &call, PyObject *const *o, bool aligned) : x(call.tensor(o[0])), w_gate(call.tensor(o[1])), w_up(call.tensor(o[2])), dtype(call.dtype(x)) {
+    Block(Call &call, PyObject *const *o, bool only_aligned) : x(call.tensor(o[0])), w_gate(call.tensor(o[1])), w_up(call.tensor(o[2])), dtype(call.dtype(x)) {
         call.need(call.good && dtype != BYZ_F32 && x.dim() == 2 && w_gate.dim() == 2 && w_up.sizes() == w_gate.sizes() &&
                   x.size(1) == w_gate.size(1) && w_gate.scalar_type() == x.scalar_type() && w_up.scalar_type() == x.scalar_type() &&
                   x.is_contiguous() && w_gate.is_contiguous() && w_up.is_contiguous());
-        if (call.good && aligned && x.size(0) > 16)
-            call.need(x.size(1) % 8 == 0 && (((uintptr_t)x.data_ptr() | (uintptr_t)w_gate.data_ptr() | (uintptr_t)w_up.data_ptr()) & 15) == 0);
+        if (call.good && only_aligned && x.size(0) > 16) call.need(aligned());
+    }
+    bool aligned() const {
+        return x.size(1) % 8 == 0 && (((uintptr_t)x.data_ptr() | (uintptr_t)w_gate.data_ptr() | (uintptr_t)w_up.data_ptr()) & 15) == 0;
     }
 };
 
@@ -298,7 +300,8 @@ PyObject *gated_ffn_backward(PyObject *, PyObject *const *o, Py_ssize_t count) {
         if (!call.good) return nullptr;
         return answer([&]() -> Result {
             at::Tensor dx = at::empty({m, k}, b.x.options()), dw_gate = at::empty({n, k}, b.x.options()), dw_up = at::empty({n, k}, b.x.options());
-            const size_t need = byz_gated_ffn_backward_workspace_bytes(m, k, n, b.dtype);
+            const size_t need = b.aligned() ? byz_gated_ffn_backward_aligned_workspace_bytes(m, k, n, b.dtype)
+                                            : byz_gated_ffn_backward_workspace_bytes(m, k, n, b.dtype);
             const at::Tensor ws = bytes(need, b.x);
             const int rc = byz_gated_ffn_backward(dh.data_ptr(), n, b.x.data_ptr(), k, b.w_gate.data_ptr(), b.w_up.data_ptr(), k, gate, up, n, m,
                                                   k, n, b.dtype, act, dx.data_ptr(), k, dw_gate.data_ptr(), dw_up.data_ptr(), k, address(ws),

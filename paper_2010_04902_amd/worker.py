@@ -53,6 +53,7 @@ def _load():
         "byz_gated_ffn_workspace_bytes": (sz, [i64, i64, i64, c_int]),
         "byz_gated_ffn": (c_int, [vp, i64, vp, vp, i64, i64, i64, i64, c_int, c_int, vp, i64, vp, vp, i64, vp, sz, vp]),
         "byz_gated_ffn_backward_workspace_bytes": (sz, [i64, i64, i64, c_int]),
+        "byz_gated_ffn_backward_aligned_workspace_bytes": (sz, [i64, i64, i64, c_int]),
         "byz_gated_ffn_backward": (c_int, [vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, i64, c_int, c_int,
                                            vp, i64, vp, vp, i64, vp, sz, vp]),
     }
@@ -360,6 +361,11 @@ def _ffn_arguments(x, w_gate, w_up):
     return m, k, n, x_ld, w_ld, device
 
 
+def _copied(k, x_ld, w_ld, xa, ga, ua):
+    """Whether rows of x or the weights are such that the kernel cannot read them as they lie."""
+    return (k | x_ld | w_ld) % 8 | (xa | ga | ua) % 16
+
+
 def byz_gated_ffn(x, w_gate, w_up, act=BYZ_ACT_SILU, save=False, out=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T) -> h, or (h, gate, up) with save=True: both products, float32, for the
     backward pass.
@@ -390,7 +396,7 @@ def byz_gated_ffn(x, w_gate, w_up, act=BYZ_ACT_SILU, save=False, out=None, strea
             gate, up = gate[:, :n], up[:, :n]
     xa, ga, ua = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
     nbytes, ws, at = 0, None, None
-    if m > 16 and (k | x_ld | w_ld) % 8 | (xa | ga | ua) % 16:  # rows that the kernel cannot read as they lie
+    if m > 16 and _copied(k, x_ld, w_ld, xa, ga, ua):
         nbytes = _workspace_bytes("byz_gated_ffn_workspace_bytes", m, k, n, dtype)
         ws, at = _workspace(nbytes, empty, device)
     _b._check(_lib.byz_gated_ffn(xa, x_ld, ga, ua, w_ld, m, k, n, dtype, act, out.data_ptr(), h_ld,
@@ -421,10 +427,12 @@ def byz_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, act=BYZ_ACT_SILU, stre
     dx = empty((m, k), dtype=kind, device=device)
     dw_gate = empty((n, k), dtype=kind, device=device)
     dw_up = empty((n, k), dtype=kind, device=device)
-    nbytes = _workspace_bytes("byz_gated_ffn_backward_workspace_bytes", m, k, n, dtype)
+    xa, ga, ua = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    nbytes = _workspace_bytes("byz_gated_ffn_backward_workspace_bytes" if _copied(k, x_ld, w_ld, xa, ga, ua) else
+                              "byz_gated_ffn_backward_aligned_workspace_bytes", m, k, n, dtype)
     ws, at = _workspace(nbytes, empty, device)
     _b._check(_lib.byz_gated_ffn_backward(
-        dh.data_ptr(), dh_ld, x.data_ptr(), x_ld, w_gate.data_ptr(), w_up.data_ptr(), w_ld, gate.data_ptr(),
+        dh.data_ptr(), dh_ld, xa, x_ld, ga, ua, w_ld, gate.data_ptr(),
         up.data_ptr(), gate_ld, m, k, n, dtype, act, dx.data_ptr(), k, dw_gate.data_ptr(), dw_up.data_ptr(), k,
         at, nbytes, _stream(stream, gpu)), "byz_gated_ffn_backward")
     return dx, dw_gate, dw_up
