@@ -8,6 +8,9 @@ alone, bit for bit, which is what the server's vote over the copies of a file's 
 """
 import ctypes
 import functools
+import importlib
+import subprocess
+import warnings
 
 from . import binding as _b
 
@@ -23,19 +26,37 @@ _torch = None
 _dtypes = {}
 
 
+class _NoCalls:
+    """Stands in for the native module where there is none: every call is left to the Python below."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+def _load_calls():
+    """csrc/worker_calls.cpp's module; built once where it is missing or made for another torch, and done without, with a
+    warning, where that fails."""
+    for build in (False, True):
+        try:
+            if build:
+                from . import build as _build
+                _build.build_calls()
+                importlib.invalidate_caches()
+            return importlib.import_module("._worker_calls", __package__)
+        except (ImportError, OSError, subprocess.CalledProcessError) as e:
+            reason = e
+    warnings.warn("the worker operators' native module is not there (%s): small calls take about twice the host's time" % reason,
+                  RuntimeWarning, stacklevel=3)
+    return _NoCalls()
+
+
 def _load():
     global _lib, _torch, _calls
     if _lib is not None:
         return _lib
     L = _b._load()
     torch = _torch = _b._torch()
-    try:
-        from . import _worker_calls
-    except ModuleNotFoundError:  # not built yet: build once, loudly
-        from . import build as _build
-        _build.build_calls()
-        from . import _worker_calls
-    _calls = _worker_calls
+    _calls = _load_calls()
     _dtypes.update({torch.float32: BYZ_F32, torch.bfloat16: BYZ_BF16, torch.float16: BYZ_F16})
     vp, c_int, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     sig = {
