@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -18,10 +19,12 @@
 namespace {
 
 PyObject *get_device = nullptr, *get_stream = nullptr;  // torch's: the current GPU, the handle of its current stream
+constexpr char no_graph[] =  // as in worker.py
+    "outputs are not part of autograd's graph: gradients come from the operator's own backward call (no warning under torch.no_grad)";
 
 // The tensors of a call: each is looked at once, and the first that is not as it has to be spoils the call.
 struct Call {
-    bool good = true;
+    bool good = true, graph = false;  // graph: of a tensor that requires a gradient
     int device = -1;
     void need(bool b) { good = good && b; }
     // a tensor of torch's own class on the call's GPU; an empty one where the call is spoilt
@@ -30,6 +33,7 @@ struct Call {
         if (!good || !THPVariable_CheckExact(o)) return good = false, nothing;
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_cuda() || t.layout() != c10::kStrided || t.numel() == 0) return good = false, nothing;
+        graph = graph || t.requires_grad();
         if (device < 0)
             device = t.get_device();
         else
@@ -65,6 +69,11 @@ struct Call {
         const int code = type == at::kFloat ? BYZ_F32 : type == at::kBFloat16 ? BYZ_BF16 : type == at::kHalf ? BYZ_F16 : -1;
         need(code >= 0);
         return code;
+    }
+    // A forward call whose outputs somebody may take for part of autograd's graph is worth a word; where warnings are
+    // errors the Python path raises it.
+    void outside_the_graph() {
+        if (good && graph && at::GradMode::is_enabled()) good = PyErr_WarnEx(PyExc_RuntimeWarning, no_graph, 2) == 0;
     }
     // the handle of the current stream; spoils the call if its tensors are not on the current GPU
     void *stream() {
@@ -155,6 +164,7 @@ PyObject *group_norm(PyObject *, PyObject *const *o, Py_ssize_t count) {
         const float eps = call.real(o[4]);
         const float *gamma = call.floats(o[2], {f.c}, true), *beta = call.floats(o[3], {f.c}, true);
         void *const stream = call.stream();
+        call.outside_the_graph();
         if (!call.good || groups < 1) return nullptr;
         return answer([&]() -> Result {
             at::Tensor y = at::empty_like(x), mean = fp32({f.n, groups}, x), rstd = fp32({f.n, groups}, x);
@@ -212,6 +222,7 @@ PyObject *distill_loss(PyObject *, PyObject *const *o, Py_ssize_t count) {
         const Distill d(call, o);
         const float temperature = call.real(o[3]);
         void *const stream = call.stream();
+        call.outside_the_graph();
         if (!call.good) return nullptr;
         const int64_t rows = d.logits.size(0), vocab = d.logits.size(1), k = d.teacher.size(1);
         return answer([&]() -> Result {
@@ -271,6 +282,7 @@ PyObject *gated_ffn(PyObject *, PyObject *const *o, Py_ssize_t count) {
         call.need(PyBool_Check(o[4]));
         const bool save = o[4] == Py_True;
         void *const stream = call.stream();
+        call.outside_the_graph();
         if (!call.good) return nullptr;
         const int64_t m = b.x.size(0), k = b.x.size(1), n = b.w_gate.size(0);
         if (save && n % 4) return nullptr;  // rows of the saved products are padded

@@ -2,7 +2,8 @@
 the gated feed-forward block, distillation from a teacher's top logits, each with its gradients.
 
 Same manner as the server's entry points: torch CUDA tensors in, outputs allocated with torch where
-the caller gives none, work enqueued on `stream` (the current one by default), nothing synchronised.
+the caller gives none, work enqueued on `stream` (the current one by default), nothing synchronised.  Autograd knows nothing of
+them: outputs are not part of its graph, gradients are explicit calls (a forward call warns where a tensor requires one).
 A layout the kernels do not read is refused (the feed-forward's rows may be copied to a workspace).  Results depend on the arguments
 alone, bit for bit, which is what the server's vote over the copies of a file's gradient needs.
 """
@@ -19,6 +20,9 @@ BYZ_ACTS = {"none": BYZ_ACT_NONE, "relu": BYZ_ACT_RELU, "silu": BYZ_ACT_SILU, "g
             "sigmoid": BYZ_ACT_SIGMOID}
 BYZ_MAX_TEACHER = 1024
 BYZ_F32, BYZ_BF16, BYZ_F16 = range(3)
+
+_NO_GRAPH = ("outputs are not part of autograd's graph: gradients come from the operator's own backward call "
+             "(no warning under torch.no_grad)")
 
 _lib = None
 _calls = None
@@ -164,6 +168,11 @@ def _workspace(nbytes, empty, device):
     return t, t.data_ptr()
 
 
+def _outside_the_graph(*tensors):
+    if _torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        warnings.warn(_NO_GRAPH, RuntimeWarning, stacklevel=3)
+
+
 def _done(r, where):
     """A common call's outputs, or its error."""
     if r.__class__ is int:
@@ -224,6 +233,7 @@ def byz_group_norm(x, groups, gamma=None, beta=None, eps=1e-5, act=BYZ_ACT_NONE,
         done = _calls.group_norm(x, groups, gamma, beta, eps, act)
         if done is not None:
             return _done(done, "byz_group_norm")
+    _outside_the_graph(x, gamma, beta)
     n, p, c, xs, xp = _features(x, "x")
     index = _device(x, "x")
     device, dtype, groups = x.device, _dtype(x, "x"), int(groups)
@@ -315,6 +325,7 @@ def byz_distill_loss(logits, teacher, index, temperature=1.0, stream=None):
         done = _calls.distill_loss(logits, teacher, index, temperature)
         if done is not None:
             return _done(done, "byz_distill_loss")
+    _outside_the_graph(logits, teacher)
     rows, vocab, ld, k, tld, gpu = _distill_arguments(logits, teacher, index)
     device, dtype = logits.device, _dtype(logits, "logits")
     empty = _torch.empty if stream is None else _b._empty_on(stream)
@@ -398,6 +409,7 @@ def byz_gated_ffn(x, w_gate, w_up, act=BYZ_ACT_SILU, save=False, out=None, strea
         done = _calls.gated_ffn(x, w_gate, w_up, act, save)
         if done is not None:
             return _done(done, "byz_gated_ffn")
+    _outside_the_graph(x, w_gate, w_up)
     m, k, n, x_ld, w_ld, gpu = _ffn_arguments(x, w_gate, w_up)
     device, dtype, kind = x.device, _dtype(x, "x"), x.dtype
     empty = _torch.empty if stream is None else _b._empty_on(stream)
