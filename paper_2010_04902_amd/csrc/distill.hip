@@ -289,8 +289,10 @@ __device__ __forceinline__ void write_places(const Args &a, const Teacher &t, co
     }
 }
 
+// The step of 256 threads in 96 registers, five blocks a compute unit: 8192 x 20000 fp16 takes 176 us so, 192 with three more.
+// bf16 does without being told, and is slower told (20011 words 188 us for 178).
 template <typename T, int NT, Mode MODE>
-__global__ __launch_bounds__(NT) void distill_kernel(Args a) {
+__global__ __launch_bounds__(NT, MODE == kStep && NT == 256 && (std::is_same_v<T, f16>) ? 5 : NT / 256) void distill_kernel(Args a) {
     extern __shared__ char lds_raw[];
     __shared__ double red[32];
     constexpr int V = 16 / sizeof(T);
@@ -300,9 +302,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
     Teacher t(lds_raw, a.k);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<T> r(a.logits, row, a.ld, a.vocab);
+        // sent ahead of the teacher's chain; in the step, which is at its registers' end, later
+        const float given = MODE == kGradient ? a.lse[row] : 0.0f, early = MODE == kGradient ? a.dloss[row] : 0.0f;
         read_teacher<T, NT>(a, row, r.at, t, tid, red);
         double m, log_sum;  // the student's log-sum-exp is m / tau + log_sum
-        const float given = MODE == kGradient ? a.lse[row] : 0.0f;
         if (MODE != kGradient || !lse_is_good(given)) {
             RunningSum s;
             if (tid < r.tail) {
@@ -310,7 +313,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
                 s.add(x, c);
             }
             auto add_up = [&](auto odd) {
-                constexpr int kUnroll = MODE == kGradient ? 1 : odd.value ? 3 : 4;
+                constexpr int kUnroll = odd.value ? 3 : 4;
                 int64_t i = tid;
                 for (; i + (kUnroll - 1) * NT < r.vectors; i += kUnroll * NT) {
                     Words<T, V> v[kUnroll];
@@ -332,12 +335,24 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
                     s.add(x, c);
                 }
             };
-            if (r.odd())
+            if constexpr (MODE == kGradient) {
+                // the exception, in few registers, or all rows would have fewer waves
+#pragma unroll 1
+                for (int64_t i = tid; i < r.vectors * (V / 4); i += NT) {
+                    const Words<T, 4> v = get_words<T, 4>(r.at + i * 4);
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) x[e] = v[e];
+                    s.add(x, c);
+                }
+            } else if (r.odd()) {
                 add_up(std::true_type{});
-            else
+            } else {
                 add_up(std::false_type{});
+            }
             s = row_join<NT>(s, c, red);
-            m = s.m, log_sum = log((double)s.s);
+            // the gradient's needs no more than fp32; a logarithm in fp64 would cost all rows two waves
+            m = s.m, log_sum = MODE == kGradient ? (double)(__builtin_amdgcn_logf(s.s) * 0.69314718f) : log((double)s.s);
         } else {
             m = (float)(given * tau), log_sum = given - m / tau;
         }
@@ -352,7 +367,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(Args a) {
             for (int j = tid; j < a.k; j += NT) t.p[j] = t.index[j] < 0 ? 0.0f : (float)(t.weight[j] / t.total);
         }
         if constexpr (MODE != kLoss) {
-            const Softmax<T> q(m, log_sum, tau, t.total != t.total ? NAN : a.temperature * a.dloss[row]);
+            const Softmax<T> q(m, log_sum, tau, t.total != t.total ? NAN : a.temperature * (MODE == kGradient ? early : a.dloss[row]));
             T *out = (T *)a.dlogits + row * a.dlogits_ld;
             __syncthreads();  // the logits at the teacher's places are read: they may be written now
             if (tid < r.tail) {
