@@ -2,9 +2,11 @@
  * byzshield_worker.h -- operators of a worker's training step (C-ABI of libbyzshield, one MI355X).
  *
  * The server of byzshield.h compares the r copies of a file's gradient bit by bit, so honest
- * workers have to compute the same bits.  The operators here do: a call's result depends on its
- * arguments alone (no atomics, every sum in a fixed order, a launch shape chosen by sizes, types
- * and alignment), none mixes the samples of a file, and all of them enqueue work and nothing else.
+ * workers have to compute the same bits.  The operators here do: calls of the same sizes and type on
+ * the same values give the same bits, wherever their tensors lie and whatever their pitches are (no
+ * atomics, every sum in a fixed order, launch shapes chosen by sizes and type alone).  A file within a
+ * call of more rows or samples is a call of other sizes: copies have to be computed by calls alike.
+ * None mixes the samples of a file, and all of them enqueue work and nothing else.
  *
  * Conventions (beyond those of byzshield.h)
  *   - Device pointers of the current device; `stream` is a hipStream_t passed as void*.  No
@@ -12,7 +14,7 @@
  *   - Values of type `dtype`; statistics, losses, parameters of the norm and their gradients are
  *     fp32.  Sums are held in fp32 or more, each output is rounded once.
  *   - Pitches and strides count elements.  Any alignment to the element's size works; 16-byte
- *     aligned bases with pitches of whole 16 bytes are faster.
+ *     aligned bases with pitches of whole 16 bytes are faster (the feed-forward of more than 16 tokens copies others first).
  *   - Sizes of zero are valid and give what is left (no output, or zero gradients).
  *   - Outputs do not overlap inputs unless a function says so.
  */

@@ -4,18 +4,19 @@
 // difference of larger terms, and k values cost nothing next to the vocabulary), and the student's
 // log-sum-exp over the vocabulary, joined over the row's threads in a fixed order.  The gradient is dense, dloss T q_v,
 // with the few places of the teacher's entries written again after it (each thread that owns an entry adds up all
-// p at its place, so entries at one place write one value).
+// p at its place, so entries at one place write one value).  A thread's values are counted from the row's start, wherever that
+// lies: the bits of a row do not depend on its address.
 //
 // Bound by memory: logits in, gradients out.  Loss and gradient in one call hold a long row in registers ("resident"): it
 // is read once, and as soon as a thread has stored a piece of its gradient it loads that piece of its next row, so reads,
 // the two exponentials of a value and writes overlap although a row fills a compute unit's registers.  Nothing else is
 // in that kernel: the teacher's softmax, fp64 functions and the few places are kernels before and behind it (places
-// written in it, behind a barrier, cost 17 % of its time).  Short rows are a wave's.  Rows between, too long ones and the other calls stream:
-// with a running maximum m and a sum of exp((s - m) / T).
+// written in it, behind a barrier, cost 17 % of its time).  Short rows are a wave's.  Rows between, too long ones and the other
+// calls stream: with a running maximum m and a sum of exp((s - m) / T).
 //
-// 8192 x 131072 bf16, loss and gradient: resident 822 us (4.3 GB at 5.2 TB/s, a copy reaches 6.5; vector instructions issue 0.47 of the
-// time), teacher and places 45.
-// 30 x 10 and 750 x 1000: 5.8 us a call, one launch, bound by the host; through LDS and barriers 7.2 and 8.1.
+// 8192 x 131072 bf16, loss and gradient: resident 818 us (4.3 GB at 5.3 TB/s, a copy reaches 6.5; vector instructions issue
+// 0.51 of the time), teacher 29, places 18.  8192 x 20000, twice read: loss 83, loss and gradient 174, gradient alone 140.
+// 30 x 10 and 750 x 1000: 6.0 us a call, one launch, bound by the host; through LDS and barriers 7.2 and 8.1.
 #include <algorithm>
 #include <type_traits>
 
@@ -46,6 +47,9 @@ struct Args {
     int64_t dlogits_ld;
 };
 
+// A sum of positive terms in fp32: a thread adds some hundred of them at most, and the threads' sums are joined pairwise, so it
+// is good to some 2^-23 of itself, of which the loss has the logarithm.  In fp64 it would be ten times nearer, for a conversion
+// and an fp64 addition a value.
 struct RunningSum {
     float m = -INFINITY, s = 0.0f;  // maximum of the raw logits, sum of exp2((x - m) c)
     template <int N>

@@ -14,9 +14,10 @@
 // Few tokens: the weights' bytes bound the call; a wave multiplies 16 rows of each weight with up to 16 tokens,
 // straight from memory into the matrix instruction's registers, the waves of a block split k and join in LDS.
 //
-// us, traced (TFLOP/s; a large library product reaches 1161 in bf16): 8192 x 4096 x 10944 bf16 forward with saved sums 1391 (1056),
-// dgate | dup 258, dx 1233 (1191), both dw 1388 (1058).  1920 x 512 x 1376: 17.7, 8.2, 18.9, 15.0, short products on less than
-// two blocks a compute unit.  333 x 1000 x 2731 fp16 forward 18.  One token of 2048 -> 5504: 9.3 (45 MB, 4.9 TB/s).
+// us, traced (TFLOP/s; a large library product reaches 1161 in bf16): 8192 x 4096 x 10944 bf16 forward with saved sums 1349 (1089),
+// dgate | dup 261, dx 1212 (1212), both dw 1349 (1089).  1920 x 512 x 1376: 18.2, 8.7, 19.3, 14.6, short products on less than
+// two blocks a compute unit.  333 x 1000 x 2731 fp16 forward 18: 129 blocks of 16 steps.  One token of 2048 -> 5504: 9.3 (45 MB,
+// 4.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -96,7 +97,8 @@ __device__ __forceinline__ int column_turn(int row) {  // by columns: what the 6
 // 1024 bytes from memory to LDS without registers: lane i's 16 bytes at `from` go to lds + 16 i.  Written out
 // because the compiler, where it sees such a load, lets every turned read from LDS wait for all of them.  It has no
 // output register, so nothing of the compiler's can meet it in flight; vmcnt counts it, which makes the compiler's own
-// waits only longer.  Nothing else here uses m0.
+// waits only longer.  The compiler reserves m0: it keeps no value in it from one statement to another (and takes no word that
+// one changes it); nothing else in these kernels uses it, as their listing shows.
 __device__ __forceinline__ void load_to_lds(const void *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :
@@ -531,7 +533,9 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(Product p) {
     }
 }
 
-// dgate | dup from dh, gate and up: `d` is [m][2 np] (dgate, then dup), zeros in the padding.
+// dgate | dup from dh, gate and up: `d` is [m][2 np] (dgate, then dup), zeros in the padding.  They are rounded to the type,
+// which is what the matrix instructions of both products behind take: in bf16 gradients are 2.3e-3 off their 64-bit values so, for
+// 1.7e-3 of their own rounding alone; two 16-bit parts of each would double the products.
 struct Slopes {
     const void *dh;
     const float *gate, *up;

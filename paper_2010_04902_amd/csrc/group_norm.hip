@@ -18,14 +18,16 @@
 // of a sample fits the registers of one block ("whole") everything is read once.  Larger samples are cut into
 // chunks: a first kernel writes their statistics, a second joins them in chunk order, a third reads the chunks again and
 // stores past the caches, which then still hold inputs for the next pass (backward sums behind the forward pass 46.6 / 38.4 us,
-// gradients 54.9 / 48.8, without / with that).  Registers for 200 KB slices, 16 vectors a thread, spill and were slower (64 us
-// for 58 in three kernels on 64 x 56 x 56 x 256 bf16).
+// gradients 54.9 / 48.8, without / with that).  A slice is 64 bytes of a row wide at least, which is 200 KB on 64 x 56 x 56 x 256
+// bf16: registers for that, 16 vectors a thread, spill and were slower (64 us for 58 in three kernels); narrower slices that would
+// fit, 100 KB, have not been tried.
 // No atomics.
 //
-// us, traced: 64 x 112 x 112 x 64 fp16 forward: statistics 21.5 (103 MB, 4.8 TB/s), join 4.8, pass 36.2 (206 MB, 5.7 TB/s).
-// 64 x 56 x 56 x 256 bf16: forward 20.5 + 5.0 + 33.3; backward sums 37.5 (206 MB, 5.5 TB/s), totals 5.0, pass 48.6 (309 MB, 6.3 TB/s),
-// parameters 4.8.  30 x 32 x 32 x 64 bf16: 10.9 forward, 11.4 backward (12.1 and 16.0 with joins through LDS), 3.5
-// parameters: a block's chain of loads, joins and stores.
+// us, traced: 64 x 112 x 112 x 64 fp16 forward: statistics 21.2 (103 MB, 4.9 TB/s), join 4.7, pass 36.1 (206 MB, 5.7 TB/s).
+// 64 x 56 x 56 x 256 bf16: forward 20.4 + 4.8 + 33.3; backward sums 37.2 (206 MB, 5.5 TB/s), totals 5.0, pass 48.4 (309 MB, 6.4 TB/s),
+// parameters 4.8.  30 x 32 x 32 x 64 bf16: 10.6 forward, 12.0 backward (12.1 and 16.0 with joins through LDS), 3.3
+// parameters: a block's chain of loads, joins and stores.  Slices of 64 x 28 x 28 x 512 bf16 fit: 33.7 forward (floor 16), 63
+// backward (24), as loads, joins and stores of a block follow one another with little else on the compute unit.
 #include <algorithm>
 #include <type_traits>
 

@@ -4,8 +4,9 @@ the gated feed-forward block, distillation from a teacher's top logits, each wit
 Same manner as the server's entry points: torch CUDA tensors in, outputs allocated with torch where
 the caller gives none, work enqueued on `stream` (the current one by default), nothing synchronised.  Autograd knows nothing of
 them: outputs are not part of its graph, gradients are explicit calls (a forward call warns where a tensor requires one).
-A layout the kernels do not read is refused (the feed-forward's rows may be copied to a workspace).  Results depend on the arguments
-alone, bit for bit, which is what the server's vote over the copies of a file's gradient needs.
+A layout the kernels do not read is refused (the feed-forward's rows may be copied to a workspace).  Calls of the same sizes and type on
+the same values give the same bits, wherever their tensors lie, which is what the server's vote over the copies of a file's gradient
+needs: copies of a file have to be computed by calls alike, not once alone and once within a larger batch.
 """
 import ctypes
 import functools
