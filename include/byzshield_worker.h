@@ -139,6 +139,126 @@ int byz_gated_ffn_backward(const void *dh, int64_t dh_ld, const void *x, int64_t
                            int act, void *dx, int64_t dx_ld, void *dw_gate, void *dw_up, int64_t dw_ld,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------ dropout */
+
+/*
+ * y = x / (1 - p) where a value stays, 0 where it is dropped (whatever it is), of `rows` rows of `cols` values (pitches x_ld, y_ld).
+ * Its gradient is the same call on dy.  No mask is stored: value (i, j) stays if 16 random bits of
+ * Philox 4x32-10 (key: seed; counter: j / 8, first_row + i, and the 64-bit sum of offset and *offset_at) are p 2^16 or more, p 2^16
+ * rounded to a whole number, whose p is also the scale's.  So the copies of a file drop the same values if they give
+ * the same seed, offset and first_row; calls of one step need offsets of their own.
+ * offset_at (device, 8-byte aligned) may be NULL: a captured call takes another offset at each replay from it.
+ * 0 <= p <= 1, first_row + rows <= 2^32, cols < 2^31.  y may be x itself with the same pitch.
+ */
+int byz_dropout(const void *x, int64_t rows, int64_t cols, int64_t x_ld, int dtype, float p, uint64_t seed,
+                uint64_t offset, const int64_t *offset_at, int64_t first_row, void *y, int64_t y_ld, void *stream);
+
+/* --------------------------------------- a block's output joins the residual, and norms */
+
+typedef enum byz_norm { BYZ_NORM_NONE = 0, BYZ_NORM_RMS = 1, BYZ_NORM_LAYER = 2 } byz_norm;
+
+typedef struct byz_residual_form {
+    int32_t post, pre; /* byz_norm */
+    float eps, scale, p;
+    uint64_t seed, offset; /* of the dropout, as in byz_dropout */
+    const int64_t *offset_at;
+    int64_t first_row;
+} byz_residual_form;
+
+/*
+ * For each of `rows` rows of `cols` values of the residual x and a block's output h:
+ *     u = norm_post(h) * post_weight + post_bias
+ *     out = x + scale * gate * dropout(u)
+ *     y = norm_pre(out) * pre_weight + pre_bias
+ * with norm(v) = (v - mean) / sqrt(var + eps) for BYZ_NORM_LAYER (var biased), v / sqrt(mean of v^2 + eps) for BYZ_NORM_RMS, v
+ * for BYZ_NORM_NONE; y is of the unrounded sum.  gate_rows rows one after the other share a row of gate, which has
+ * ceil(rows / gate_rows) rows, and one at least, of cols values (gate_rows = rows: one for all).  Weights and biases (cols each) and gate may be NULL
+ * (ones, zeros, ones).  Without a pre norm there is no y, and no pre_weight or pre_bias.  h NULL: no block, y = norm_pre(x), no out.
+ * stats: rows * 4, mean and 1 / sqrt(...) of both norms (0 and 1 where there is none); it may be NULL if no gradients are
+ * wanted.  out may be x or h with the same pitch, but the backward call needs both.  cols < 2^31.
+ */
+int byz_residual_norm(const void *x, int64_t x_ld, const void *h, int64_t h_ld, int64_t rows, int64_t cols, int dtype,
+                      const byz_residual_form *form, const float *post_weight, const float *post_bias, const float *gate,
+                      int64_t gate_rows, const float *pre_weight, const float *pre_bias, void *out, int64_t out_ld, void *y,
+                      int64_t y_ld, float *stats, void *stream);
+
+/*
+ * Its gradients for dout and dy (either may be NULL: zeros), from the call's x, h and stats: dx and dh (no dh without h), and those of
+ * the vectors, fp32 sums over the rows, each of which may be NULL; d_gate has gate's shape.
+ */
+size_t byz_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype, int64_t gate_rows);
+int byz_residual_norm_backward(const void *dout, int64_t dout_ld, const void *dy, int64_t dy_ld, const void *x, int64_t x_ld,
+                               const void *h, int64_t h_ld, const float *stats, int64_t rows, int64_t cols, int dtype,
+                               const byz_residual_form *form, const float *post_weight, const float *post_bias,
+                               const float *gate, int64_t gate_rows, const float *pre_weight, void *dx, int64_t dx_ld,
+                               void *dh, int64_t dh_ld, float *d_post_weight, float *d_post_bias, float *d_gate,
+                               float *d_pre_weight, float *d_pre_bias, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/* ------------------------------------------------ losses of tokens' log-probabilities */
+
+/*
+ * Row i has `vocab` logits z (pitch ld) and a token label[i]; a negative label is no token: log-probability, loss and
+ * gradient 0, whatever the logits are.
+ *     logp[i] = z_label / temperature - log sum_v exp(z_v / temperature),  q = softmax of z / temperature
+ * A logit of -inf is a banned one: q = 0 there, logp = -inf if it is the label's.  A label of vocab or more makes the row NaN, and
+ * its gradient.  stats: rows * 2, the row's largest logit m and log sum_v exp((z_v - m) / temperature), for the backward calls
+ * (0 and 0 where all are banned or there is no token); where it is an output it may be NULL.  temperature > 0; vocab < 2^31.
+ * All calls of this section take a workspace of byz_token_loss_workspace_bytes.  dlogits (pitch dlogits_ld, type dtype)
+ * may be the logits themselves with the same pitch.
+ */
+size_t byz_token_loss_workspace_bytes(int64_t rows, int64_t vocab, int dtype);
+
+/* Log-probabilities, and their gradient dlogits[i, v] = dlogp[i] / temperature * ((v = label) - q_v). */
+int byz_token_logp(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int32_t *label,
+                   float temperature, float *logp, float *stats, void *workspace, size_t workspace_bytes, void *stream);
+int byz_token_logp_backward(const float *dlogp, const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                            const int32_t *label, const float *stats, float temperature, void *dlogits, int64_t dlogits_ld,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The clipped policy loss with a KL term, of each token: with a = advantage, r = exp(logp - old), g = ref - logp,
+ *     loss = -min(r a, clamp(r, 1 - clip_low, 1 + clip_high) a) + kl (exp(g) - 1 - g)
+ * old, advantage and ref hold a value a row (ref may be NULL if kl is 0).  The gradient of the first term is that of -r a where r is
+ * within the bound on its side (at the bound too), else 0.  0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl.
+ * The step makes loss and gradient in one call for a dloss that is known beforehand (the weight of a token in a mean): the logits
+ * are read once where a row fits a compute unit.
+ */
+int byz_policy_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int32_t *label,
+                    const float *old, const float *advantage, const float *ref, float clip_low, float clip_high, float kl,
+                    float temperature, float *loss, float *logp, float *stats, void *workspace, size_t workspace_bytes,
+                    void *stream);
+int byz_policy_loss_backward(const float *dloss, const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                             const int32_t *label, const float *old, const float *advantage, const float *ref,
+                             float clip_low, float clip_high, float kl, float temperature, const float *stats,
+                             void *dlogits, int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream);
+int byz_policy_loss_step(const float *dloss, const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                         const int32_t *label, const float *old, const float *advantage, const float *ref,
+                         float clip_low, float clip_high, float kl, float temperature, float *loss, float *logp,
+                         void *dlogits, int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The preference loss of pairs of sequences: sequence s has the rows bounds[s] .. bounds[s + 1] - 1 (bounds: 2 pairs + 1, not
+ * falling, within 0 .. rows), sequences 2 i and 2 i + 1 are the chosen and the rejected one of pair i.  With sums[s] the
+ * sum of logp over s, and ref[s] the same of a reference model (NULL: zeros),
+ *     margin = beta ((sums - ref)[2 i] - (sums - ref)[2 i + 1]),  sigma(x) = 1 / (1 + exp(-x))
+ *     loss[i] = -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin),  slope[i] = d loss / d margin
+ * Rows of no sequence are in no loss, and their gradient is 0.  A pair whose bounds fall or leave 0 .. rows has a NaN loss and slope.
+ * sums (2 pairs) and slope (pairs, for the backward call) may be NULL.  0 <= smoothing <= 1; beta is finite.
+ */
+int byz_preference_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int32_t *label,
+                        const int32_t *bounds, int64_t pairs, const float *ref, float beta, float smoothing,
+                        float temperature, float *loss, float *sums, float *slope, float *stats, void *workspace,
+                        size_t workspace_bytes, void *stream);
+int byz_preference_loss_backward(const float *dloss, const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                                 const int32_t *label, const int32_t *bounds, int64_t pairs, const float *slope,
+                                 float beta, float temperature, const float *stats, void *dlogits, int64_t dlogits_ld,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+int byz_preference_loss_step(const float *dloss, const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                             const int32_t *label, const int32_t *bounds, int64_t pairs, const float *ref, float beta,
+                             float smoothing, float temperature, float *loss, float *sums, void *dlogits,
+                             int64_t dlogits_ld, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,505 @@
+// A block's output joins the residual: norm, dropout, gate and scale on the way in, and the norm in front of the next block
+// (gfx950).
+//
+//     u = norm(h) w1 + b1,  t = x + s g drop(u),  y = norm(t) w2 + b2
+// The gradients make t again from x and h instead of reading it rounded, so both passes see the same sums.  With
+// a = dy w2, means over a row, and the mean of a alone for the layer norm only,
+//     dt = dout + rstd2 (a - mean a - tn mean(a tn)),  du = s g drop(dt),  dx = dt
+//     dh = rstd1 (b - mean b - hn mean(b hn)),  b = du w1
+//     dw2 = sum dy tn,  db2 = sum dy,  dw1 = sum du hn,  db1 = sum du,  dg = sum s drop(u) dt
+#include <algorithm>
+
+#include "drop.h"
+
+using namespace byz_worker;
+
+namespace {
+
+constexpr int64_t kMaxGrid = 1 << 20;
+
+struct Args {
+    const void *x, *h;
+    int64_t x_ld, h_ld, rows, cols;
+    int post, pre;
+    float eps, scale;
+    const float *w1, *b1, *gate, *w2, *b2;
+    int64_t gate_rows;
+    Drop drop;
+    void *out, *y;
+    int64_t out_ld, y_ld;
+    float *stats;
+};
+
+struct Back {
+    const void *dout, *dy;
+    int64_t dout_ld, dy_ld;
+    const float *stats;
+    void *dx, *dh;
+    int64_t dx_ld, dh_ld;
+    float *rest;      // of each row: mean a, mean a tn, mean b, mean b hn
+    float *partials;  // [chunk][kind][column]
+    float *d_gate;
+    uint32_t kinds;     // bit k: kind k is wanted
+    int64_t chunk;      // rows a block sums
+    int64_t per_group;  // chunks of a gate's rows; 0: a chunk has whole groups
+};
+enum { kW2, kB2, kW1, kB1, kGate, kKinds };
+
+// Sums over the NT threads of a row in a fixed order; every thread gets them.  Two buffers, so that one barrier is enough.
+template <int NT>
+struct Joiner {
+    static constexpr int waves = NT / 64;
+    float2 *lds;  // 2 * waves
+    int turn = 0;
+    __device__ explicit Joiner(float2 *l) : lds(l) {}
+    __device__ __forceinline__ float2 sum(float a, float b) {
+        auto add = [](float2 p, const float2 &q) { return make_float2(p.x + q.x, p.y + q.y); };
+        float2 v = wave_reduce(make_float2(a, b), add);
+        if constexpr (waves > 1) {
+            float2 *at = lds + turn * waves;
+            turn ^= 1;
+            if (threadIdx.x % 64 == 0) at[threadIdx.x / 64] = v;
+            __syncthreads();
+            v = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < waves; w++) v = add(v, at[w]);
+        }
+        return v;
+    }
+};
+
+// V columns of a vector of parameters; 0 beyond the row's end.
+template <int V>
+__device__ __forceinline__ void parameters(const float *p, int64_t col, int n, float none, float (&v)[V]) {
+    if (p && n >= V) {
+        const auto w = get_words<float, V>(p + col);
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = e >= n ? 0.0f : p ? p[col + e] : none;
+    }
+}
+
+struct Stats {
+    float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
+};
+
+// V columns of a row: what the block gives, dropped, and the sum.
+template <typename T, int V>
+struct Piece {
+    float hn[V], v[V], sg[V], t[V];  // normalised h; drop(u); scale * gate; the sum
+    uint32_t kept;
+    __device__ __forceinline__ Piece(const Args &a, const Stats &s, uint64_t offset, int64_t row, int64_t col, int n) {
+        const auto x = get_some<T, V>((const T *)a.x + row * a.x_ld + col, n);
+        if (!a.h) {
+#pragma unroll
+            for (int e = 0; e < V; e++) hn[e] = v[e] = sg[e] = 0.0f, t[e] = x[e];
+            kept = 0;
+            return;
+        }
+        const auto h = get_some<T, V>((const T *)a.h + row * a.h_ld + col, n);
+        float w1[V], b1[V];
+        parameters<V>(a.w1, col, n, 1.0f, w1);
+        parameters<V>(a.b1, col, n, 0.0f, b1);
+        parameters<V>(a.gate ? a.gate + row / a.gate_rows * a.cols : nullptr, col, n, 1.0f, sg);
+        kept = a.drop.threshold ? DropV<V>(a.drop, offset, (uint32_t)row, (uint32_t)col).mask : ~0u;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            hn[e] = (h[e] - s.mean1) * s.rstd1;
+            v[e] = kept >> e & 1 ? fmaf(hn[e], w1[e], b1[e]) * a.drop.scale : 0.0f;
+            sg[e] *= a.scale;
+            t[e] = e < n ? fmaf(sg[e], v[e], x[e]) : 0.0f;
+        }
+    }
+};
+
+// The gradient of the sum and of u at V columns.
+template <typename T, int V>
+struct Gradients {
+    float dy[V], tn[V], dt[V], du[V];
+    __device__ __forceinline__ Gradients(const Args &a, const Back &b, const Stats &s, const Piece<T, V> &p, float mean_a, float mean_atn,
+                                         int64_t row, int64_t col, int n) {
+        float dout[V], w2[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) dout[e] = dy[e] = 0.0f;
+        if (b.dout) {
+            const auto w = get_some<T, V>((const T *)b.dout + row * b.dout_ld + col, n);
+#pragma unroll
+            for (int e = 0; e < V; e++) dout[e] = w[e];
+        }
+        if (b.dy) {
+            const auto w = get_some<T, V>((const T *)b.dy + row * b.dy_ld + col, n);
+#pragma unroll
+            for (int e = 0; e < V; e++) dy[e] = w[e];
+        }
+        parameters<V>(a.w2, col, n, 1.0f, w2);
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            tn[e] = (p.t[e] - s.mean2) * s.rstd2;
+            dt[e] = b.dy ? dout[e] + s.rstd2 * (dy[e] * w2[e] - mean_a - tn[e] * mean_atn) : dout[e];
+            du[e] = p.kept >> e & 1 ? p.sg[e] * a.drop.scale * dt[e] : 0.0f;
+        }
+    }
+};
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void forward_kernel(Args a) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float2 lds[2 * NT / 64];
+    Joiner<NT> join(lds);
+    const uint64_t offset = drop_offset(a.drop);
+    const float inv = 1.0f / (float)a.cols;
+    auto over = [&](auto f) {
+        for (int64_t col = (int64_t)threadIdx.x * V; col < a.cols; col += NT * V) f(col, (int)std::min<int64_t>(V, a.cols - col));
+    };
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        Stats s;
+        auto moments = [&](int kind, float &mean, float &rstd, auto value) {
+            if (kind == BYZ_NORM_NONE) return;
+            float sum = 0.0f;
+            if (kind == BYZ_NORM_LAYER) {
+                over([&](int64_t col, int n) { value(col, n, [&](int e, float v) { sum += v; }); });
+                mean = join.sum(sum, 0.0f).x * inv;
+                sum = 0.0f;
+            }
+            over([&](int64_t col, int n) {
+                value(col, n, [&](int e, float v) { sum += e < n ? (v - mean) * (v - mean) : 0.0f; });
+            });
+            rstd = 1.0f / sqrtf(join.sum(sum, 0.0f).x * inv + a.eps);
+        };
+        if (a.h)
+            moments(a.post, s.mean1, s.rstd1, [&](int64_t col, int n, auto f) {
+                const auto h = get_some<T, V>((const T *)a.h + row * a.h_ld + col, n);
+#pragma unroll
+                for (int e = 0; e < V; e++) f(e, h[e]);
+            });
+        moments(a.pre, s.mean2, s.rstd2, [&](int64_t col, int n, auto f) {
+            const Piece<T, V> p(a, s, offset, row, col, n);
+#pragma unroll
+            for (int e = 0; e < V; e++) f(e, p.t[e]);
+        });
+        over([&](int64_t col, int n) {
+            const Piece<T, V> p(a, s, offset, row, col, n);
+            if (a.out && a.h) put_some<T, V>((T *)a.out + row * a.out_ld + col, n, Words<T, V>::of([&](int e) { return p.t[e]; }));
+            if (a.pre == BYZ_NORM_NONE) return;
+            float w2[V], b2[V];
+            parameters<V>(a.w2, col, n, 1.0f, w2);
+            parameters<V>(a.b2, col, n, 0.0f, b2);
+            put_some<T, V>((T *)a.y + row * a.y_ld + col, n,
+                           Words<T, V>::of([&](int e) { return fmaf((p.t[e] - s.mean2) * s.rstd2, w2[e], b2[e]); }));
+        });
+        if (a.stats && threadIdx.x == 0) {
+            float *at = a.stats + row * 4;
+            at[0] = s.mean1, at[1] = s.rstd1, at[2] = s.mean2, at[3] = s.rstd2;
+        }
+    }
+}
+
+__device__ __forceinline__ Stats stats_of(const float *stats, int64_t row) {
+    Stats s;
+    s.mean1 = stats[row * 4], s.rstd1 = stats[row * 4 + 1], s.mean2 = stats[row * 4 + 2], s.rstd2 = stats[row * 4 + 3];
+    return s;
+}
+
+// dx and dh, and the means of each row that the columns' kernel needs.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void rows_kernel(Args a, Back b) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float2 lds[2 * NT / 64];
+    Joiner<NT> join(lds);
+    const uint64_t offset = drop_offset(a.drop);
+    const float inv = 1.0f / (float)a.cols;
+    const float inv_a = a.pre == BYZ_NORM_LAYER ? inv : 0.0f, inv_b = a.post == BYZ_NORM_LAYER ? inv : 0.0f;
+    const float inv_atn = a.pre != BYZ_NORM_NONE ? inv : 0.0f, inv_bhn = a.post != BYZ_NORM_NONE ? inv : 0.0f;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const Stats s = stats_of(b.stats, row);
+        float mean_a = 0.0f, mean_atn = 0.0f, mean_b = 0.0f, mean_bhn = 0.0f;
+        auto over = [&](auto f) {
+            for (int64_t col = (int64_t)threadIdx.x * V; col < a.cols; col += NT * V) {
+                const int n = (int)std::min<int64_t>(V, a.cols - col);
+                const Piece<T, V> p(a, s, offset, row, col, n);
+                f(p, Gradients<T, V>(a, b, s, p, mean_a, mean_atn, row, col, n), col, n);
+            }
+        };
+        if (a.pre != BYZ_NORM_NONE && b.dy) {
+            float p1 = 0.0f, p2 = 0.0f;
+            over([&](const Piece<T, V> &, const Gradients<T, V> &g, int64_t col, int n) {
+                float w2[V];
+                parameters<V>(a.w2, col, n, 1.0f, w2);
+#pragma unroll
+                for (int e = 0; e < V; e++) p1 += g.dy[e] * w2[e], p2 += g.dy[e] * w2[e] * g.tn[e];
+            });
+            const float2 r = join.sum(p1, p2);
+            mean_a = r.x * inv_a, mean_atn = r.y * inv_atn;
+        }
+        if (a.h && a.post != BYZ_NORM_NONE) {
+            float p3 = 0.0f, p4 = 0.0f;
+            over([&](const Piece<T, V> &p, const Gradients<T, V> &g, int64_t col, int n) {
+                float w1[V];
+                parameters<V>(a.w1, col, n, 1.0f, w1);
+#pragma unroll
+                for (int e = 0; e < V; e++) p3 += g.du[e] * w1[e], p4 += g.du[e] * w1[e] * p.hn[e];
+            });
+            const float2 r = join.sum(p3, p4);
+            mean_b = r.x * inv_b, mean_bhn = r.y * inv_bhn;
+        }
+        over([&](const Piece<T, V> &p, const Gradients<T, V> &g, int64_t col, int n) {
+            put_some<T, V>((T *)b.dx + row * b.dx_ld + col, n, Words<T, V>::of([&](int e) { return g.dt[e]; }));
+            if (!a.h) return;
+            float w1[V];
+            parameters<V>(a.w1, col, n, 1.0f, w1);
+            put_some<T, V>((T *)b.dh + row * b.dh_ld + col, n,
+                           Words<T, V>::of([&](int e) {
+                               const float v = g.du[e] * w1[e];
+                               return a.post == BYZ_NORM_NONE ? v : s.rstd1 * (v - mean_b - p.hn[e] * mean_bhn);
+                           }));
+        });
+        if (threadIdx.x == 0) {
+            float *at = b.rest + row * 4;
+            at[0] = mean_a, at[1] = mean_atn, at[2] = mean_b, at[3] = mean_bhn;
+        }
+    }
+}
+
+// Sums over a chunk's rows, four waves with a row each in turn and 64 V columns a wave.  A chunk lies in one group of gate's rows
+// (per_group chunks of it), or has whole groups, which a wave takes whole: their d_gate is written here.
+template <typename T>
+__global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
+    constexpr int V = 16 / sizeof(T), W = 4;
+    __shared__ float lds[W][64 * V];
+    const uint64_t offset = drop_offset(a.drop);
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t col = ((int64_t)blockIdx.x * 64 + lane) * V;
+    const int n = (int)std::max<int64_t>(0, std::min<int64_t>(V, a.cols - col));
+    const int64_t chunk = blockIdx.y, group_rows = a.gate ? a.gate_rows : a.rows;
+    float acc[kKinds][V] = {};
+    auto add = [&](int64_t row) {
+        if (n == 0) return;
+        const Stats s = stats_of(b.stats, row);
+        const Piece<T, V> p(a, s, offset, row, col, n);
+        const Gradients<T, V> g(a, b, s, p, b.rest[row * 4], b.rest[row * 4 + 1], row, col, n);
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            acc[kW2][e] += g.dy[e] * g.tn[e], acc[kB2][e] += g.dy[e];
+            acc[kW1][e] += g.du[e] * p.hn[e], acc[kB1][e] += g.du[e];
+            acc[kGate][e] += a.scale * p.v[e] * g.dt[e];
+        }
+    };
+    if (b.per_group) {
+        const int64_t group = chunk / b.per_group, start = group * group_rows + chunk % b.per_group * b.chunk;
+        const int64_t end = std::min({start + b.chunk, (group + 1) * group_rows, a.rows});
+        for (int64_t row = start + wave; row < end; row += W) add(row);
+    } else {
+        const int64_t end = std::min(a.rows, (chunk + 1) * b.chunk);
+        for (int64_t start = chunk * b.chunk + wave * group_rows; start < end; start += W * group_rows) {
+            for (int64_t row = start; row < std::min(end, start + group_rows); row++) add(row);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                if (b.d_gate && e < n) b.d_gate[start / group_rows * a.cols + col + e] = acc[kGate][e];
+                acc[kGate][e] = 0.0f;
+            }
+        }
+    }
+    int at = 0;
+#pragma unroll
+    for (int k = 0; k < kKinds; k++) {
+        if (!(b.kinds >> k & 1)) continue;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; e++) lds[wave][lane * V + e] = acc[k][e];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 64 * V; i += 256) {
+            const int64_t c = (int64_t)blockIdx.x * 64 * V + i;
+            if (c < a.cols)
+                b.partials[(chunk * __builtin_popcount(b.kinds) + at) * a.cols + c] = (lds[0][i] + lds[1][i]) + (lds[2][i] + lds[3][i]);
+        }
+        at++;
+    }
+}
+
+struct Outputs {
+    float *of[kKinds];
+};
+
+// Sums of the chunks' partials: a block 64 columns of one kind (and one group of gate's rows), its waves every fourth chunk.
+__global__ __launch_bounds__(256) void finish_kernel(const float *partials, Outputs out, uint32_t kinds, int64_t cols, int64_t chunks,
+                                                     int64_t per_group, int64_t groups) {
+    __shared__ float lds[4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, count = __builtin_popcount(kinds);
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    int kind = 0, left = blockIdx.y;
+    for (int k = 0; k < kKinds; k++)
+        if (kinds >> k & 1) {
+            if (left == 0) kind = k;
+            left--;
+        }
+    const bool gate = kind == kGate;
+    for (int64_t group = blockIdx.z; group < (gate ? groups : 1); group += gridDim.z) {
+        const int64_t from = gate ? group * per_group : 0, to = gate ? from + per_group : chunks;
+        float sum = 0.0f;
+        if (col < cols)
+            for (int64_t c = from + wave; c < to; c += 4) sum += partials[(c * count + blockIdx.y) * cols + col];
+        __syncthreads();
+        lds[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && col < cols) {
+            float *to_ = out.of[0];
+#pragma unroll
+            for (int k = 1; k < kKinds; k++) to_ = kind == k ? out.of[k] : to_;
+            to_[(gate ? group * cols : 0) + col] = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+        }
+    }
+}
+
+// How the rows are cut for the sums of columns: about 512 chunks, each within a group of gate's rows, or of whole groups where these
+// are short.
+struct Cut {
+    int64_t chunk, per_group, groups, chunks;
+    Cut(int64_t rows, int64_t gate_rows) {
+        const int64_t want = std::max<int64_t>(4, (rows + 511) / 512);
+        groups = (rows + gate_rows - 1) / gate_rows;
+        if (gate_rows >= want) {
+            chunk = want, per_group = (gate_rows + chunk - 1) / chunk, chunks = groups * per_group;
+        } else {
+            chunk = (want + gate_rows - 1) / gate_rows * gate_rows, per_group = 0, chunks = (rows + chunk - 1) / chunk;
+        }
+    }
+};
+
+bool sizes_ok(int64_t rows, int64_t cols, int dtype, int64_t gate_rows) {
+    int64_t values;
+    return rows >= 0 && cols >= 1 && cols <= INT32_MAX && dtype_known(dtype) && gate_rows >= 1 &&
+           !__builtin_mul_overflow(rows, cols, &values) && values <= (INT64_MAX >> 8);
+}
+
+size_t rest_bytes(int64_t rows) { return (size_t)rows * 16; }
+
+size_t workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
+    return rows == 0 ? 0 : rest_bytes(rows) + (size_t)Cut(rows, std::min(gate_rows, rows)).chunks * kKinds * (size_t)cols * 4;
+}
+
+template <typename T>
+int launch_forward(const Args &a, hipStream_t s) {
+    forward_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+template <typename T>
+int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, hipStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
+    BYZ_HIP(hipGetLastError());
+    if (!b.kinds && !b.d_gate) return BYZ_OK;
+    columns_kernel<T><<<dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), (unsigned)cut.chunks), 256, 0, s>>>(a, b);
+    BYZ_HIP(hipGetLastError());
+    if (!b.kinds) return BYZ_OK;
+    const unsigned depth = b.kinds >> kGate & 1 ? (unsigned)std::min<int64_t>(cut.groups, 1024) : 1;
+    finish_kernel<<<dim3((unsigned)((a.cols + 63) / 64), (unsigned)__builtin_popcount(b.kinds), depth), 256, 0, s>>>(
+        b.partials, out, b.kinds, a.cols, cut.chunks, cut.per_group, cut.groups);
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+__global__ void zero_kernel(float *p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = 0.0f;
+}
+
+bool norm_known(int n) { return n >= BYZ_NORM_NONE && n <= BYZ_NORM_LAYER; }
+bool real(float v) { return v > -INFINITY && v < INFINITY; }
+
+// A matrix that may not be there.
+bool matrix_ok(const void *p, int64_t ld, int64_t rows, int64_t cols, int dtype) {
+    return !p || (aligned(p, dtype_size(dtype)) && ld >= cols && extent_ok(rows, ld, cols));
+}
+bool floats_ok(const float *p) { return aligned(p, 4); }
+
+int check(const Args &a, const byz_residual_form *f, int dtype) {
+    if (!f || !sizes_ok(a.rows, a.cols, dtype, a.gate_rows) || !norm_known(f->post) || !norm_known(f->pre) || !(f->eps >= 0.0f) ||
+        !real(f->eps) || !real(f->scale) || !drop_ok(f->p, f->offset_at, f->first_row, a.rows, a.cols))
+        return BYZ_EINVAL;
+    if (a.rows > 0 && !a.h && (f->post != BYZ_NORM_NONE || a.w1 || a.b1 || a.gate || f->pre == BYZ_NORM_NONE)) return BYZ_EINVAL;
+    if (f->pre == BYZ_NORM_NONE && (a.w2 || a.b2)) return BYZ_EINVAL;
+    if (!floats_ok(a.w1) || !floats_ok(a.b1) || !floats_ok(a.gate) || !floats_ok(a.w2) || !floats_ok(a.b2)) return BYZ_EINVAL;
+    if (a.rows == 0) return BYZ_OK;
+    if (!a.x || !matrix_ok(a.x, a.x_ld, a.rows, a.cols, dtype) || !matrix_ok(a.h, a.h_ld, a.rows, a.cols, dtype)) return BYZ_EINVAL;
+    return BYZ_OK;
+}
+
+Args args_of(const void *x, int64_t x_ld, const void *h, int64_t h_ld, int64_t rows, int64_t cols, const byz_residual_form *f,
+             const float *w1, const float *b1, const float *gate, int64_t gate_rows, const float *w2, const float *b2) {
+    Args a{};
+    a.x = x, a.h = h, a.x_ld = x_ld, a.h_ld = h_ld, a.rows = rows, a.cols = cols;
+    a.w1 = w1, a.b1 = b1, a.gate = gate, a.w2 = w2, a.b2 = b2;
+    a.gate_rows = gate ? std::min(gate_rows, std::max<int64_t>(rows, 1)) : std::max<int64_t>(rows, 1);
+    if (gate && gate_rows < 1) a.gate_rows = gate_rows;  // refused
+    if (!f) return a;
+    a.post = f->post, a.pre = f->pre, a.eps = f->eps, a.scale = f->scale;
+    return a;
+}
+
+}  // namespace
+
+extern "C" int byz_residual_norm(const void *x, int64_t x_ld, const void *h, int64_t h_ld, int64_t rows, int64_t cols, int dtype,
+                                 const byz_residual_form *form, const float *post_weight, const float *post_bias, const float *gate,
+                                 int64_t gate_rows, const float *pre_weight, const float *pre_bias, void *out, int64_t out_ld,
+                                 void *y, int64_t y_ld, float *stats, void *stream) {
+    Args a = args_of(x, x_ld, h, h_ld, rows, cols, form, post_weight, post_bias, gate, gate_rows, pre_weight, pre_bias);
+    const int rc = check(a, form, dtype);
+    if (rc != BYZ_OK || rows == 0) return rc;
+    if ((h && !out) || (form->pre != BYZ_NORM_NONE && !y) || !floats_ok(stats) || !matrix_ok(h ? out : nullptr, out_ld, rows, cols, dtype) ||
+        !matrix_ok(form->pre != BYZ_NORM_NONE ? y : nullptr, y_ld, rows, cols, dtype))
+        return BYZ_EINVAL;
+    a.drop = drop_of(form->p, form->seed, form->offset, form->offset_at, form->first_row);
+    a.out = out, a.out_ld = out_ld, a.y = y, a.y_ld = y_ld, a.stats = stats;
+    const hipStream_t s = (hipStream_t)stream;
+    return dtype == BYZ_F32 ? launch_forward<float>(a, s) : dtype == BYZ_BF16 ? launch_forward<bf16>(a, s) : launch_forward<f16>(a, s);
+}
+
+extern "C" size_t byz_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype, int64_t gate_rows) {
+    return sizes_ok(rows, cols, dtype, gate_rows) ? workspace(rows, cols, gate_rows) : 0;
+}
+
+extern "C" int byz_residual_norm_backward(const void *dout, int64_t dout_ld, const void *dy, int64_t dy_ld, const void *x,
+                                          int64_t x_ld, const void *h, int64_t h_ld, const float *stats, int64_t rows, int64_t cols,
+                                          int dtype, const byz_residual_form *form, const float *post_weight,
+                                          const float *post_bias, const float *gate, int64_t gate_rows, const float *pre_weight,
+                                          void *dx, int64_t dx_ld, void *dh, int64_t dh_ld, float *d_post_weight,
+                                          float *d_post_bias, float *d_gate, float *d_pre_weight, float *d_pre_bias,
+                                          void *workspace_, size_t workspace_bytes, void *stream) {
+    Args a = args_of(x, x_ld, h, h_ld, rows, cols, form, post_weight, post_bias, gate, gate_rows, pre_weight, nullptr);
+    const int rc = check(a, form, dtype);
+    if (rc != BYZ_OK) return rc;
+    if (!floats_ok(d_post_weight) || !floats_ok(d_post_bias) || !floats_ok(d_gate) || !floats_ok(d_pre_weight) || !floats_ok(d_pre_bias) ||
+        (rows > 0 && !h && (d_post_weight || d_post_bias || d_gate)) || (d_gate && !gate) ||
+        (form->pre == BYZ_NORM_NONE && (d_pre_weight || d_pre_bias || dy)))
+        return BYZ_EINVAL;
+    const hipStream_t s = (hipStream_t)stream;
+    const Outputs out{{d_pre_weight, d_pre_bias, d_post_weight, d_post_bias, d_gate}};
+    if (rows == 0) {
+        for (int k = 0; k < kKinds; k++)
+            if (out.of[k]) {
+                zero_kernel<<<(unsigned)((cols + 255) / 256), 256, 0, s>>>(out.of[k], cols);
+                BYZ_HIP(hipGetLastError());
+            }
+        return BYZ_OK;
+    }
+    if (!dx || (h && !dh) || !stats || !floats_ok(stats) || (!dout && !dy) || !matrix_ok(dout, dout_ld, rows, cols, dtype) ||
+        !matrix_ok(dy, dy_ld, rows, cols, dtype) || !matrix_ok(dx, dx_ld, rows, cols, dtype) ||
+        !matrix_ok(h ? dh : nullptr, dh_ld, rows, cols, dtype))
+        return BYZ_EINVAL;
+    if (!workspace_ || !aligned(workspace_, 16) || workspace_bytes < workspace(rows, cols, a.gate_rows)) return BYZ_ENOMEM;
+    a.drop = drop_of(form->p, form->seed, form->offset, form->offset_at, form->first_row);
+    const Cut cut(rows, a.gate_rows);
+    Back b{};
+    b.dout = dout, b.dout_ld = dout_ld, b.dy = dy, b.dy_ld = dy_ld, b.stats = stats;
+    b.dx = dx, b.dx_ld = dx_ld, b.dh = dh, b.dh_ld = dh_ld;
+    b.rest = (float *)workspace_, b.partials = b.rest + rows * 4;
+    b.d_gate = cut.per_group ? nullptr : d_gate;
+    for (int k = 0; k < kKinds; k++)
+        if (out.of[k] && (k != kGate || cut.per_group)) b.kinds |= 1u << k;
+    b.chunk = cut.chunk, b.per_group = cut.per_group;
+    return dtype == BYZ_F32 ? launch_backward<float>(a, b, cut, out, s)
+           : dtype == BYZ_BF16 ? launch_backward<bf16>(a, b, cut, out, s) : launch_backward<f16>(a, b, cut, out, s);
+}

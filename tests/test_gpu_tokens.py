@@ -1,0 +1,630 @@
+"""The token operators against their definitions in 64 bits.
+
+Tolerances.  u = finfo(type).eps / 2 is what one rounding can be off, relative to the value; fp32 arithmetic
+is allowed some dozens of 2^-24 of the terms that enter a result (tests/token_forms.py has them beside each result).
+"""
+import itertools
+import math
+
+import pytest
+import torch
+
+import paper_2010_04902_amd as B
+from token_forms import E, kept, kept_scale, logp_terms, policy, preference, residual
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _randn(gen, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(*shape, generator=gen, device=DEV) * scale).to(dtype)
+
+
+def _u(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def _tiny(dtype):
+    return torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+
+
+def _near(got, want, tol, what):
+    got, want = got.double().cpu(), want.cpu()
+    assert got.shape == want.shape, what
+    same = (got == want) | (got.isnan() & want.isnan())
+    bad = ~(((got - want).abs() <= tol.cpu()) | same)
+    assert not bool(bad.any()), "%s: %d of %d off, worst by %.3g of what is allowed" % (
+        what, int(bad.sum()), bad.numel(), float(((got - want).abs() / tol.cpu()).nan_to_num(nan=math.inf)[bad].max()))
+
+
+def _same_bits(a, b):
+    view = torch.int32 if a.dtype == F32 else torch.int16
+    return torch.equal(a.contiguous().view(view), b.contiguous().view(view))
+
+
+# ------------------------------------------------------------------ dropout
+
+
+def _dropped(x, p, seed, offset=0, first_row=0):
+    mask = kept(*x.shape, p, seed, offset, first_row)
+    return torch.where(mask, x.double().cpu() * kept_scale(p), 0.0), mask
+
+
+def _dropout_check(y, x, p, *key):
+    want, mask = _dropped(x, p, *key)
+    # the scale's rounding to fp32, the product's, and the result's
+    _near(y, want, (_u(x.dtype) + 2 * E) * want.abs() + _tiny(x.dtype), "y")
+    assert bool((y.cpu()[~mask] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, cols", [(1, 1), (1, 7), (1, 8), (3, 9), (30, 512), (257, 13), (5, 4099), (1, 100003), (1000, 3),
+                                        (700, 264)])
+def test_dropout(rows, cols, dtype):
+    x = _randn(_gen(rows), rows, cols, dtype=dtype)
+    for p, seed, offset in ((0.1, 7, 0), (0.5, 2 ** 64 - 3, 2 ** 63 + 11), (0.0, 1, 1), (1.0, 1, 1), (2.0 ** -16, 3, 5)):
+        _dropout_check(B.byz_dropout(x, p, seed, offset), x, p, seed, offset)
+
+
+def test_dropout_of_rows_in_parts():
+    x = _randn(_gen(0), 300, 77, dtype=BF16)
+    whole = B.byz_dropout(x, 0.3, 11, 5)
+    parts = [B.byz_dropout(x[at:at + 100], 0.3, 11, 5, first_row=at) for at in (0, 100, 200)]
+    assert _same_bits(torch.cat(parts), whole)
+    last = 2 ** 32 - 2
+    _dropout_check(B.byz_dropout(x[:2], 0.3, 11, 5, first_row=last), x[:2], 0.3, 11, 5, last)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_dropout_of_other_layouts(dtype):
+    wide = _randn(_gen(1), 41, 203, dtype=dtype)
+    for part in (wide[:, 1:100], wide[::2, 3:200], wide[:, :8]):
+        dense = B.byz_dropout(part.contiguous(), 0.25, 3)
+        assert _same_bits(B.byz_dropout(part, 0.25, 3), dense)
+        out = torch.full_like(wide, 5.0)
+        place = out[:part.shape[0], 2:2 + part.shape[1]]
+        assert B.byz_dropout(part, 0.25, 3, out=place) is place
+        assert _same_bits(place, dense)
+        place.fill_(5.0)
+        assert bool((out == 5.0).all())  # nothing beside it was written
+    copy = wide.clone()
+    B.byz_dropout(copy, 0.25, 3, out=copy)
+    assert _same_bits(copy, B.byz_dropout(wide, 0.25, 3))
+
+
+def test_dropout_takes_what_is_not_finite():
+    x = torch.full((4, 64), math.nan, device=DEV)
+    x[2:] = math.inf
+    y, mask = B.byz_dropout(x, 0.5, 9).cpu(), kept(4, 64, 0.5, 9)
+    assert bool((y[~mask] == 0).all()) and bool(y[:2][mask[:2]].isnan().all()) and bool(y[2:][mask[2:]].isinf().all())
+
+
+def test_dropout_share():
+    # 4 million values: the share that stays is binomial, 6 deviations are allowed
+    y = B.byz_dropout(torch.ones(2048, 2048, device=DEV), 0.1, 1234, 1)
+    n, q = 2 ** 22, 1 - round(0.1 * 65536) / 65536
+    assert abs(int((y != 0).sum()) - n * q) < 6 * math.sqrt(n * q * (1 - q))
+    other = B.byz_dropout(torch.ones(2048, 2048, device=DEV), 0.1, 1234, 2)
+    both = int(((y != 0) & (other != 0)).sum())
+    assert abs(both - n * q * q) < 6 * math.sqrt(n * q * q * (1 - q * q))
+
+
+def test_dropout_offset_from_memory():
+    x = _randn(_gen(2), 9, 100)
+    at = torch.tensor([5], device=DEV)
+    assert _same_bits(B.byz_dropout(x, 0.5, 1, 7, offset_at=at), B.byz_dropout(x, 0.5, 1, 12))
+    at.fill_(-3)
+    assert _same_bits(B.byz_dropout(x, 0.5, 1, 2, offset_at=at), B.byz_dropout(x, 0.5, 1, -1))
+
+
+def test_dropout_of_more_than_2_31_values():
+    # the far rows of a matrix whose places pass 32 bits, as parts of it
+    rows, cols = 2 ** 17 + 3, 2 ** 14 + 5
+    x = torch.ones(rows, cols, dtype=BF16, device=DEV)
+    y = B.byz_dropout(x, 0.5, 3)
+    for at in (0, rows // 2, rows - 5):
+        assert _same_bits(y[at:at + 5], B.byz_dropout(x[at:at + 5], 0.5, 3, first_row=at))
+    want, _ = _dropped(x[:2], 0.5, 3, 0, rows - 2)
+    assert torch.equal(y[rows - 2:].double().cpu(), want)
+
+
+# ------------------------------------------------------------------ residual and norms
+
+
+def _residual_case(rows, cols, dtype, post, pre, gate, p, bias=None, weights=True, seed=0):
+    gen = _gen(seed)
+    c = {"x": _randn(gen, rows, cols, dtype=dtype, scale=2.0), "h": (_randn(gen, rows, cols) + 0.5).to(dtype)}
+    make = lambda mean, there: mean + _randn(gen, cols, scale=0.3) if there else None  # noqa: E731
+    bias1, bias2 = (post == "layer", pre == "layer") if bias is None else (bias, bias and pre != "none")
+    c["w1"], c["b1"] = make(1, weights), make(0, bias1)
+    c["w2"], c["b2"] = make(1, weights and pre != "none"), make(0, bias2)
+    c["gate"] = None if gate == 0 else 1 + _randn(gen, cols, scale=0.3) if gate == 1 else 1 + _randn(gen, gate, cols, scale=0.3)
+    c["dout"] = _randn(gen, rows, cols, dtype=dtype)
+    c["dy"] = _randn(gen, rows, cols, dtype=dtype) if pre != "none" else None
+    c["form"] = B.byz_residual_form(post=B.BYZ_NORMS[post], pre=B.BYZ_NORMS[pre], scale=0.75, p=p, seed=99, offset=seed)
+    return c
+
+
+def _cpu(t):
+    return None if t is None else t.cpu()
+
+
+def _residual_want(c, post, pre, p, dout=True, dy=True):
+    x = c["x"]
+    mask = kept(*x.shape, p, 99, c["form"].offset, c["form"].first_row)
+    return residual(x.cpu(), _cpu(c["h"]), post, pre, 0.75, float(torch.tensor(1e-5, dtype=F32)), mask, kept_scale(p), _cpu(c["w1"]),
+                    _cpu(c["b1"]), _cpu(c["gate"]), _cpu(c["w2"]), _cpu(c["b2"]), _cpu(c["dout"]) if dout else None,
+                    _cpu(c["dy"]) if dy else None)
+
+
+def _residual_run(c, stream=None, dout=True, dy=True):
+    vectors = (c["w1"], c["b1"], c["gate"], c["w2"], c["b2"])
+    out, y, stats = B.byz_residual_norm(c["x"], c["h"], c["form"], *vectors, stream=stream)
+    dx, dh, grads = B.byz_residual_norm_backward(c["dout"] if dout else None, c["dy"] if dy else None, c["x"], c["h"], stats,
+                                                 c["form"], *vectors, stream=stream)
+    got = {"out": out, "y": y, "stats": stats, "dx": dx, "dh": dh}
+    got.update(zip(("d_post_weight", "d_post_bias", "d_gate", "d_pre_weight", "d_pre_bias"), grads))
+    return {name: t for name, t in got.items() if t is not None}
+
+
+def _residual_check(got, want, dtype):
+    for name, t in got.items():
+        u = 0.0 if t.dtype == F32 else _u(dtype)
+        _near(t, want[name], u * want[name].abs() + 64 * E * want[name + "_scale"] + _tiny(t.dtype), name)
+
+
+KINDS = list(itertools.product(("none", "rms", "layer"), ("none", "rms", "layer")))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("post, pre", KINDS)
+@pytest.mark.parametrize("gate, p", [(0, 0.0), (1, 0.2), (3, 0.1)])
+def test_residual_kinds(post, pre, gate, p, dtype):
+    c = _residual_case(36, 200, dtype, post, pre, gate, p)
+    _residual_check(_residual_run(c), _residual_want(c, post, pre, p), dtype)
+
+
+WIDTHS = [(1, 1), (3, 2), (2, 7), (5, 8), (7, 33), (4, 64), (9, 127), (3, 128), (40, 257), (4, 512), (3, 515), (6, 1000),
+          (3, 1024), (5, 2048), (2, 2051), (3, 4096), (2, 4104), (3, 8192), (2, 8200), (2, 16384), (2, 33000), (1, 70001)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, cols", WIDTHS)
+def test_residual_widths(rows, cols, dtype):
+    c = _residual_case(rows, cols, dtype, "rms", "layer", 1, 0.1, seed=cols)
+    _residual_check(_residual_run(c), _residual_want(c, "rms", "layer", 0.1), dtype)
+    # every vector and bias there is, with a gate of each row
+    c = _residual_case(rows, cols, dtype, "layer", "rms", rows, 0.3, bias=True, seed=cols + 1)
+    _residual_check(_residual_run(c), _residual_want(c, "layer", "rms", 0.3), dtype)
+
+
+@pytest.mark.parametrize("rows, gate", [(1000, 1), (1000, 1000), (1000, 500), (1024, 64), (999, 3), (4096, 2), (4099, 1)])
+def test_residual_many_rows(rows, gate):
+    c = _residual_case(rows, 72, F32, "rms", "rms", gate, 0.1, bias=True)
+    _residual_check(_residual_run(c), _residual_want(c, "rms", "rms", 0.1), F32)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_residual_without_vectors(dtype):
+    for post, pre in KINDS:
+        c = _residual_case(19, 130, dtype, post, pre, 0, 0.5, bias=False, weights=False)
+        _residual_check(_residual_run(c), _residual_want(c, post, pre, 0.5), dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, cols", [(3, 64), (70, 1000), (2, 9000)])
+def test_norm_alone(rows, cols, dtype):
+    for pre in ("rms", "layer"):
+        c = _residual_case(rows, cols, dtype, "none", pre, 0, 0.0)
+        c["h"] = c["w1"] = c["b1"] = None
+        got, want = _residual_run(c), _residual_want(c, "none", pre, 0.0)
+        assert got.pop("out") is c["x"] and "dh" not in got
+        _residual_check(got, want, dtype)
+
+
+def test_residual_one_gradient_alone():
+    for dout, dy in ((True, False), (False, True)):
+        for rows, cols in ((20, 300), (2, 9000)):
+            c = _residual_case(rows, cols, BF16, "layer", "rms", 1, 0.1)
+            _residual_check(_residual_run(c, dout=dout, dy=dy), _residual_want(c, "layer", "rms", 0.1, dout, dy), BF16)
+
+
+def test_residual_everything_dropped():
+    c = _residual_case(6, 100, F32, "rms", "rms", 1, 1.0)
+    got = _residual_run(c)
+    assert _same_bits(got["out"], c["x"]) and bool((got["dh"] == 0).all()) and bool((got["d_gate"] == 0).all())
+    _residual_check(got, _residual_want(c, "rms", "rms", 1.0), F32)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cols", [50, 203, 1001, 9001])
+def test_residual_of_other_layouts(cols, dtype):
+    """Odd pitches and addresses: the same bits, and nothing beside the rows is written."""
+    c = _residual_case(13, cols, dtype, "rms", "layer", 1, 0.1)
+    dense = _residual_run(c)
+    for left, right in ((1, 2), (3, 0), (8, 8)):
+        moved = dict(c)
+        for name in ("x", "h", "dout", "dy"):
+            wide = torch.full((13, left + cols + right), math.nan, dtype=dtype, device=DEV)
+            wide[:, left:left + cols] = c[name]
+            moved[name] = wide[:, left:left + cols]
+        for name in ("w1", "gate", "w2", "b2"):
+            wide = torch.full((left + cols,), math.nan, device=DEV)
+            wide[left:] = c[name]
+            moved[name] = wide[left:]
+        got = _residual_run(moved)
+        for name in dense:
+            assert _same_bits(got[name], dense[name]), name
+        room = torch.full((13, left + cols + right), 5.0, dtype=dtype, device=DEV)
+        out = room[:, left:left + cols]
+        B.byz_residual_norm(moved["x"], moved["h"], c["form"], c["w1"], None, c["gate"], c["w2"], c["b2"], out=out)
+        assert _same_bits(out, dense["out"])
+        out.fill_(5.0)
+        assert bool((room == 5.0).all())
+
+
+@pytest.mark.parametrize("cols", [96, 1000, 9001, 40000])
+def test_residual_in_place(cols):
+    c = _residual_case(5, cols, BF16, "layer", "rms", 1, 0.1)
+    vectors = (c["w1"], c["b1"], c["gate"], c["w2"], c["b2"])
+    want = B.byz_residual_norm(c["x"], c["h"], c["form"], *vectors)
+    for name in ("x", "h"):
+        x, h = c["x"].clone(), c["h"].clone()
+        out, y, stats = B.byz_residual_norm(x, h, c["form"], *vectors, out=x if name == "x" else h)
+        assert all(_same_bits(a, b) for a, b in zip((out, y, stats), want))
+
+
+def test_residual_without_rows():
+    c = _residual_case(4, 40, F32, "layer", "layer", 1, 0.1)
+    for name in ("x", "h", "dout", "dy"):
+        c[name] = c[name][:0]
+    got = _residual_run(c)
+    assert got["out"].shape == (0, 40) and got["dx"].shape == (0, 40)
+    for name in ("d_post_weight", "d_post_bias", "d_gate", "d_pre_weight", "d_pre_bias"):
+        assert bool((got[name] == 0).all()), name
+
+
+def test_residual_gradients_against_differences():
+    """Loss = <out, dout> + <y, dy>; central differences of the 64-bit form along a direction against the operator's gradients."""
+    c = _residual_case(12, 40, F32, "layer", "rms", 3, 0.25, bias=True)
+    got = _residual_run(c)
+    mask, eps = kept(12, 40, 0.25, 99, c["form"].offset), float(torch.tensor(1e-5, dtype=F32))
+
+    def loss(v):
+        r = residual(v["x"], v["h"], "layer", "rms", 0.75, eps, mask, kept_scale(0.25), v["w1"], v["b1"], v["gate"], v["w2"], v["b2"])
+        return float((r["out"] * c["dout"].cpu().double()).sum() + (r["y"] * c["dy"].cpu().double()).sum())
+
+    base = {n: c[n].cpu().double() for n in ("x", "h", "w1", "b1", "gate", "w2", "b2")}
+    for name, grad in (("x", "dx"), ("h", "dh"), ("w1", "d_post_weight"), ("b1", "d_post_bias"), ("gate", "d_gate"),
+                       ("w2", "d_pre_weight"), ("b2", "d_pre_bias")):
+        torch.manual_seed(1)
+        way, step = torch.randn(base[name].shape, dtype=torch.float64), 1e-5
+        ahead, behind = (loss({**base, name: base[name] + s * way}) for s in (step, -step))
+        slope = float((got[grad].cpu().double() * way).sum())
+        # the third derivative's share is some 1e-10, rounding of a loss of some hundred over the step 1e-9, fp32 results 1e-6
+        assert abs((ahead - behind) / (2 * step) - slope) < 1e-5 * (1 + float((got[grad].cpu().abs() * way.abs()).sum())), name
+
+
+def test_residual_ignores_what_is_dropped():
+    """A value that is not finite where the mask drops it reaches neither the sum nor its gradient (without a norm of h)."""
+    c = _residual_case(8, 64, F32, "none", "rms", 1, 0.5)
+    want = _residual_run(c)
+    mask = kept(8, 64, 0.5, 99, c["form"].offset)
+    c["h"] = torch.where(mask.to(DEV), c["h"], math.inf)
+    got = _residual_run(c)
+    for name in ("out", "y", "stats", "dx", "dh", "d_gate"):
+        assert _same_bits(got[name], want[name]), name
+
+
+# ------------------------------------------------------------------ losses
+
+
+def _logits(rows, vocab, dtype, seed=0, banned=0.0, scale=2.0, shift=0.0):
+    gen = _gen(seed)
+    z = _randn(gen, rows, vocab, scale=scale) + shift
+    label = torch.randint(0, vocab, (rows,), generator=gen, device=DEV)
+    z[torch.arange(rows, device=DEV), label] += math.log(vocab)
+    if banned:
+        ban = torch.rand(rows, vocab, generator=gen, device=DEV) < banned
+        ban[torch.arange(rows, device=DEV), label] = False
+        z = z.masked_fill(ban, -math.inf)
+    label = label.to(torch.int32)
+    if rows > 2:
+        label[rows // 2] = -1  # no token
+    return z.to(dtype), label
+
+
+def _logp_tol(logp):
+    # the fp32 sum of exponentials and its logarithm; logp's own rounding
+    return torch.where(logp.isinf(), 0.0, 64 * E + 2 * E * logp.abs())
+
+
+def _gradient_tol(want, w, w_tol, q, dtype):
+    """w (onehot - q): w's error, that of q (its exponent's rounding grows with it), the result's rounding."""
+    q_log = torch.where(q > 0, -q.clamp_min(1e-300).log(), 0.0)
+    near = w_tol[:, None] * (want / torch.where(w == 0, 1.0, w)[:, None]).abs() + E * w.abs()[:, None] * (q * (128 + 4 * q_log) + 8 * (want * w[:, None] > 0))
+    return _u(dtype) * want.abs() + near + _tiny(dtype) + w.abs()[:, None] * 2.0 ** -149
+
+
+ROWS = [(1, 1), (2, 3), (3, 10), (30, 10), (4, 1000), (5, 2047), (3, 8193), (7, 20011), (300, 5000), (2, 50021), (1, 200003),
+        (130, 40000), (140, 70000), (131, 131072)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", ROWS)
+def test_token_logp(rows, vocab, dtype):
+    for temperature, banned in ((1.0, 0.0), (0.7, 0.2 if vocab > 5 else 0.0)):
+        z, label = _logits(rows, vocab, dtype, vocab, banned)
+        logp, stats = B.byz_token_logp(z, label, temperature)
+        want, q, hot = logp_terms(z, label, temperature)
+        _near(logp, want, _logp_tol(want), "logp")
+        d = _randn(_gen(1), rows)
+        grad = B.byz_token_logp_backward(d, z, label, stats, temperature)
+        w = d.double() / temperature
+        full = w[:, None] * (hot - q)
+        # the statistics' rounding to fp32 is in q: the log-sum's is E of it
+        _near(grad, full, _gradient_tol(full, w, 4 * E * w.abs(), q, dtype) + E * w.abs()[:, None] * q * 16, "dlogits")
+
+
+def _policy_case(rows, vocab, dtype, temperature, kl, seed=0):
+    z, label = _logits(rows, vocab, dtype, seed)
+    logp, q, hot = logp_terms(z, label, temperature)
+    gen = _gen(seed + 1)
+    moved = _randn(gen, rows, scale=0.2).double()
+    for end in (0.8, 1.28):  # no ratio within rounding of the clipping's ends
+        moved = torch.where((moved.exp() - end).abs() < 1e-3, moved + 0.01, moved)
+    old, ref = (logp - moved).float(), (logp + _randn(gen, rows, scale=0.3)).float()
+    advantage = _randn(gen, rows)
+    advantage[::5] = 0.0
+    dloss = torch.rand(rows, generator=gen, device=DEV) + 0.5
+    terms = {"ref": ref if kl else None, "kl": kl, "clip_low": 0.2, "clip_high": 0.28, "temperature": temperature}
+    loss, slope, scale = policy(logp, old, advantage, ref, 0.2, 0.28, kl)
+    none = label < 0
+    loss, slope = torch.where(none, 0.0, loss), torch.where(none, 0.0, slope)
+    w = dloss.double() * slope / temperature
+    # logp's error acts through the slope's own terms
+    rough = (dloss.double() / temperature * scale) * (64 * E + 4 * E * (logp.abs() + old.double().abs()))
+    want = {"loss": loss, "logp": logp, "dlogits": w[:, None] * (hot - q)}
+    lossy = scale * (64 * E + 4 * E * (logp.abs() + old.double().abs() + ref.double().abs())) + 4 * E * loss.abs()
+    tol = {"loss": lossy + 2.0 ** -140, "logp": _logp_tol(logp), "dlogits": _gradient_tol(want["dlogits"], w, rough, q, dtype)}
+    return (z, label, old, advantage), dloss, terms, want, tol, w, q
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", ROWS)
+def test_policy_loss(rows, vocab, dtype):
+    for temperature, kl in ((1.0, 0.0), (0.7, 0.05)):
+        given, dloss, terms, want, tol, w, q = _policy_case(rows, vocab, dtype, temperature, kl, vocab)
+        loss, logp, stats = B.byz_policy_loss(*given, **terms)
+        _near(loss, want["loss"], tol["loss"], "loss")
+        _near(logp, want["logp"], tol["logp"], "logp")
+        loss2, logp2, grad = B.byz_policy_loss_step(*given, dloss, **terms)
+        _near(loss2, want["loss"], tol["loss"], "loss of the step")
+        _near(logp2, want["logp"], tol["logp"], "logp of the step")
+        _near(grad, want["dlogits"], tol["dlogits"], "dlogits of the step")
+        alone = B.byz_policy_loss_backward(dloss, *given, stats, **terms)
+        _near(alone, want["dlogits"], tol["dlogits"] + 16 * E * w.abs()[:, None] * q, "dlogits")
+
+
+def test_policy_loss_at_its_ends():
+    """Ratios of exactly 0 and infinity, advantages of 0, banned labels, labels that are none."""
+    z = torch.zeros(8, 16, device=DEV)
+    label = torch.arange(8, dtype=torch.int32, device=DEV)
+    z[3, 3] = -math.inf  # its token is banned
+    z[4] = -math.inf  # nothing is left
+    z[5] = math.nan
+    label[5] = -1
+    label[6] = 16
+    old = torch.full((8,), -math.log(16.0), device=DEV)
+    old[0] = math.inf  # ratio 0
+    old[1] = -math.inf  # ratio infinite
+    advantage = torch.tensor([1.0, 1.0, 0.0, 1.0, 1.0, 1.0, 1.0, -1.0], device=DEV)
+    loss, logp, stats = B.byz_policy_loss(z, label, old, advantage)
+    dloss = torch.ones(8, device=DEV)
+    _, _, step = B.byz_policy_loss_step(z, label, old, advantage, dloss)
+    alone = B.byz_policy_loss_backward(dloss, z, label, old, advantage, stats)
+    want = torch.tensor([0.0, -1.2, 0.0, 0.0, 0.0, 0.0, math.nan, 1.0], dtype=torch.float64)
+    _near(loss, want, torch.full((8,), 1e-6, dtype=torch.float64), "loss")
+    assert logp[3] == -math.inf and logp[4] == -math.inf and logp[5] == 0
+    for grad in (step, alone):
+        grad = grad.cpu()
+        for row in (0, 1, 2, 3, 4, 5):  # clipped, without advantage, of ratio 0, or no token
+            assert bool((grad[row] == 0).all()), row
+        assert bool(grad[6].isnan().all())
+        assert grad[7, 7] > 0.9 and bool((grad[7, :7] < 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(6, 700), (200, 30000), (140, 80000)])
+def test_logits_far_from_zero(rows, vocab, dtype):
+    """Rows shifted far, masked with the type's lowest value, or of it alone, are those of what remains."""
+    z, label = _logits(rows, vocab, dtype, 3)
+    label[rows // 2] = 1
+    far = z.clone()
+    lowest = torch.finfo(dtype).min
+    far[0] = lowest  # all alike
+    far[1, 10:] = lowest
+    label[1] = 3
+    far[2] = lowest
+    far[2, 5:9] = z[2, 5:9]
+    label[2] = 6
+    if dtype == F32:
+        far[3] = z[3].round() + 2.0 ** 20
+    else:
+        far[3] = (z[3] * 8).round() * 32 + 40000 // (1 if dtype == F16 else 8)
+    far[4] = -math.inf
+    far[4, 7] = lowest
+    label[4] = 7
+    far[5] = torch.finfo(dtype).max
+    for temperature in (1.0, 0.5):
+        want, q, hot = logp_terms(far, label, temperature)
+        logp, stats = B.byz_token_logp(far, label, temperature)
+        _near(logp, want, _logp_tol(want), "logp")
+        d = _randn(_gen(4), rows)
+        w = d.double() / temperature
+        full = w[:, None] * (hot - q)
+        tol = _gradient_tol(full, w, 4 * E * w.abs(), q, dtype) + E * w.abs()[:, None] * q * 16
+        _near(B.byz_token_logp_backward(d, far, label, stats, temperature), full, tol, "dlogits")
+        # the step's gradient at ratio 1 and advantage -1 is that of logp
+        old = torch.where(want.isinf(), 0.0, want).float()
+        loss, logp2, grad = B.byz_policy_loss_step(far, label, old, -torch.ones(rows, device=DEV), d, temperature=temperature,
+                                                   clip_low=1.0)
+        _near(logp2, want, _logp_tol(want), "logp of the step")
+        r = (want - old.double()).exp()
+        _near(grad, full * r[:, None], tol + full.abs() * 64 * E, "dlogits of the step")
+
+
+def _pairs_case(lengths, pad, vocab, dtype, ref=True, seed=0):
+    rows = sum(lengths) + pad
+    z, label = _logits(rows, vocab, dtype, seed)
+    at = 0
+    for n in lengths:  # a prompt
+        label[at:at + n // 4] = -1
+        at += n
+    bounds = torch.tensor([0] + list(itertools.accumulate(lengths)), dtype=torch.int32)
+    logp, q, hot = logp_terms(z, label, 1.0)
+    reference = None
+    if ref and len(lengths):
+        edges = bounds.tolist()
+        sums = torch.stack([logp[a:b].sum() for a, b in zip(edges, edges[1:])])
+        reference = (sums + _randn(_gen(seed + 1), len(lengths), scale=3.0)).float()
+    return z, label, bounds, reference, logp.cpu(), q, hot
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("lengths, pad, vocab", [
+    ([1, 1], 0, 1), ([3, 2], 1, 10), ([5, 0, 0, 4], 3, 33), ([0, 0], 2, 8), ([20, 31, 7, 1, 300, 2], 5, 1000), ([40, 41] * 20, 9, 257),
+    ([9, 4, 3, 8], 0, 20011), ([60, 70], 10, 40000), ([700, 650], 3, 300), ([], 4, 12)], ids=str)
+def test_preference_loss(lengths, pad, vocab, dtype):
+    for ref, smoothing in ((True, 0.0), (False, 0.1)):
+        beta = 0.3
+        z, label, bounds, reference, logp, q, hot = _pairs_case(lengths, pad, vocab, dtype, ref, vocab)
+        loss, sums, slope, sequence = preference(logp, bounds, _cpu(reference), beta, smoothing)
+        pairs = len(lengths) // 2
+        dloss = torch.rand(pairs, generator=_gen(5), device=DEV) + 0.5
+        sign = torch.where(sequence % 2 == 0, 1.0, -1.0).double()
+        each = torch.cat((beta * slope * dloss.cpu().double(), torch.zeros(1, dtype=torch.float64)))
+        w = sign * each[torch.where(sequence >= 0, sequence // 2, pairs)] * (label.cpu() >= 0)
+        want = w.to(DEV)[:, None] * (hot - q)
+        # a sum's error: that of each of its log-probabilities
+        long = max(lengths, default=0)
+        sums_tol = torch.full_like(sums, 64 * E * long) + 2 * E * sums.abs()
+        margin_tol = beta * (128 * E * long + 4 * E * (float(reference.abs().max()) if reference is not None and pairs else 0.0))
+        w_tol = w.abs() * 8 * E + margin_tol * beta * 1.5
+        given = (z, label, bounds.to(DEV))
+        terms = {"beta": beta, "smoothing": smoothing}
+        got, got_sums, got_slope, stats = B.byz_preference_loss(*given, reference, **terms)
+        _near(got, loss, margin_tol + 4 * E * loss + 2.0 ** -140, "loss")
+        _near(got_sums, sums, sums_tol, "sums")
+        _near(got_slope, slope, torch.full_like(slope, margin_tol) + 4 * E, "slope")
+        tol = _gradient_tol(want, w.to(DEV), w_tol.to(DEV), q, dtype)
+        got2, sums2, grad = B.byz_preference_loss_step(*given, dloss, reference, **terms)
+        assert _same_bits(got2, got) and _same_bits(sums2, got_sums)
+        _near(grad, want, tol, "dlogits of the step")
+        alone = B.byz_preference_loss_backward(dloss, *given, got_slope, stats, beta)
+        _near(alone, want, tol + 24 * E * w.abs().to(DEV)[:, None] * (q + (hot > 0)), "dlogits")
+        assert bool((grad[sum(lengths):] == 0).all()) and bool((alone[sum(lengths):] == 0).all())
+
+
+def test_preference_loss_of_large_margins():
+    """Margins of some hundred, either way: finite losses, and gradients that vanish or do not."""
+    z = torch.zeros(4, 4, device=DEV)
+    z[0, 0] = z[3, 0] = 200.0
+    label = torch.tensor([0, 1, 1, 0], dtype=torch.int32, device=DEV)
+    z[1, 0] = z[2, 0] = 200.0
+    bounds = torch.tensor([0, 1, 2, 3, 4], dtype=torch.int32, device=DEV)
+    loss, sums, slope, _ = B.byz_preference_loss(z, label, bounds, beta=2.0)
+    assert loss[0] == 0 and abs(float(loss[1]) - 400) < 1e-3 and slope[0] > -1e-30 and slope[1] == -1
+    loss, _, _, _ = B.byz_preference_loss(z, label, bounds, beta=2.0, smoothing=0.25)
+    assert abs(float(loss[0]) - 100) < 1e-3 and abs(float(loss[1]) - 300) < 1e-3
+
+
+def test_preference_loss_of_wrong_bounds():
+    """Bounds that fall or leave the rows: the pair's loss is NaN, nothing is read or written beyond, others are whole."""
+    z, label = _logits(12, 50, F32)
+    good = torch.tensor([0, 3, 6, 9, 12], dtype=torch.int32, device=DEV)
+    want = B.byz_preference_loss(z, label, good)[0]
+    for wrong in ([0, 3, 6, 5, 12], [0, 3, 6, 9, 13], [-1, 3, 6, 9, 12], [2 ** 31 - 1] * 5, [-2 ** 31] * 5):
+        bounds = torch.tensor(wrong, dtype=torch.int32, device=DEV)
+        loss, sums, slope, stats = B.byz_preference_loss(z, label, bounds)
+        ones = torch.ones(2, device=DEV)
+        _, _, grad = B.byz_preference_loss_step(z, label, bounds, ones)
+        alone = B.byz_preference_loss_backward(ones, z, label, bounds, slope, stats)
+        assert grad.shape == alone.shape == z.shape
+        for pair in range(2):
+            a, b, c = wrong[2 * pair:2 * pair + 3]
+            if 0 <= a <= b <= c <= 12:
+                assert loss[pair] == want[pair]
+            else:
+                assert bool(loss[pair].isnan()) and bool(slope[pair].isnan())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(9, 101), (20, 3001), (3, 20011), (140, 70001), (2, 131073)])
+def test_losses_of_other_layouts(rows, vocab, dtype):
+    """Odd pitches and addresses, results in place: the same bits, and nothing beside the rows is written."""
+    given, dloss, terms, *_ = _policy_case(rows, vocab, dtype, 1.0, 0.05)
+    z, rest = given[0], given[1:]
+    bounds = torch.tensor([0, rows // 2, rows], dtype=torch.int32, device=DEV)
+    one = torch.ones(1, device=DEV)
+    dense = B.byz_policy_loss(*given, **terms) + B.byz_policy_loss_step(*given, dloss, **terms)
+    dense += B.byz_preference_loss_step(z, given[1], bounds, one)
+    d = _randn(_gen(7), rows)
+    dense += (B.byz_token_logp_backward(d, z, given[1], dense[2]),)
+    for left, right in ((1, 2), (4, 0), (8, 8)):
+        wide = torch.full((rows, left + vocab + right), math.nan, dtype=dtype, device=DEV)
+        place = wide[:, left:left + vocab]
+        got = []
+
+        def fresh():
+            place.copy_(z)
+            return place
+
+        got += B.byz_policy_loss(fresh(), *rest, **terms)
+        got += [t.clone() for t in B.byz_policy_loss_step(fresh(), *rest, dloss, out=place, **terms)]
+        got += [t.clone() for t in B.byz_preference_loss_step(fresh(), given[1], bounds, one, out=place)]
+        got += [B.byz_token_logp_backward(d, fresh(), given[1], dense[2], out=place).clone()]
+        for at, (a, b) in enumerate(zip(got, dense)):
+            assert _same_bits(a, b), at
+        place.fill_(math.nan)
+        assert bool(wide.isnan().all())
+
+
+def test_losses_without_rows():
+    z, label = torch.zeros(0, 9, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV)
+    none = torch.zeros(0, device=DEV)
+    assert B.byz_token_logp(z, label)[0].shape == (0,)
+    assert B.byz_policy_loss_step(z, label, none, none, none)[2].shape == (0, 9)
+    bounds = torch.zeros(3, dtype=torch.int32, device=DEV)
+    loss, sums, grad = B.byz_preference_loss_step(z, label, bounds, torch.ones(1, device=DEV))
+    assert abs(float(loss[0]) - math.log(2)) < 1e-6 and bool((sums == 0).all()) and grad.shape == (0, 9)
+
+
+def test_loss_gradients_against_differences():
+    """Central differences of the operators' own fp32 losses along one direction."""
+    gen = _gen(11)
+    z, label, bounds, reference, *_ = _pairs_case([7, 9, 4, 6], 2, 60, F32)
+    way, step = _randn(gen, *z.shape), 2.0 ** -7
+    rows = z.shape[0]
+    logp = B.byz_token_logp(z, label)[0]
+    old, advantage = logp - 0.02, _randn(gen, rows) + 0.1
+    terms = {"ref": logp + 0.3, "kl": 0.1, "clip_low": 0.9, "clip_high": 9.0}
+    ones, pairs = torch.ones(rows, device=DEV), torch.ones(2, device=DEV)
+    at = bounds.to(DEV)
+    cases = [(lambda v: B.byz_token_logp(v, label)[0], B.byz_token_logp_backward(ones, z, label, B.byz_token_logp(z, label)[1])),
+             (lambda v: B.byz_policy_loss(v, label, old, advantage, **terms)[0],
+              B.byz_policy_loss_step(z, label, old, advantage, ones, **terms)[2]),
+             (lambda v: B.byz_preference_loss(v, label, at, reference, 0.3)[0],
+              B.byz_preference_loss_step(z, label, at, pairs, reference, 0.3)[2])]
+    for loss, grad in cases:
+        ahead, behind = (loss(z + s * way).double().sum() for s in (step, -step))
+        slope = float((grad.double() * way.double()).sum())
+        # third derivatives of some units a token times step^2 / 6, and fp32's rounding of losses of some units over the step
+        assert abs(float(ahead - behind) / (2 * step) - slope) < rows * (8 * step ** 2 / 6 + 16 * 8 * E / step)
