@@ -16,6 +16,7 @@ using namespace byz_worker;
 namespace {
 
 constexpr int64_t kMaxGrid = 1 << 20;
+constexpr int kCus = 256;  // compute units
 
 struct Args {
     const void *x, *h;
@@ -318,14 +319,387 @@ __global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
     }
 }
 
+// ------------------------------------------------------------------ rows in registers
+
+// Sums over the TPR threads of a row: part of a wave, a wave, or a block.
+template <int TPR>
+struct RowJoiner {
+    static constexpr int waves = TPR / 64;
+    float2 *lds;  // 2 * waves
+    int turn = 0;
+    __device__ explicit RowJoiner(float2 *l) : lds(l) {}
+    // over 2^LANES lanes that lie together; every one gets the same bits
+    template <int LANES>
+    static __device__ __forceinline__ float2 lanes(float2 v) {
+        auto step = [&](auto k) {
+            if constexpr (k.value < LANES) {
+                float2 p, q;
+                wave_pair<k.value>(v, p, q);
+                v = make_float2(p.x + q.x, p.y + q.y);
+            }
+        };
+        wave_steps(1, step);
+        return v;
+    }
+    __device__ __forceinline__ float2 sum(float a, float b) {
+        constexpr int own = TPR >= 64 ? 6 : TPR == 32 ? 5 : 4;
+        float2 v = lanes<own>(make_float2(a, b));
+        if constexpr (waves > 1) {
+            float2 *at = lds + turn * waves;
+            turn ^= 1;
+            if (threadIdx.x % 64 == 0) at[threadIdx.x / 64] = v;
+            __syncthreads();
+            v = lanes<waves == 16 ? 4 : waves == 8 ? 3 : waves == 4 ? 2 : 1>(at[threadIdx.x % waves]);
+        }
+        return v;
+    }
+};
+
+// Which of a block's rows a thread is at: a number that the compiler knows to be a wave's where it is.
+template <int TPR>
+__device__ __forceinline__ int slot_of() {
+    if constexpr (TPR > 64) return 0;
+    const int slot = threadIdx.x / TPR;
+    return TPR == 64 ? __builtin_amdgcn_readfirstlane(slot) : slot;
+}
+
+constexpr int kCols = 8;  // columns of a thread: one call of the generator
+template <int TPR>
+constexpr int block_of() {
+    return TPR <= 64 ? 256 : TPR;
+}
+
+// A vector's values from the `skip`-th on.
+template <typename T, int V>
+__device__ __forceinline__ void put_from(T *to, int skip, const Words<T, V> &v) {
+    if (skip == 0) return put_words(to, v);
+#pragma unroll
+    for (int e = 0; e < V; e++)
+        if (e >= skip) to[e] = round_to<T>(v[e]);
+}
+
+// A thread's eight columns.  The vector of a row's last thread ends with the row, so its first `skip` columns are those of the
+// thread before it; threads beyond have nothing but such columns.  They are read, but in no sum, and not written.
+template <int TPR>
+struct Columns {
+    int first, skip, number;  // number: of the generator's group
+    __device__ __forceinline__ explicit Columns(int64_t cols) {
+        const int own = threadIdx.x % TPR;
+        first = std::min(own * kCols, (int)cols - kCols);
+        skip = std::min(own * kCols - first, kCols);
+        number = std::min(own, ((int)cols - 1) / kCols);
+    }
+    // The address is a row's, which a wave shares, and 32 bits of a thread's own, made afresh: six tensors' whole addresses kept
+    // over the rows would take twelve registers.
+    template <typename T>
+    __device__ __forceinline__ T *at(const void *base, int64_t row, int64_t ld) const {
+        return (T *)((char *)((T *)base + row * ld) + (uint32_t)afresh(first) * (uint32_t)sizeof(T));
+    }
+    template <typename T>
+    __device__ __forceinline__ Words<T, kCols> get(const void *base, int64_t row, int64_t ld) const {
+        return get_words<T, kCols>(at<T>(base, row, ld));
+    }
+    // with zeros for the columns that are skipped
+    template <typename T>
+    __device__ __forceinline__ Words<T, kCols> get_own(const void *base, int64_t row, int64_t ld) const {
+        Words<T, kCols> w = get<T>(base, row, ld);
+        if (skip) {
+            const Words<T, kCols> v = w;
+            w = Words<T, kCols>::of([&](int e) { return e >= skip ? v[e] : 0.0f; });
+        }
+        return w;
+    }
+    template <typename T>
+    __device__ __forceinline__ void put(void *base, int64_t row, int64_t ld, const Words<T, kCols> &w) const {
+        put_from(at<T>(base, row, ld), skip, w);
+    }
+    __device__ __forceinline__ void parameters_of(const float *p, float none, float (&v)[kCols]) const {
+        if (p) {
+            const auto w = get_words<float, kCols>(p + first);
+#pragma unroll
+            for (int e = 0; e < kCols; e++) v[e] = w[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kCols; e++) v[e] = none;
+        }
+    }
+    // 1 where a column is the thread's own and stays
+    __device__ __forceinline__ void kept(const Args &a, uint64_t offset, int64_t row, float (&keep)[kCols]) const {
+        uint32_t mask = ~0u;
+        if (a.drop.threshold) mask = DropV<kCols>(a.drop, offset, (uint32_t)row, (uint32_t)number * kCols).mask;
+        mask <<= skip;
+#pragma unroll
+        for (int e = 0; e < kCols; e++) keep[e] = mask >> e & 1 ? 1.0f : 0.0f;
+    }
+};
+
+// What is dropped is multiplied by 0 below.  Without a norm of h, whose sums it would be in, a value that is not finite is
+// not to reach anything from there: it is 0 from the start.
+template <typename T>
+__device__ __forceinline__ void drop_first(const Args &a, Words<T, kCols> &h, const float (&keep)[kCols]) {
+    if (a.post != BYZ_NORM_NONE || !a.drop.threshold) return;
+    const Words<T, kCols> v = h;
+    h = Words<T, kCols>::of([&](int e) { return keep[e] != 0.0f ? v[e] : 0.0f; });
+}
+
+// What a block's normalised output is multiplied by on its way into the sum, and the bias on that way: scale, gate, weight and
+// dropout's scale are one factor, for a group of gate's rows.
+template <int TPR, bool GENERAL>
+struct Way {
+    float w[kCols], b[kCols];
+    __device__ __forceinline__ Way() {}
+    __device__ __forceinline__ Way(const Args &a, const Columns<TPR> &mine, int64_t group) {
+        float g[kCols];
+        mine.parameters_of(a.gate ? a.gate + group * a.cols : nullptr, 1.0f, g);
+        mine.parameters_of(a.w1, 1.0f, w);
+        if constexpr (GENERAL) mine.parameters_of(a.b1, 0.0f, b);
+#pragma unroll
+        for (int e = 0; e < kCols; e++) {
+            g[e] *= a.scale * a.drop.scale, w[e] *= g[e];
+            if constexpr (GENERAL) b[e] *= g[e];
+        }
+    }
+    __device__ __forceinline__ float of(int e, float normal) const { return GENERAL ? fmaf(normal, w[e], b[e]) : normal * w[e]; }
+};
+
+// Eight columns of a row to each of TPR threads.  GENERAL: means and biases; without, there are none.
+template <typename T, int TPR, bool GENERAL>
+__global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a) {
+    constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
+    __shared__ float2 lds[2 * TPR / 16];
+    RowJoiner<TPR> join(lds);
+    const Columns<TPR> mine(a.cols);
+    const uint64_t offset = drop_offset(a.drop);
+    const float inv = 1.0f / (float)a.cols;
+    float w2[V], b2[V];
+    mine.parameters_of(a.w2, 1.0f, w2);
+    if constexpr (GENERAL) mine.parameters_of(a.b2, 0.0f, b2);
+    Way<TPR, GENERAL> way;
+    int64_t group_end = 0;
+    for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
+        const Words<T, V> x = mine.template get_own<T>(a.x, row, a.x_ld);
+        Words<T, V> h = {};
+        if (a.h) h = mine.template get_own<T>(a.h, row, a.h_ld);
+        if (row >= group_end) {
+            const int64_t group = row / a.gate_rows;
+            way = Way<TPR, GENERAL>(a, mine, group);
+            group_end = (group + 1) * a.gate_rows;
+        }
+        Stats s;
+        float t[V];
+        // the mean of rows of the layer norm first, then that of the squares about it
+        auto moments = [&](int kind, float &mean, float &rstd, auto value) __attribute__((always_inline)) {
+            float sum = 0.0f;
+            if (GENERAL && kind == BYZ_NORM_LAYER) {
+#pragma unroll
+                for (int e = 0; e < V; e++) sum += value(e);
+                mean = join.sum(sum, 0.0f).x * inv;
+                sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const float d = value(e) - mean;
+                    sum += e >= mine.skip ? d * d : 0.0f;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e++) sum = fmaf(value(e), value(e), sum);
+            }
+            rstd = 1.0f / sqrtf(join.sum(sum, 0.0f).x * inv + a.eps);
+        };
+        if (a.h) {
+            float keep[V];
+            mine.kept(a, offset, row, keep);
+            drop_first(a, h, keep);
+            if (a.post != BYZ_NORM_NONE) moments(a.post, s.mean1, s.rstd1, [&](int e) { return h[e]; });
+#pragma unroll
+            for (int e = 0; e < V; e++)
+                t[e] = fmaf(way.of(e, GENERAL ? (h[e] - s.mean1) * s.rstd1 : h[e] * s.rstd1), keep[e], x[e]);
+            mine.template put<T>(a.out, row, a.out_ld, Words<T, V>::of([&](int e) { return t[e]; }));
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e++) t[e] = x[e];
+        }
+        if (a.pre != BYZ_NORM_NONE) {
+            moments(a.pre, s.mean2, s.rstd2, [&](int e) { return t[e]; });
+            mine.template put<T>(a.y, row, a.y_ld, Words<T, V>::of([&](int e) {
+                                     return GENERAL ? fmaf((t[e] - s.mean2) * s.rstd2, w2[e], b2[e]) : t[e] * s.rstd2 * w2[e];
+                                 }));
+        }
+        if (a.stats && threadIdx.x % TPR == 0) {
+            float *at = a.stats + row * 4;
+            at[0] = s.mean1, at[1] = s.rstd1, at[2] = s.mean2, at[3] = s.rstd2;
+        }
+    }
+}
+
+// dx and dh of a chunk's rows, and the chunk's sums of the columns: a thread has eight columns of every row of its slot, whose
+// sums stay in its registers.  Chunks are those of columns_kernel.  Over a group of gate's rows
+//     A = sum drop(dt) hn,  B = sum drop(dt)   give   dw1 = s g A,  db1 = s g B,  dg = s (w1 A + b1 B).
+template <typename T, int TPR, bool GENERAL>
+__global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
+    constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
+    __shared__ float2 lds[2 * TPR / 16];
+    extern __shared__ float room[];
+    RowJoiner<TPR> join(lds);
+    const Columns<TPR> mine(a.cols);
+    const uint64_t offset = drop_offset(a.drop);
+    const float inv = 1.0f / (float)a.cols;
+    const float inv_a = a.pre == BYZ_NORM_LAYER ? inv : 0.0f, inv_b = a.post == BYZ_NORM_LAYER ? inv : 0.0f;
+    const int slot = slot_of<TPR>();
+    float w2[V], sum_w2[V] = {}, sum_b2[V] = {}, sum_a[V] = {}, sum_b[V] = {};
+    mine.parameters_of(a.w2, 1.0f, w2);
+    Way<TPR, GENERAL> way;
+    struct Loaded {
+        Words<T, V> x, h, dout, dy;
+        Stats s;
+    };
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        Loaded l = {};
+        l.s = stats_of(b.stats, row);
+        if (a.h) l.h = mine.template get<T>(a.h, row, a.h_ld);
+        l.x = mine.template get<T>(a.x, row, a.x_ld);
+        if (b.dy) l.dy = mine.template get_own<T>(b.dy, row, b.dy_ld);
+        if (b.dout) l.dout = mine.template get<T>(b.dout, row, b.dout_ld);
+        return l;
+    };
+    // The row that l has, and the loads of the next one where the registers of most of this one's values are free.
+    auto work = [&](Loaded &l, int64_t row, int64_t next) __attribute__((always_inline)) {
+        const Words<T, V> x = l.x;
+        Words<T, V> h = l.h, dout = l.dout, dy = l.dy;
+        const Stats s = l.s;
+        float keep[V], tn[V];
+        mine.kept(a, offset, row, keep);
+        drop_first(a, h, keep);
+        auto hn = [&](int e) { return GENERAL ? (h[e] - s.mean1) * s.rstd1 : h[e] * s.rstd1; };
+        float p1 = 0.0f, p2 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            const float t = a.h ? fmaf(way.of(e, hn(e)), keep[e], x[e]) : x[e];
+            tn[e] = GENERAL ? (t - s.mean2) * s.rstd2 : t * s.rstd2;
+            const float g = dy[e] * w2[e];
+            if constexpr (GENERAL) p1 += g;
+            p2 = fmaf(g, tn[e], p2);
+        }
+        h.keep(), dout.keep(), dy.keep();  // unpacked again below, which takes fewer registers
+        float mean_a = 0.0f, mean_atn = 0.0f;
+        if (b.dy) {
+            const float2 r = join.sum(p1, p2);
+            mean_a = r.x * inv_a * -s.rstd2, mean_atn = r.y * inv * -s.rstd2;
+        }
+        float dt[V], p3 = 0.0f, p4 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            dt[e] = dout[e];
+            if (b.dy) {
+                dt[e] = fmaf(s.rstd2, dy[e] * w2[e], GENERAL ? dt[e] + mean_a : dt[e]);
+                dt[e] = fmaf(tn[e], mean_atn, dt[e]);
+            }
+            sum_w2[e] = fmaf(dy[e], tn[e], sum_w2[e]);
+            if constexpr (GENERAL) sum_b2[e] += dy[e];
+        }
+        mine.template put<T>(b.dx, row, b.dx_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            const float normal = hn(e), dv = keep[e] * dt[e];
+            sum_a[e] = fmaf(dv, normal, sum_a[e]);
+            if constexpr (GENERAL) sum_b[e] += dv;
+            dt[e] = dv * way.w[e];
+            if constexpr (GENERAL) p3 += dt[e];
+            p4 = fmaf(dt[e], normal, p4);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        l = load(next);
+        if (!a.h) return;
+        if (a.post != BYZ_NORM_NONE) {
+            h.keep();
+            const float2 r = join.sum(p3, p4);
+            const float mean_b = r.x * inv_b * -s.rstd1, mean_bhn = r.y * inv * -s.rstd1;
+#pragma unroll
+            for (int e = 0; e < V; e++) dt[e] = fmaf(hn(e), mean_bhn, GENERAL ? fmaf(s.rstd1, dt[e], mean_b) : s.rstd1 * dt[e]);
+        }
+        mine.template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
+    };
+    // one span of a group's rows for the slots together, or spans of whole groups for each
+    const int64_t chunk = blockIdx.x, group_rows = a.gate_rows;
+    const bool part = b.per_group != 0;
+    int64_t group = part ? chunk / b.per_group : chunk * b.chunk / group_rows + slot;
+    const int64_t first = part ? group * group_rows + chunk % b.per_group * b.chunk + slot : 0;
+    const int64_t end = std::min(a.rows, part ? std::min(first - slot + b.chunk, (group + 1) * group_rows) : (chunk + 1) * b.chunk);
+    float *const own_w1 = room + threadIdx.x * V, *const own_b1 = own_w1 + NT * V;  // over the groups
+    if (!part) {
+#pragma unroll
+        for (int e = 0; e < V; e++) own_w1[e] = own_b1[e] = 0.0f;
+    }
+    // sums of a group's rows to those of its vectors
+    auto close = [&](auto gate_sum, auto w1_sum, auto b1_sum) __attribute__((always_inline)) {
+        float g[V], w1[V], b1[V];
+        mine.parameters_of(a.gate ? a.gate + group * a.cols : nullptr, 1.0f, g);
+        mine.parameters_of(a.w1, 1.0f, w1);
+        mine.parameters_of(a.b1, 0.0f, b1);
+        const float factor = a.scale * a.drop.scale;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            gate_sum(e, factor * (w1[e] * sum_a[e] + (GENERAL ? b1[e] * sum_b[e] : 0.0f)));
+            w1_sum(e, factor * g[e] * sum_a[e]), b1_sum(e, factor * g[e] * sum_b[e]);
+        }
+    };
+    for (int64_t row = part ? first : group * group_rows; row < end; group += SLOTS, row = group * group_rows) {
+        way = Way<TPR, GENERAL>(a, mine, group);
+        const int64_t stop = part ? end : std::min(end, row + group_rows), step = part ? SLOTS : 1;
+        Loaded l = load(row);
+        for (; row < stop; row += step) work(l, row, std::min(row + step, stop - 1));
+        if (part) break;
+        close([&](int e, float v) { if (b.d_gate && e >= mine.skip) b.d_gate[group * a.cols + mine.first + e] = v; },
+              [&](int e, float v) { own_w1[e] += v; }, [&](int e, float v) { own_b1[e] += v; });
+#pragma unroll
+        for (int e = 0; e < V; e++) sum_a[e] = sum_b[e] = 0.0f;
+    }
+    // what the chunk has for each kind, joined over the slots
+    float gate_sum[V], w1_sum[V], b1_sum[V];
+    if (part) {
+        close([&](int e, float v) { gate_sum[e] = v; }, [&](int e, float v) { w1_sum[e] = v; }, [&](int e, float v) { b1_sum[e] = v; });
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) w1_sum[e] = own_w1[e], b1_sum[e] = own_b1[e], gate_sum[e] = 0.0f;
+    }
+    int at = 0;
+#pragma unroll
+    for (int k = 0; k < kKinds; k++) {
+        if (!(b.kinds >> k & 1)) continue;
+        float *to = b.partials + (chunk * __builtin_popcount(b.kinds) + at) * a.cols;
+        at++;
+        if constexpr (SLOTS > 1) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (e >= mine.skip) {
+                const float sum = k == kW2 ? sum_w2[e] : k == kB2 ? sum_b2[e] : k == kW1 ? w1_sum[e] : k == kB1 ? b1_sum[e] : gate_sum[e];
+                if constexpr (SLOTS > 1)
+                    room[slot * (TPR * V) + mine.first + e] = sum;
+                else
+                    to[mine.first + e] = sum;
+            }
+        if constexpr (SLOTS > 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < (int)a.cols; i += NT) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int l = 0; l < SLOTS; l++) sum += room[l * (TPR * V) + i];
+                to[i] = sum;
+            }
+        }
+    }
+}
+
 struct Outputs {
     float *of[kKinds];
 };
 
-// Sums of the chunks' partials: a block 64 columns of one kind (and one group of gate's rows), its waves every fourth chunk.
-__global__ __launch_bounds__(256) void finish_kernel(const float *partials, Outputs out, uint32_t kinds, int64_t cols, int64_t chunks,
-                                                     int64_t per_group, int64_t groups) {
-    __shared__ float lds[4][64];
+// Sums of the chunks' partials: a block 64 columns of one kind (and one group of gate's rows), its sixteen waves every sixteenth
+// chunk.
+__global__ __launch_bounds__(1024) void finish_kernel(const float *partials, Outputs out, uint32_t kinds, int64_t cols, int64_t chunks,
+                                                      int64_t per_group, int64_t groups) {
+    constexpr int W = 16;
+    __shared__ float lds[W][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, count = __builtin_popcount(kinds);
     const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     int kind = 0, left = blockIdx.y;
@@ -338,26 +712,57 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *partials, Outp
     for (int64_t group = blockIdx.z; group < (gate ? groups : 1); group += gridDim.z) {
         const int64_t from = gate ? group * per_group : 0, to = gate ? from + per_group : chunks;
         float sum = 0.0f;
-        if (col < cols)
-            for (int64_t c = from + wave; c < to; c += 4) sum += partials[(c * count + blockIdx.y) * cols + col];
+        if (col < cols) {
+            const float *at = partials + ((from + wave) * count + blockIdx.y) * cols + col;
+            const int64_t step = W * count * cols;
+#pragma unroll 8
+            for (int64_t c = from + wave; c < to; c += W, at += step) sum += *at;
+        }
         __syncthreads();
         lds[wave][lane] = sum;
         __syncthreads();
         if (wave == 0 && col < cols) {
+            sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; w++) sum += lds[w][lane];
             float *to_ = out.of[0];
 #pragma unroll
             for (int k = 1; k < kKinds; k++) to_ = kind == k ? out.of[k] : to_;
-            to_[(gate ? group * cols : 0) + col] = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+            to_[(gate ? group * cols : 0) + col] = sum;
         }
     }
 }
 
-// How the rows are cut for the sums of columns: about 512 chunks, each within a group of gate's rows, or of whole groups where these
-// are short.
+constexpr int64_t kRowsInRegisters = 1024 * kCols;  // columns a block's threads hold
+constexpr int64_t kGroupsInLds = 512 * kCols;        // columns whose sums over short groups of gate's rows are kept in LDS
+bool in_registers(int64_t cols) { return cols >= kCols && cols <= kRowsInRegisters; }
+
+// fn(threads of a row as a constant)
+template <typename F>
+int with_threads(int64_t cols, F fn) {
+    const int64_t threads = (cols + kCols - 1) / kCols;
+    if (threads <= 16) return fn(std::integral_constant<int, 16>{});
+    if (threads <= 32) return fn(std::integral_constant<int, 32>{});
+    if (threads <= 64) return fn(std::integral_constant<int, 64>{});
+    if (threads <= 128) return fn(std::integral_constant<int, 128>{});
+    if (threads <= 256) return fn(std::integral_constant<int, 256>{});
+    if (threads <= 512) return fn(std::integral_constant<int, 512>{});
+    return fn(std::integral_constant<int, 1024>{});
+}
+
+// How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of four rows a slot at least, each
+// within a group of gate's rows, or of whole groups where these are short.
 struct Cut {
     int64_t chunk, per_group, groups, chunks;
-    Cut(int64_t rows, int64_t gate_rows) {
-        const int64_t want = std::max<int64_t>(4, (rows + 511) / 512);
+    Cut(int64_t rows, int64_t cols, int64_t gate_rows) {
+        int64_t blocks = 512, least = 4;
+        if (in_registers(cols))
+            with_threads(cols, [&](auto tpr) -> int {
+                constexpr int NT = block_of<tpr.value>();
+                blocks = kCus * 1024 / NT, least = 4 * (NT / tpr.value);
+                return 0;
+            });
+        const int64_t want = std::max(least, (rows + blocks - 1) / blocks);
         groups = (rows + gate_rows - 1) / gate_rows;
         if (gate_rows >= want) {
             chunk = want, per_group = (gate_rows + chunk - 1) / chunk, chunks = groups * per_group;
@@ -376,11 +781,21 @@ bool sizes_ok(int64_t rows, int64_t cols, int dtype, int64_t gate_rows) {
 size_t rest_bytes(int64_t rows) { return (size_t)rows * 16; }
 
 size_t workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
-    return rows == 0 ? 0 : rest_bytes(rows) + (size_t)Cut(rows, std::min(gate_rows, rows)).chunks * kKinds * (size_t)cols * 4;
+    return rows == 0 ? 0 : rest_bytes(rows) + (size_t)Cut(rows, cols, std::min(gate_rows, rows)).chunks * kKinds * (size_t)cols * 4;
 }
 
 template <typename T>
 int launch_forward(const Args &a, hipStream_t s) {
+    if (in_registers(a.cols)) {
+        const bool general = a.b1 || a.b2 || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
+        return with_threads(a.cols, [&](auto tpr) -> int {
+            constexpr int TPR = tpr.value, NT = block_of<TPR>(), slots = NT / TPR;
+            const int64_t blocks = std::min((a.rows + slots - 1) / slots, (int64_t)kCus * 2048 / NT);
+            (general ? &forward_rows_kernel<T, TPR, true> : &forward_rows_kernel<T, TPR, false>)<<<(unsigned)blocks, NT, 0, s>>>(a);
+            BYZ_HIP(hipGetLastError());
+            return BYZ_OK;
+        });
+    }
     forward_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
@@ -389,14 +804,26 @@ int launch_forward(const Args &a, hipStream_t s) {
 template <typename T>
 int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
-    BYZ_HIP(hipGetLastError());
-    if (!b.kinds && !b.d_gate) return BYZ_OK;
-    columns_kernel<T><<<dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), (unsigned)cut.chunks), 256, 0, s>>>(a, b);
-    BYZ_HIP(hipGetLastError());
+    if (in_registers(a.cols) && (cut.per_group || a.cols <= kGroupsInLds)) {
+        const bool general = a.b1 || (b.kinds & (1u << kB1 | 1u << kB2)) || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
+        const int rc = with_threads(a.cols, [&](auto tpr) -> int {
+            constexpr int TPR = tpr.value, NT = block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
+            const int bytes = !cut.per_group ? 2 * each : NT > TPR ? each : 0;
+            (general ? &backward_rows_kernel<T, TPR, true> : &backward_rows_kernel<T, TPR, false>)<<<(unsigned)cut.chunks, NT, bytes, s>>>(a, b);
+            BYZ_HIP(hipGetLastError());
+            return BYZ_OK;
+        });
+        if (rc != BYZ_OK) return rc;
+    } else {
+        rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
+        BYZ_HIP(hipGetLastError());
+        if (!b.kinds && !b.d_gate) return BYZ_OK;
+        columns_kernel<T><<<dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), (unsigned)cut.chunks), 256, 0, s>>>(a, b);
+        BYZ_HIP(hipGetLastError());
+    }
     if (!b.kinds) return BYZ_OK;
     const unsigned depth = b.kinds >> kGate & 1 ? (unsigned)std::min<int64_t>(cut.groups, 1024) : 1;
-    finish_kernel<<<dim3((unsigned)((a.cols + 63) / 64), (unsigned)__builtin_popcount(b.kinds), depth), 256, 0, s>>>(
+    finish_kernel<<<dim3((unsigned)((a.cols + 63) / 64), (unsigned)__builtin_popcount(b.kinds), depth), 1024, 0, s>>>(
         b.partials, out, b.kinds, a.cols, cut.chunks, cut.per_group, cut.groups);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
@@ -491,7 +918,7 @@ extern "C" int byz_residual_norm_backward(const void *dout, int64_t dout_ld, con
         return BYZ_EINVAL;
     if (!workspace_ || !aligned(workspace_, 16) || workspace_bytes < workspace(rows, cols, a.gate_rows)) return BYZ_ENOMEM;
     a.drop = drop_of(form->p, form->seed, form->offset, form->offset_at, form->first_row);
-    const Cut cut(rows, a.gate_rows);
+    const Cut cut(rows, cols, a.gate_rows);
     Back b{};
     b.dout = dout, b.dout_ld = dout_ld, b.dy = dy, b.dy_ld = dy_ld, b.stats = stats;
     b.dx = dx, b.dx_ld = dx_ld, b.dh = dh, b.dh_ld = dh_ld;
