@@ -1,4 +1,5 @@
-"""Builds libbyzshield.so (HIP kernels + host library + C-ABI) for gfx950, and _worker_calls.so, in-tree."""
+"""Builds libbyzshield.so (HIP kernels + host library + C-ABI) for gfx950, and the Python modules of the worker operators' calls,
+in-tree."""
 import concurrent.futures
 import os
 import subprocess
@@ -21,27 +22,37 @@ OTHER_SOURCES = [os.path.join(CSRC, name) for name in
 
 
 CALLS = os.path.join(PKG, "_worker_calls.so")
+TOKEN_CALLS = os.path.join(PKG, "_token_calls.so")
 
 
 def build_calls(verbose=False):
     """Compiles the Python module of the worker operators' common calls against torch's headers (ten seconds)."""
+    return _build_module(CALLS, "worker_calls.cpp", verbose)
+
+
+def build_token_calls(verbose=False):
+    """The same for the token operators."""
+    return _build_module(TOKEN_CALLS, "token_calls.cpp", verbose)
+
+
+def _build_module(target, source, verbose):
     import sysconfig
 
     import torch
     root = os.path.dirname(torch.__file__)
-    made = CALLS + ".%d.so" % os.getpid()
+    made = target + ".%d.so" % os.getpid()
     cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),
            "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           os.path.join(CSRC, "worker_calls.cpp"), "-o", made, "-L", PKG, "-lbyzshield",
+           os.path.join(CSRC, source), "-o", made, "-L", PKG, "-lbyzshield",
            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
     if verbose:
         print(" ".join(cmd), flush=True)
-    if os.path.exists(CALLS):  # one that is left from before would be used with a library it does not belong to
-        os.remove(CALLS)
+    if os.path.exists(target):  # one that is left from before would be used with a library it does not belong to
+        os.remove(target)
     subprocess.run(cmd, check=True)
-    os.replace(made, CALLS)  # whole, also where several processes build it at once
-    return CALLS
+    os.replace(made, target)  # whole, also where several processes build it at once
+    return target
 
 
 def build(verbose=False):
@@ -82,10 +93,11 @@ def build(verbose=False):
     if verbose:
         print(" ".join(link), flush=True)
     subprocess.run(link, check=True)
-    try:
-        build_calls(verbose)
-    except (ImportError, OSError, subprocess.CalledProcessError) as e:
-        warnings.warn("%s was not built (%s); the binding does without it" % (os.path.basename(CALLS), e), RuntimeWarning)
+    for target, module in ((CALLS, build_calls), (TOKEN_CALLS, build_token_calls)):
+        try:
+            module(verbose)
+        except (ImportError, OSError, subprocess.CalledProcessError) as e:
+            warnings.warn("%s was not built (%s); the binding does without it" % (os.path.basename(target), e), RuntimeWarning)
     return LIB
 
 

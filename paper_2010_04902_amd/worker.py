@@ -38,16 +38,16 @@ class _NoCalls:
         return lambda *args: None
 
 
-def _load_calls():
-    """csrc/worker_calls.cpp's module; built once where it is missing or made for another torch, and done without, with a
-    warning, where that fails."""
+def _load_calls(name="_worker_calls", builder="build_calls"):
+    """csrc/worker_calls.cpp's module, or that of another name; built once where it is missing or made for another torch, and
+    done without, with a warning, where that fails."""
     for build in (False, True):
         try:
             if build:
                 from . import build as _build
-                _build.build_calls()
+                getattr(_build, builder)()
                 importlib.invalidate_caches()
-            return importlib.import_module("._worker_calls", __package__)
+            return importlib.import_module("." + name, __package__)
         except (ImportError, OSError, subprocess.CalledProcessError) as e:
             reason = e
     warnings.warn("the worker operators' native module is not there (%s): small calls take about twice the host's time" % reason,

@@ -15,6 +15,7 @@ BYZ_NORMS = {"none": BYZ_NORM_NONE, "rms": BYZ_NORM_RMS, "layer": BYZ_NORM_LAYER
 _WORD = 2 ** 64 - 1
 
 _lib = None
+_calls = None
 _torch = None
 
 
@@ -42,11 +43,12 @@ class byz_residual_form(ctypes.Structure):
 
 
 def _load():
-    global _lib, _torch
+    global _lib, _calls, _torch
     if _lib is not None:
         return _lib
     L = _w._load()
-    _torch = _w._torch
+    _torch, _calls = _w._torch, _w._load_calls("_token_calls", "build_token_calls")
+    _calls.use_form(byz_residual_form)
     vp, c_int, i64, u64, sz, f32 = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t,
                                     ctypes.c_float)
     form = ctypes.POINTER(byz_residual_form)
@@ -113,6 +115,10 @@ def byz_dropout(x, p, seed, offset=0, offset_at=None, first_row=0, out=None, str
     the GPU, for captured calls), first_row + the row, and the column, and on nothing else.  out may be x."""
     if _lib is None:
         _load()
+    if out is None and stream is None and offset_at is None:
+        done = _calls.dropout(x, p, seed, offset, first_row)
+        if done is not None:
+            return _w._done(done, "byz_dropout")
     _w._outside_the_graph(x)
     rows, cols, ld = _w._matrix(x, "x")
     index, dtype = _w._device(x, "x"), _w._dtype(x, "x")
@@ -165,6 +171,11 @@ def byz_residual_norm(x, h, form, post_weight=None, post_bias=None, gate=None, p
     h None: y = norm_pre(x) alone, and out is x.  out may be x or h (the backward call needs both)."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.residual_norm(x, h, form, post_weight, post_bias, gate, pre_weight, pre_bias)
+        if done is not None:
+            total, y, stats = _w._done(done, "byz_residual_norm")
+            return x if h is None else total, y, stats
     _w._outside_the_graph(x, h, post_weight, post_bias, gate, pre_weight, pre_bias)
     rows, cols, x_ld = _w._matrix(x, "x")
     index, dtype = _w._device(x, "x"), _w._dtype(x, "x")
@@ -194,6 +205,11 @@ def byz_residual_norm_backward(dout, dy, x, h, stats, form, post_weight=None, po
     A vector that was None has no gradient; parameters=False: none of them has.  dh is None without h."""
     if _lib is None:
         _load()
+    if stream is None and parameters:
+        done = _calls.residual_norm_backward(dout, dy, stats, x, h, form, post_weight, post_bias, gate, pre_weight, pre_bias)
+        if done is not None:
+            done = _w._done(done, "byz_residual_norm_backward")
+            return done[0], done[1], done[2:]
     rows, cols, x_ld = _w._matrix(x, "x")
     index, dtype = _w._device(x, "x"), _w._dtype(x, "x")
     device, empty = x.device, _empties(stream)
@@ -257,6 +273,10 @@ def byz_token_logp(logits, label, temperature=1.0, stream=None):
     logits [rows, vocab] float32, bfloat16 or float16; label int32 [rows], negative where there is no token: logp 0."""
     if _lib is None:
         _load()
+    if stream is None:
+        done = _calls.token_logp(logits, label, temperature)
+        if done is not None:
+            return _w._done(done, "byz_token_logp")
     _w._outside_the_graph(logits)
     r = _Rows(logits, label, stream)
     logp, stats = r.results(r.rows, (r.rows, 2))
@@ -268,6 +288,10 @@ def byz_token_logp_backward(dlogp, logits, label, stats, temperature=1.0, out=No
     """-> dlogits (type of logits) for dlogp[rows] float32, from byz_token_logp's stats.  out may be logits."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.token_logp_backward(logits, label, dlogp, stats, temperature)
+        if done is not None:
+            return _w._done(done, "byz_token_logp_backward")
     r = _Rows(logits, label, stream)
     d, s = r.floats(dlogp, "dlogp"), _w._floats(stats, (r.rows, 2), "stats", r.index)
     out, ld = r.gradient(out, logits)
@@ -282,7 +306,11 @@ def byz_policy_loss(logits, label, old, advantage, ref=None, clip_low=0.2, clip_
     the reference model; None if kl is 0): float32 [rows]."""
     if _lib is None:
         _load()
-    _w._outside_the_graph(logits)
+    if stream is None:
+        done = _calls.policy_loss(logits, label, old, advantage, ref, clip_low, clip_high, kl, temperature)
+        if done is not None:
+            return _w._done(done, "byz_policy_loss")
+    _w._outside_the_graph(logits, old, advantage, ref)
     r = _Rows(logits, label, stream)
     o, a, f = r.floats(old, "old"), r.floats(advantage, "advantage"), r.floats(ref, "ref")
     loss, logp, stats = r.results(r.rows, r.rows, (r.rows, 2))
@@ -296,6 +324,10 @@ def byz_policy_loss_backward(dloss, logits, label, old, advantage, stats, ref=No
     """-> dlogits (type of logits) for dloss[rows] float32, from byz_policy_loss' stats.  out may be logits."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.policy_loss_backward(logits, label, old, advantage, ref, clip_low, clip_high, kl, temperature, dloss, stats)
+        if done is not None:
+            return _w._done(done, "byz_policy_loss_backward")
     r = _Rows(logits, label, stream)
     d, o, a, f = r.floats(dloss, "dloss"), r.floats(old, "old"), r.floats(advantage, "advantage"), r.floats(ref, "ref")
     s = _w._floats(stats, (r.rows, 2), "stats", r.index)
@@ -311,6 +343,10 @@ def byz_policy_loss_step(logits, label, old, advantage, dloss, ref=None, clip_lo
     -> (loss[rows] float32, logp[rows] float32, dlogits).  out (dlogits) may be logits."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.policy_loss_step(logits, label, old, advantage, ref, clip_low, clip_high, kl, temperature, dloss)
+        if done is not None:
+            return _w._done(done, "byz_policy_loss_step")
     r = _Rows(logits, label, stream)
     d, o, a, f = r.floats(dloss, "dloss"), r.floats(old, "old"), r.floats(advantage, "advantage"), r.floats(ref, "ref")
     out, ld = r.gradient(out, logits)
@@ -334,7 +370,11 @@ def byz_preference_loss(logits, label, bounds, ref=None, beta=0.1, smoothing=0.0
     sequences 2 i and 2 i + 1 are pair i's chosen and rejected one.  ref: the reference model's sums, float32 [2 * pairs]."""
     if _lib is None:
         _load()
-    _w._outside_the_graph(logits)
+    if stream is None:
+        done = _calls.preference_loss(logits, label, bounds, ref, beta, smoothing, temperature)
+        if done is not None:
+            return _w._done(done, "byz_preference_loss")
+    _w._outside_the_graph(logits, ref)
     r = _Rows(logits, label, stream)
     at, pairs = _pairs(bounds, r)
     f = r.floats(ref, "ref", 2 * pairs)
@@ -348,6 +388,10 @@ def byz_preference_loss_backward(dloss, logits, label, bounds, slope, stats, bet
     """-> dlogits (type of logits) for dloss[pairs] float32, from byz_preference_loss' slope and stats.  out may be logits."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.preference_loss_backward(logits, label, bounds, dloss, slope, stats, beta, temperature)
+        if done is not None:
+            return _w._done(done, "byz_preference_loss_backward")
     r = _Rows(logits, label, stream)
     at, pairs = _pairs(bounds, r)
     d, l = r.floats(dloss, "dloss", pairs), r.floats(slope, "slope", pairs)
@@ -364,6 +408,10 @@ def byz_preference_loss_step(logits, label, bounds, dloss, ref=None, beta=0.1, s
     -> (loss[pairs] float32, sums[2 * pairs] float32, dlogits).  out (dlogits) may be logits."""
     if _lib is None:
         _load()
+    if out is None and stream is None:
+        done = _calls.preference_loss_step(logits, label, bounds, dloss, ref, beta, smoothing, temperature)
+        if done is not None:
+            return _w._done(done, "byz_preference_loss_step")
     r = _Rows(logits, label, stream)
     at, pairs = _pairs(bounds, r)
     d, f = r.floats(dloss, "dloss", pairs), r.floats(ref, "ref", 2 * pairs)
