@@ -45,6 +45,7 @@ struct Args {
     // workspace
     Terms *terms;
     double *logp64;
+    float2 *parts;
 };
 
 // log(s) of a sum in fp32, to 2^-24 or 2^-24 of itself; 0 for an empty row's sum
@@ -157,6 +158,51 @@ __global__ __launch_bounds__(NT) void rows_kernel(Args a) {
     }
 }
 
+// Few long rows: `parts` blocks a row, whose maxima and sums join_kernel joins.
+template <typename T>
+__global__ __launch_bounds__(256) void parts_kernel(Args a, int64_t each) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ double red[8];
+    const float c = (float)(1.4426950408889634 / (double)a.temperature);
+    const int64_t row = blockIdx.y, part = blockIdx.x;
+    if (a.label[row] < 0) return;
+    const Row<T> r(a.logits, row, a.ld, a.vocab);
+    RunningSum s;
+    if (part == gridDim.x - 1 && (int)threadIdx.x < r.tail) {
+        const float x[1] = {(float)r.at[r.edge(threadIdx.x)]};
+        s.add(x, c);
+    }
+    const int64_t to = std::min(r.vectors, (part + 1) * each);
+#pragma unroll 4
+    for (int64_t i = part * each + threadIdx.x; i < to; i += 256) {
+        const Words<T, V> v = r.vector(i);
+        float x[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) x[e] = v[e];
+        s.add(x, c);
+    }
+    s = row_join<256>(s, c, red);
+    if (threadIdx.x == 0) a.parts[row * gridDim.x + part] = make_float2(s.m, s.s);
+}
+
+template <typename T>
+__global__ __launch_bounds__(64) void join_kernel(Args a, int parts) {
+    const float c = (float)(1.4426950408889634 / (double)a.temperature);
+    const int64_t row = blockIdx.x;
+    const int32_t label = a.label[row];
+    RunningSum s;
+    float z = 0.0f;
+    if (label >= 0) {
+        if (label < a.vocab) z = (float)((const T *)a.logits)[row * a.ld + label];
+        if ((int)threadIdx.x < parts) {
+            const float2 p = a.parts[row * parts + threadIdx.x];
+            s.m = p.x, s.s = p.y;
+        }
+        s = wave_join(s, c);
+    }
+    if (threadIdx.x == 0) finish(a, row, label, s.m, s.s, z);
+}
+
 // What a gradient's own call needs of its rows.
 template <typename T>
 __global__ __launch_bounds__(256) void terms_kernel(Args a) {
@@ -225,29 +271,33 @@ __global__ __launch_bounds__(256) void pairs_kernel(Args a) {
     }
 }
 
-// The dense gradient: `parts` blocks a row.  Rows without a token or weight are not read.
-template <typename T>
+// The dense gradient: `parts` blocks a row, or a wave each of short rows.  Rows without a token or weight are not read.  The last rows
+// come first: they were read for their sums last, the caches still have some of them, and the results go past these.  us, so /
+// with results in the caches and the first rows first: preference step on 8192 x 20000 bf16 171 / 195, on 1000 x 200000 192 / 236.
+template <typename T, int NT>
 __global__ __launch_bounds__(256) void gradient_kernel(Args a, int64_t parts, int64_t each) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), SLOTS = 256 / NT;
     const int64_t total = a.rows * parts;
-    for (int64_t block = blockIdx.x; block < total; block += gridDim.x) {
-        const int64_t row = block / parts, part = block - row * parts;
+    const int slot = SLOTS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, tid = threadIdx.x % NT;
+    for (int64_t unit = (int64_t)blockIdx.x * SLOTS + slot; unit < total; unit += (int64_t)gridDim.x * SLOTS) {
+        const int64_t row = a.rows - 1 - unit / parts, part = unit % parts;
         const Terms t = a.terms[row];
         const Row<T> r(a.logits, row, a.ld, a.vocab);
         T *out = (T *)a.dlogits + row * a.dlogits_ld;
         const int64_t from = part * each, to = std::min(r.vectors, from + each);
-        const bool last = part == parts - 1 && (int)threadIdx.x < r.tail;
-        const int64_t edge = r.edge(threadIdx.x);
+        const bool last = part == parts - 1 && tid < r.tail;
+        const int64_t edge = r.edge(tid);
         if (t.w == 0.0f) {
-            for (int64_t i = from + threadIdx.x; i < to; i += 256) put_words(out + i * V, Words<T, V>::of([](int) { return 0.0f; }));
+            for (int64_t i = from + tid; i < to; i += NT) put_words(out + i * V, Words<T, V>::of([](int) { return 0.0f; }));
             if (last) out[edge] = (T)0.0f;
             continue;
         }
         const Softmax<T> q((double)t.m, (double)t.log_sum, (double)a.temperature, -t.w);
         auto write = [&](auto odd) {
-            for (int64_t i = from + threadIdx.x; i < to; i += 256) {
+            for (int64_t i = from + tid; i < to; i += NT) {
                 const Words<T, V> v = r.template vector_of<odd.value>(i);
-                put_words(out + i * V, Words<T, V>::of([&](int e) { return q.weighted(v[e]); }));
+                const Words<T, V> d = Words<T, V>::of([&](int e) { return q.weighted(v[e]); });
+                put_past_caches(out + i * V, d);
                 const int64_t at = t.label - i * V;
                 if (at >= 0 && at < V) {
                     float x = 0.0f;
@@ -268,23 +318,283 @@ __global__ __launch_bounds__(256) void gradient_kernel(Args a, int64_t parts, in
     }
 }
 
+// The same weight in fp32 from a row's sum, for results of 16 bits: good to some 2^-20 of the terms it is made of, where a
+// result has 2^-9 or 2^-12, and a tenth of the instructions.
+__device__ __forceinline__ float policy_slope(const Args &a, int64_t row, float m, float sum, float z) {
+    const float advantage = a.advantage[row], log2e = 1.44269504f;
+    const float logp = (z - m) / a.temperature - __builtin_amdgcn_logf(sum) * 0.69314718f;
+    const float r = __builtin_amdgcn_exp2f((logp - a.old[row]) * log2e);
+    const bool above = advantage >= 0.0f && r > a.high, below = !(advantage >= 0.0f) && r < a.low;
+    float slope = above || below ? 0.0f * advantage : -advantage * r;
+    if (a.kl != 0.0f) slope -= a.kl * (__builtin_amdgcn_exp2f((a.ref[row] - logp) * log2e) - 1.0f);
+    return slope;
+}
+
+// A row in the registers of NT threads, R vectors of 16 bytes each, so that it is read once: its maximum and sum, and with STEP the
+// gradient of the policy loss.  A block of 1024 threads has a compute unit for itself: as soon as a thread has stored a piece
+// of its gradient it loads that piece of its next row, so reads, exponentials and writes overlap, and what the losses are
+// made of is left to losses_kernel.  Smaller blocks share a compute unit, and overlap one another; short rows are a wave's, four to
+// a block.  ODD: rows of 16-bit values may start at odd multiples of two bytes.
+template <typename T, int NT, int R, bool STEP, bool ODD>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args a) {
+    constexpr int V = 16 / sizeof(T), SLOTS = NT == 64 ? 4 : 1;
+    constexpr bool kAlone = NT == 1024;
+    static_assert(STEP || !kAlone, "");
+    __shared__ double red[32];
+    const int tid = threadIdx.x % NT;
+    const float c = (float)(1.4426950408889634 / (double)a.temperature);
+    Words<T, V> x[R];
+    word_t next_word[ODD ? R : 1];
+    T edge = (T)0.0f;
+    // A row here is shorter than 2^31 bytes.  A thread's number is made afresh for each use, or the places of all R vectors would be
+    // kept in registers; threads without a v-th vector load the last, without a branch, and leave it.
+    auto vector_at = [](auto *base, int number) { return base + (uint32_t)number * (uint32_t)V; };
+    // Of an odd row x has the words that hold the values but for the last value's; shifted where the row is begun.
+    auto load = [&](const Row<T> &r, int own, int v) __attribute__((always_inline)) {
+        const T *from = vector_at(r.at - (ODD && r.odd() ? 1 : 0), std::max(0, std::min(own + v * NT, (int)r.vectors - 1)));
+        x[v] = get_words<T, V>(from);
+        if constexpr (ODD)
+            if (r.odd()) next_word[v] = *(const word_t *)(from + V);
+    };
+    auto load_row = [&](int64_t row) __attribute__((always_inline)) {
+        if (row >= a.rows || a.label[row] < 0) return;
+        const Row<T> r(a.logits, row, a.ld, a.vocab);
+        const int own = afresh(tid);
+        if (NT > 64 || r.vectors > 0) {  // there are none in a row shorter than one
+#pragma unroll
+            for (int v = 0; v < R; v++) load(r, own, v);
+        }
+        if (tid < r.tail) edge = r.at[r.edge(tid)];
+    };
+    if constexpr (kAlone) load_row(blockIdx.x);
+    const int slot = SLOTS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot; row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
+        const int32_t label = a.label[row];
+        if constexpr (!kAlone) load_row(row);
+        const Row<T> r(a.logits, row, a.ld, a.vocab);
+        const int vectors = (int)r.vectors;
+        const bool has_edge = tid < r.tail;
+        float z = 0.0f, w = 0.0f;
+        RunningSum s;
+        if (label >= 0) {
+            if (label < a.vocab) z = (float)r.at[label];
+            if constexpr (ODD)
+                if (r.odd())
+#pragma unroll
+                    for (int v = 0; v < R; v++) x[v] = shifted(x[v], next_word[v]);
+            // A thread's sum of exp2((x - m) c).  The maximum of its first values is m.  The row's sum of NT such sums has to stay
+            // below fp32's 2^128, so what reaches 2^117 (or is not finite) is summed again from the maximum of all.
+            if (tid < vectors) {
+                float top = x[0][0];
+#pragma unroll
+                for (int e = 1; e < V; e++) top = fmaxf(top, x[0][e]);
+                s.m = top;
+            } else if (has_edge) {
+                s.m = (float)edge;
+            }
+            const int own = afresh(tid);
+            auto add_up = [&](float m) __attribute__((always_inline)) {
+                float all = 0.0f;
+#pragma unroll
+                for (int v = 0; v < R; v++) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum += __builtin_amdgcn_exp2f((x[v][e] - m) * c);
+                    all += own + v * NT < vectors ? sum : 0.0f;
+                    x[v].keep();
+                    __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
+                }
+                return has_edge ? all + __builtin_amdgcn_exp2f(((float)edge - m) * c) : all;
+            };
+            s.s = add_up(s.m);
+            if (!(s.s < 0x1p117f)) {
+                float top = has_edge ? fmaxf((float)edge, -INFINITY) : -INFINITY;
+#pragma unroll
+                for (int v = 0; v < R; v++) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) top = own + v * NT < vectors ? fmaxf(top, x[v][e]) : top;
+                    x[v].keep();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                s.m = top;
+                // nothing but -inf (or NaN, which has to stay) adds up to 0
+                s.s = add_up(s.m == -INFINITY ? 0.0f : s.m);
+            }
+            s = row_join<NT>(s, c, red);
+        }
+        if constexpr (kAlone) {
+            if (tid == 0) a.terms[row] = Terms{s.m, s.s, z, label};
+            if (label >= 0) {
+                if (s.m == -INFINITY) s.m = 0.0f;
+                if constexpr (sizeof(T) == 2) {
+                    const float sum = s.s == 0.0f ? 1.0f : s.s;  // of a row without anything
+                    w = label >= a.vocab ? NAN : a.dloss[row] * policy_slope(a, row, s.m, sum, z) / a.temperature;
+                } else {
+                    double loss, slope;
+                    policy(a, row, ((double)z - (double)s.m) / (double)a.temperature - log_of(s.s), loss, slope);
+                    w = label >= a.vocab ? NAN : (float)((double)a.dloss[row] * slope / (double)a.temperature);
+                }
+            }
+        } else if constexpr (NT == 64) {
+            if (tid == 0) w = finish(a, row, label, s.m, s.s, z).w;
+            w = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, w)));
+            if (s.m == -INFINITY) s.m = 0.0f;
+        } else {
+            __syncthreads();
+            Terms *const shared = reinterpret_cast<Terms *>(red + 16);
+            if (tid == 0) *shared = finish(a, row, label, s.m, s.s, z);
+            __syncthreads();
+            w = shared->w;
+            if (s.m == -INFINITY) s.m = 0.0f;
+        }
+        if constexpr (!STEP) continue;
+        T *out = (T *)a.dlogits + row * a.dlogits_ld;
+        const Softmax<T> q(s.m, s.s == 0.0f ? 1.0f : s.s, a.temperature, -w, c);
+        const int64_t ahead = row + gridDim.x;
+        const bool more = kAlone && ahead < a.rows && a.label[ahead] >= 0;
+        const Row<T> next(a.logits, more ? ahead : row, a.ld, a.vocab);
+        if (has_edge) {
+            const int64_t at = r.edge(tid);
+            out[at] = w == 0.0f ? (T)0.0f : round_to<T>(at == label ? q.less((float)edge, 1.0f) : q.weighted((float)edge));
+            if (more) edge = next.at[next.edge(tid)];
+        }
+        const int then = afresh(tid);
+        auto put_result = [](T *to, const Words<T, V> &v) {
+            if constexpr (NT == 64)
+                put_words(to, v);
+            else
+                put_past_caches(to, v);
+        };
+        const int own_label = (uint32_t)(label / V) % NT == (uint32_t)tid ? label / V / NT : -1;  // which of the thread's vectors has it
+        auto pass = [&](auto some, auto loads) __attribute__((always_inline)) {
+#pragma unroll
+            for (int v = 0; v < R; v++) {
+                if (then + v * NT < vectors) {
+                    T *const to = vector_at(out, then + v * NT);
+                    put_result(to, Words<T, V>::of([&](int e) { return some.value ? q.weighted(x[v][e]) : 0.0f; }));
+                    if (some.value && v == own_label) to[label % V] = round_to<T>(q.less(z, 1.0f));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (loads.value) {
+                    load(next, then, v);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
+        if (more) {
+            if (w == 0.0f)
+                pass(std::false_type{}, std::true_type{});
+            else
+                pass(std::true_type{}, std::true_type{});
+        } else if (w == 0.0f) {
+            pass(std::false_type{}, std::false_type{});
+        } else {
+            pass(std::true_type{}, std::false_type{});
+        }
+    }
+}
+
+// The losses of rows whose maxima and sums held_rows_kernel has left.
+__global__ __launch_bounds__(256) void losses_kernel(Args a) {
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= a.rows) return;
+    const Terms t = a.terms[row];
+    Args only = a;
+    only.dloss = nullptr, only.terms = nullptr;
+    finish(only, row, t.label, t.m, t.log_sum, t.w);
+}
+
 // ------------------------------------------------------------------ launches
 
+constexpr int kCus = 256;  // compute units
+
+template <typename T>
+int64_t vectors_of(int64_t vocab) {
+    return vocab * (int64_t)sizeof(T) / 16;
+}
+
+// Whether rows of 16-bit values may start at odd multiples of two bytes.
+template <typename T>
+bool may_be_odd(const Args &a) {
+    return sizeof(T) == 2 && (((uintptr_t)a.logits & 2) || (a.ld & 1));
+}
+
+template <typename T, int NT, int R, bool STEP>
+int launch_held(const Args &a, hipStream_t s) {
+    constexpr int slots = NT == 64 ? 4 : 1;
+    const unsigned grid = (unsigned)std::min((a.rows + slots - 1) / slots, NT == 1024 ? (int64_t)kCus : kMaxGrid);
+    if (may_be_odd<T>(a)) {
+        if constexpr (sizeof(T) == 2) held_rows_kernel<T, NT, R, STEP, true><<<grid, NT * slots, 0, s>>>(a);
+    } else {
+        held_rows_kernel<T, NT, R, STEP, false><<<grid, NT * slots, 0, s>>>(a);
+    }
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+// The policy loss' step of rows that registers hold; of more than 128 KB where there is one for every other compute unit at least.
+// Blocks of 1024 threads were slower up to there: 8192 x 50000 bf16 370 us for 331 in blocks of 512.
+template <typename T>
+bool step_is_held(const Args &a) {
+    return vectors_of<T>(a.vocab) <= 512 * 16 || (vectors_of<T>(a.vocab) <= 1024 * 16 && a.rows >= kCus / 2);
+}
+
+template <typename T>
+int launch_step(const Args &a, hipStream_t s) {
+    const int64_t vectors = vectors_of<T>(a.vocab);
+    if (vectors <= 64 * 4) return launch_held<T, 64, 4, true>(a, s);
+    if (vectors <= 64 * 16) return launch_held<T, 64, 16, true>(a, s);
+    if (vectors <= 256 * 8) return launch_held<T, 256, 8, true>(a, s);
+    if (vectors <= 256 * 16) return launch_held<T, 256, 16, true>(a, s);
+    if (vectors <= 512 * 16) return launch_held<T, 512, 16, true>(a, s);
+    const int rc = launch_held<T, 1024, 16, true>(a, s);
+    if (rc != BYZ_OK) return rc;
+    losses_kernel<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a);
+    BYZ_HIP(hipGetLastError());
+    return BYZ_OK;
+}
+
+// Blocks of a row: of few rows of 256 KB and more, so many that there are some for every compute unit, each with 16 KB at least.
+int64_t row_parts(int64_t rows, int64_t vectors) {
+    if (rows >= kCus / 2 || vectors < 16384) return 1;
+    return std::min<int64_t>({64, vectors / 1024, (2 * kCus + rows - 1) / rows});
+}
+
 size_t terms_bytes(int64_t rows) { return (size_t)rows * sizeof(Terms); }
-size_t workspace_of(int64_t rows) { return terms_bytes(rows) + (size_t)rows * sizeof(double); }
+size_t workspace_of(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t parts = row_parts(rows, vocab * (int64_t)dtype_size(dtype) / 16);
+    return terms_bytes(rows) + (size_t)rows * sizeof(double) + (parts > 1 ? (size_t)(rows * parts) * sizeof(float2) : 0);
+}
 
 template <typename T>
 int launch_rows(const Args &a, hipStream_t s) {
-    rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
+    const int64_t vectors = vectors_of<T>(a.vocab), parts = row_parts(a.rows, vectors);
+    if (vectors <= 64 * 4) return launch_held<T, 64, 4, false>(a, s);
+    if (vectors <= 64 * 16) return launch_held<T, 64, 16, false>(a, s);
+    if (parts > 1) {
+        parts_kernel<T><<<dim3((unsigned)parts, (unsigned)a.rows), 256, 0, s>>>(a, (vectors + parts - 1) / parts);
+        BYZ_HIP(hipGetLastError());
+        join_kernel<T><<<(unsigned)a.rows, 64, 0, s>>>(a, (int)parts);
+        BYZ_HIP(hipGetLastError());
+        return BYZ_OK;
+    }
+    if (a.rows < kCus / 2)
+        rows_kernel<T, 1024><<<(unsigned)a.rows, 1024, 0, s>>>(a);
+    else
+        rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
 
 template <typename T>
 int launch_gradient(const Args &a, hipStream_t s) {
-    const int64_t vectors = a.vocab * (int64_t)sizeof(T) / 16, each = 1024;
-    const int64_t parts = std::max<int64_t>(1, (vectors + each - 1) / each);
-    gradient_kernel<T><<<(unsigned)std::min(a.rows * parts, kMaxGrid), 256, 0, s>>>(a, parts, each);
+    const int64_t vectors = vectors_of<T>(a.vocab), each = 1024;
+    if (vectors <= 256) {
+        gradient_kernel<T, 64><<<(unsigned)std::min((a.rows + 3) / 4, kMaxGrid), 256, 0, s>>>(a, 1, vectors);
+    } else {
+        const int64_t parts = (vectors + each - 1) / each;
+        gradient_kernel<T, 256><<<(unsigned)std::min(a.rows * parts, kMaxGrid), 256, 0, s>>>(a, parts, each);
+    }
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -307,6 +617,7 @@ int launch_pairs(const Args &a, hipStream_t s) {
 template <typename T>
 int launch_all(const Args &a, hipStream_t s) {
     int rc = BYZ_OK;
+    if (a.rows && a.kind == kPolicy && a.dlogits && !a.given_stats && step_is_held<T>(a)) return launch_step<T>(a, s);
     if (a.rows) rc = a.given_stats ? launch_terms<T>(a, s) : launch_rows<T>(a, s);
     if (rc == BYZ_OK && a.kind == kPreference && !a.given_stats) rc = launch_pairs(a, s);
     if (rc == BYZ_OK && a.rows && a.dlogits) rc = launch_gradient<T>(a, s);
@@ -340,9 +651,10 @@ int check(Args &a, int dtype, bool gradient, void *workspace, size_t bytes) {
     if (gradient && (!a.dlogits || !a.dloss || !floats_ok(a.dloss) || !aligned(a.dlogits, dtype_size(dtype)) || a.dlogits_ld < a.vocab ||
                      !extent_ok(a.rows, a.dlogits_ld, a.vocab)))
         return BYZ_EINVAL;
-    if (!workspace || !aligned(workspace, 16) || bytes < workspace_of(a.rows)) return BYZ_ENOMEM;
+    if (!workspace || !aligned(workspace, 16) || bytes < workspace_of(a.rows, a.vocab, dtype)) return BYZ_ENOMEM;
     a.terms = (Terms *)workspace;
     a.logp64 = (double *)((char *)workspace + terms_bytes(a.rows));
+    a.parts = (float2 *)(a.logp64 + a.rows);
     return BYZ_OK;
 }
 
@@ -365,7 +677,7 @@ void set_preference(Args &a, const int32_t *bounds, int64_t pairs, const float *
 }  // namespace
 
 extern "C" size_t byz_token_loss_workspace_bytes(int64_t rows, int64_t vocab, int dtype) {
-    return sizes_ok(rows, vocab, dtype) ? workspace_of(rows) : 0;
+    return sizes_ok(rows, vocab, dtype) ? workspace_of(rows, vocab, dtype) : 0;
 }
 
 extern "C" int byz_token_logp(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int32_t *label,
