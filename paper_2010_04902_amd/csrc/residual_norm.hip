@@ -41,8 +41,7 @@ struct Back {
     float *partials;  // [chunk][kind][column]
     float *d_gate;
     uint32_t kinds;     // bit k: kind k is wanted
-    int64_t chunk;      // rows a block sums
-    int64_t per_group;  // chunks of a gate's rows; 0: a chunk has whole groups
+    int64_t chunks, per_group;  // per_group: of a group of gate's rows; 0: a chunk has whole groups
 };
 enum { kW2, kB2, kW1, kB1, kGate, kKinds };
 
@@ -263,8 +262,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(Args a, Back b) {
     }
 }
 
-// Sums over a chunk's rows, four waves with a row each in turn and 64 V columns a wave.  A chunk lies in one group of gate's rows
-// (per_group chunks of it), or has whole groups, which a wave takes whole: their d_gate is written here.
+// Sums over a chunk's rows, four waves with a row each in turn and 64 V columns a wave.  A group of gate's rows is dealt out to
+// per_group chunks, row by row, so that the chunks are at neighbouring rows at any time (with runs of neighbouring rows for each they would
+// be a power of two apart, in a few of the memory's channels); or a chunk has whole groups, which a wave takes whole: their
+// d_gate is written here.
 template <typename T>
 __global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
     constexpr int V = 16 / sizeof(T), W = 4;
@@ -288,12 +289,11 @@ __global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
         }
     };
     if (b.per_group) {
-        const int64_t group = chunk / b.per_group, start = group * group_rows + chunk % b.per_group * b.chunk;
-        const int64_t end = std::min({start + b.chunk, (group + 1) * group_rows, a.rows});
-        for (int64_t row = start + wave; row < end; row += W) add(row);
+        const int64_t group = chunk / b.per_group, end = std::min((group + 1) * group_rows, a.rows);
+        for (int64_t row = group * group_rows + chunk % b.per_group * W + wave; row < end; row += b.per_group * W) add(row);
     } else {
-        const int64_t end = std::min(a.rows, (chunk + 1) * b.chunk);
-        for (int64_t start = chunk * b.chunk + wave * group_rows; start < end; start += W * group_rows) {
+        for (int64_t start = (chunk * W + wave) * group_rows; start < a.rows; start += b.chunks * W * group_rows) {
+            const int64_t end = a.rows;
             for (int64_t row = start; row < std::min(end, start + group_rows); row++) add(row);
 #pragma unroll
             for (int e = 0; e < V; e++) {
@@ -399,15 +399,12 @@ struct Columns {
     __device__ __forceinline__ Words<T, kCols> get(const void *base, int64_t row, int64_t ld) const {
         return get_words<T, kCols>(at<T>(base, row, ld));
     }
-    // with zeros for the columns that are skipped
+    // zeros for the columns that are skipped
     template <typename T>
-    __device__ __forceinline__ Words<T, kCols> get_own(const void *base, int64_t row, int64_t ld) const {
-        Words<T, kCols> w = get<T>(base, row, ld);
-        if (skip) {
-            const Words<T, kCols> v = w;
-            w = Words<T, kCols>::of([&](int e) { return e >= skip ? v[e] : 0.0f; });
-        }
-        return w;
+    __device__ __forceinline__ void only_own(Words<T, kCols> &w) const {
+        if (skip == 0) return;
+        const Words<T, kCols> v = w;
+        w = Words<T, kCols>::of([&](int e) { return e >= skip ? v[e] : 0.0f; });
     }
     template <typename T>
     __device__ __forceinline__ void put(void *base, int64_t row, int64_t ld, const Words<T, kCols> &w) const {
@@ -425,11 +422,25 @@ struct Columns {
     }
     // 1 where a column is the thread's own and stays
     __device__ __forceinline__ void kept(const Args &a, uint64_t offset, int64_t row, float (&keep)[kCols]) const {
-        uint32_t mask = ~0u;
-        if (a.drop.threshold) mask = DropV<kCols>(a.drop, offset, (uint32_t)row, (uint32_t)number * kCols).mask;
-        mask <<= skip;
+        if (a.drop.threshold) {
+            const Drop8 r(a.drop, offset, (uint32_t)row, (uint32_t)number);
 #pragma unroll
-        for (int e = 0; e < kCols; e++) keep[e] = mask >> e & 1 ? 1.0f : 0.0f;
+            for (int e = 0; e < kCols; e++) keep[e] = r.kept(e, a.drop.threshold) ? 1.0f : 0.0f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kCols; e++) keep[e] = 1.0f;
+        }
+        if (skip) {  // the group's columns are the vector's last ones
+            float v[kCols];
+#pragma unroll
+            for (int e = 0; e < kCols; e++) {
+                v[e] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < e; f++) v[e] = e - f == skip ? keep[f] : v[e];
+            }
+#pragma unroll
+            for (int e = 0; e < kCols; e++) keep[e] = v[e];
+        }
     }
 };
 
@@ -477,9 +488,9 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
     Way<TPR, GENERAL> way;
     int64_t group_end = 0;
     for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
-        const Words<T, V> x = mine.template get_own<T>(a.x, row, a.x_ld);
-        Words<T, V> h = {};
-        if (a.h) h = mine.template get_own<T>(a.h, row, a.h_ld);
+        Words<T, V> x = mine.template get<T>(a.x, row, a.x_ld), h = {};
+        if (a.h) h = mine.template get<T>(a.h, row, a.h_ld);
+        mine.only_own(x), mine.only_own(h);
         if (row >= group_end) {
             const int64_t group = row / a.gate_rows;
             way = Way<TPR, GENERAL>(a, mine, group);
@@ -546,35 +557,63 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
     const float inv = 1.0f / (float)a.cols;
     const float inv_a = a.pre == BYZ_NORM_LAYER ? inv : 0.0f, inv_b = a.post == BYZ_NORM_LAYER ? inv : 0.0f;
     const int slot = slot_of<TPR>();
-    float w2[V], sum_w2[V] = {}, sum_b2[V] = {}, sum_a[V] = {}, sum_b[V] = {};
-    mine.parameters_of(a.w2, 1.0f, w2);
-    Way<TPR, GENERAL> way;
+    float sum_w2[V] = {}, sum_b2[V] = {}, sum_a[V] = {}, sum_b[V] = {}, bias[V];
+    // A thread's own weights in LDS, read where they are used: in registers they would take sixteen.
+    float *const rest = room + 2 * NT * V;
+    enum { kWay, kPre };
+    auto store = [&](int which, const float (&v)[V]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < V; e++) room[((which * 2 + e / 4) * NT + threadIdx.x) * 4 + e % 4] = v[e];
+    };
+    auto fetch = [&](int which, float (&v)[V]) __attribute__((always_inline)) {
+        const int at = afresh((int)threadIdx.x);
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            const float4 w = *(const float4 *)&room[((which * 2 + q) * NT + at) * 4];
+            v[q * 4] = w.x, v[q * 4 + 1] = w.y, v[q * 4 + 2] = w.z, v[q * 4 + 3] = w.w;
+        }
+    };
+    {
+        float w2[V];
+        mine.parameters_of(a.w2, 1.0f, w2);
+        store(kPre, w2);
+    }
     struct Loaded {
         Words<T, V> x, h, dout, dy;
         Stats s;
     };
+    // What is absent is read from x and set to zero in use: with loads that may not be made, waiting for one is waiting for all.
+    const void *const h_at = a.h ? a.h : a.x, *const dy_at = b.dy ? b.dy : a.x, *const dout_at = b.dout ? b.dout : a.x;
+    const int64_t h_ld = a.h ? a.h_ld : a.x_ld, dy_ld = b.dy ? b.dy_ld : a.x_ld, dout_ld = b.dout ? b.dout_ld : a.x_ld;
     auto load = [&](int64_t row) __attribute__((always_inline)) {
-        Loaded l = {};
+        Loaded l;
         l.s = stats_of(b.stats, row);
-        if (a.h) l.h = mine.template get<T>(a.h, row, a.h_ld);
+        l.h = mine.template get<T>(h_at, row, h_ld);
         l.x = mine.template get<T>(a.x, row, a.x_ld);
-        if (b.dy) l.dy = mine.template get_own<T>(b.dy, row, b.dy_ld);
-        if (b.dout) l.dout = mine.template get<T>(b.dout, row, b.dout_ld);
+        l.dy = mine.template get<T>(dy_at, row, dy_ld);
+        l.dout = mine.template get<T>(dout_at, row, dout_ld);
         return l;
     };
-    // The row that l has, and the loads of the next one where the registers of most of this one's values are free.
+    // The row that l has; the next one is loaded meanwhile.
     auto work = [&](Loaded &l, int64_t row, int64_t next) __attribute__((always_inline)) {
         const Words<T, V> x = l.x;
         Words<T, V> h = l.h, dout = l.dout, dy = l.dy;
         const Stats s = l.s;
-        float keep[V], tn[V];
+        l = load(next);
+        float keep[V], tn[V], w2[V], way[V];
+        fetch(kWay, way), fetch(kPre, w2);
         mine.kept(a, offset, row, keep);
+        if (!b.dy) dy = {};
+        if (!b.dout) dout = {};
+        if (!a.h) h = {};
+        mine.only_own(dy);
         drop_first(a, h, keep);
         auto hn = [&](int e) { return GENERAL ? (h[e] - s.mean1) * s.rstd1 : h[e] * s.rstd1; };
         float p1 = 0.0f, p2 = 0.0f;
 #pragma unroll
         for (int e = 0; e < V; e++) {
-            const float t = a.h ? fmaf(way.of(e, hn(e)), keep[e], x[e]) : x[e];
+            const float u = GENERAL ? fmaf(hn(e), way[e], bias[e]) : hn(e) * way[e];
+            const float t = a.h ? fmaf(u, keep[e], x[e]) : x[e];
             tn[e] = GENERAL ? (t - s.mean2) * s.rstd2 : t * s.rstd2;
             const float g = dy[e] * w2[e];
             if constexpr (GENERAL) p1 += g;
@@ -586,6 +625,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
             const float2 r = join.sum(p1, p2);
             mean_a = r.x * inv_a * -s.rstd2, mean_atn = r.y * inv * -s.rstd2;
         }
+        fetch(kPre, w2);
         float dt[V], p3 = 0.0f, p4 = 0.0f;
 #pragma unroll
         for (int e = 0; e < V; e++) {
@@ -598,17 +638,16 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
             if constexpr (GENERAL) sum_b2[e] += dy[e];
         }
         mine.template put<T>(b.dx, row, b.dx_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
+        fetch(kWay, way);
 #pragma unroll
         for (int e = 0; e < V; e++) {
             const float normal = hn(e), dv = keep[e] * dt[e];
             sum_a[e] = fmaf(dv, normal, sum_a[e]);
             if constexpr (GENERAL) sum_b[e] += dv;
-            dt[e] = dv * way.w[e];
+            dt[e] = dv * way[e];
             if constexpr (GENERAL) p3 += dt[e];
             p4 = fmaf(dt[e], normal, p4);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        l = load(next);
         if (!a.h) return;
         if (a.post != BYZ_NORM_NONE) {
             h.keep();
@@ -619,13 +658,12 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
         }
         mine.template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
     };
-    // one span of a group's rows for the slots together, or spans of whole groups for each
+    // some of a group's rows, or whole groups for each slot
     const int64_t chunk = blockIdx.x, group_rows = a.gate_rows;
     const bool part = b.per_group != 0;
-    int64_t group = part ? chunk / b.per_group : chunk * b.chunk / group_rows + slot;
-    const int64_t first = part ? group * group_rows + chunk % b.per_group * b.chunk + slot : 0;
-    const int64_t end = std::min(a.rows, part ? std::min(first - slot + b.chunk, (group + 1) * group_rows) : (chunk + 1) * b.chunk);
-    float *const own_w1 = room + threadIdx.x * V, *const own_b1 = own_w1 + NT * V;  // over the groups
+    int64_t group = part ? chunk / b.per_group : chunk * SLOTS + slot;
+    const int64_t step = part ? b.per_group * SLOTS : 1, groups = part ? group + 1 : (a.rows + group_rows - 1) / group_rows;
+    float *const own_w1 = rest + threadIdx.x * V, *const own_b1 = own_w1 + NT * V;  // over the groups
     if (!part) {
 #pragma unroll
         for (int e = 0; e < V; e++) own_w1[e] = own_b1[e] = 0.0f;
@@ -643,11 +681,18 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
             w1_sum(e, factor * g[e] * sum_a[e]), b1_sum(e, factor * g[e] * sum_b[e]);
         }
     };
-    for (int64_t row = part ? first : group * group_rows; row < end; group += SLOTS, row = group * group_rows) {
-        way = Way<TPR, GENERAL>(a, mine, group);
-        const int64_t stop = part ? end : std::min(end, row + group_rows), step = part ? SLOTS : 1;
-        Loaded l = load(row);
-        for (; row < stop; row += step) work(l, row, std::min(row + step, stop - 1));
+    for (; group < groups; group += (int64_t)gridDim.x * SLOTS) {
+        const Way<TPR, GENERAL> way(a, mine, group);
+        store(kWay, way.w);
+        if constexpr (GENERAL)
+#pragma unroll
+            for (int e = 0; e < V; e++) bias[e] = way.b[e];
+        const int64_t end = std::min(a.rows, (group + 1) * group_rows);
+        int64_t row = group * group_rows + (part ? chunk % b.per_group * SLOTS + slot : 0);
+        if (row < end) {
+            Loaded l = load(row);
+            for (; row < end; row += step) work(l, row, row + step < end ? row + step : row);
+        }
         if (part) break;
         close([&](int e, float v) { if (b.d_gate && e >= mine.skip) b.d_gate[group * a.cols + mine.first + e] = v; },
               [&](int e, float v) { own_w1[e] += v; }, [&](int e, float v) { own_b1[e] += v; });
@@ -674,7 +719,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
             if (e >= mine.skip) {
                 const float sum = k == kW2 ? sum_w2[e] : k == kB2 ? sum_b2[e] : k == kW1 ? w1_sum[e] : k == kB1 ? b1_sum[e] : gate_sum[e];
                 if constexpr (SLOTS > 1)
-                    room[slot * (TPR * V) + mine.first + e] = sum;
+                    rest[slot * (TPR * V) + mine.first + e] = sum;
                 else
                     to[mine.first + e] = sum;
             }
@@ -683,7 +728,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
             for (int i = threadIdx.x; i < (int)a.cols; i += NT) {
                 float sum = 0.0f;
 #pragma unroll
-                for (int l = 0; l < SLOTS; l++) sum += room[l * (TPR * V) + i];
+                for (int l = 0; l < SLOTS; l++) sum += rest[l * (TPR * V) + i];
                 to[i] = sum;
             }
         }
@@ -753,7 +798,7 @@ int with_threads(int64_t cols, F fn) {
 // How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of four rows a slot at least, each
 // within a group of gate's rows, or of whole groups where these are short.
 struct Cut {
-    int64_t chunk, per_group, groups, chunks;
+    int64_t per_group, groups, chunks;
     Cut(int64_t rows, int64_t cols, int64_t gate_rows) {
         int64_t blocks = 512, least = 4;
         if (in_registers(cols))
@@ -765,9 +810,10 @@ struct Cut {
         const int64_t want = std::max(least, (rows + blocks - 1) / blocks);
         groups = (rows + gate_rows - 1) / gate_rows;
         if (gate_rows >= want) {
-            chunk = want, per_group = (gate_rows + chunk - 1) / chunk, chunks = groups * per_group;
+            per_group = (gate_rows + want - 1) / want, chunks = groups * per_group;
         } else {
-            chunk = (want + gate_rows - 1) / gate_rows * gate_rows, per_group = 0, chunks = (rows + chunk - 1) / chunk;
+            const int64_t each = (want + gate_rows - 1) / gate_rows;  // groups of a chunk
+            per_group = 0, chunks = (groups + each - 1) / each;
         }
     }
 };
@@ -804,11 +850,11 @@ int launch_forward(const Args &a, hipStream_t s) {
 template <typename T>
 int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
+    const bool general = a.b1 || (b.kinds & (1u << kB1 | 1u << kB2)) || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
     if (in_registers(a.cols) && (cut.per_group || a.cols <= kGroupsInLds)) {
-        const bool general = a.b1 || (b.kinds & (1u << kB1 | 1u << kB2)) || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
         const int rc = with_threads(a.cols, [&](auto tpr) -> int {
             constexpr int TPR = tpr.value, NT = block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
-            const int bytes = !cut.per_group ? 2 * each : NT > TPR ? each : 0;
+            const int bytes = 2 * each + (!cut.per_group ? 2 * each : NT > TPR ? each : 0);
             (general ? &backward_rows_kernel<T, TPR, true> : &backward_rows_kernel<T, TPR, false>)<<<(unsigned)cut.chunks, NT, bytes, s>>>(a, b);
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;
@@ -926,7 +972,7 @@ extern "C" int byz_residual_norm_backward(const void *dout, int64_t dout_ld, con
     b.d_gate = cut.per_group ? nullptr : d_gate;
     for (int k = 0; k < kKinds; k++)
         if (out.of[k] && (k != kGate || cut.per_group)) b.kinds |= 1u << k;
-    b.chunk = cut.chunk, b.per_group = cut.per_group;
+    b.chunks = cut.chunks, b.per_group = cut.per_group;
     return dtype == BYZ_F32 ? launch_backward<float>(a, b, cut, out, s)
            : dtype == BYZ_BF16 ? launch_backward<bf16>(a, b, cut, out, s) : launch_backward<f16>(a, b, cut, out, s);
 }
