@@ -31,6 +31,11 @@ struct Args {
     float *stats;
 };
 
+// Which of gate's rows row has; there are 2^32 rows at most.
+__device__ __forceinline__ int64_t group_of(const Args &a, int64_t row) {
+    return row < a.gate_rows ? 0 : (int64_t)((uint32_t)row / (uint32_t)a.gate_rows);
+}
+
 struct Back {
     const void *dout, *dy;
     int64_t dout_ld, dy_ld;
@@ -41,7 +46,8 @@ struct Back {
     float *partials;  // [chunk][kind][column]
     float *d_gate;
     uint32_t kinds;     // bit k: kind k is wanted
-    int64_t chunks, per_group;  // per_group: of a group of gate's rows; 0: a chunk has whole groups
+    uint32_t chunks, per_group;  // per_group: of a group of gate's rows; 0: a chunk has whole groups
+    int64_t groups;
 };
 enum { kW2, kB2, kW1, kB1, kGate, kKinds };
 
@@ -102,7 +108,7 @@ struct Piece {
         float w1[V], b1[V];
         parameters<V>(a.w1, col, n, 1.0f, w1);
         parameters<V>(a.b1, col, n, 0.0f, b1);
-        parameters<V>(a.gate ? a.gate + row / a.gate_rows * a.cols : nullptr, col, n, 1.0f, sg);
+        parameters<V>(a.gate ? a.gate + group_of(a, row) * a.cols : nullptr, col, n, 1.0f, sg);
         kept = a.drop.threshold ? DropV<V>(a.drop, offset, (uint32_t)row, (uint32_t)col).mask : ~0u;
 #pragma unroll
         for (int e = 0; e < V; e++) {
@@ -289,15 +295,16 @@ __global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
         }
     };
     if (b.per_group) {
-        const int64_t group = chunk / b.per_group, end = std::min((group + 1) * group_rows, a.rows);
-        for (int64_t row = group * group_rows + chunk % b.per_group * W + wave; row < end; row += b.per_group * W) add(row);
+        const uint32_t group = blockIdx.y / b.per_group;
+        const int64_t end = std::min((group + 1) * group_rows, a.rows);
+        for (int64_t row = group * group_rows + blockIdx.y % b.per_group * W + wave; row < end; row += b.per_group * W) add(row);
     } else {
-        for (int64_t start = (chunk * W + wave) * group_rows; start < a.rows; start += b.chunks * W * group_rows) {
-            const int64_t end = a.rows;
-            for (int64_t row = start; row < std::min(end, start + group_rows); row++) add(row);
+        for (int64_t group = chunk * W + wave; group < b.groups; group += b.chunks * W) {
+            const int64_t end = std::min((group + 1) * group_rows, a.rows);
+            for (int64_t row = group * group_rows; row < end; row++) add(row);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                if (b.d_gate && e < n) b.d_gate[start / group_rows * a.cols + col + e] = acc[kGate][e];
+                if (b.d_gate && e < n) b.d_gate[group * a.cols + col + e] = acc[kGate][e];
                 acc[kGate][e] = 0.0f;
             }
         }
@@ -369,13 +376,21 @@ constexpr int block_of() {
     return TPR <= 64 ? 256 : TPR;
 }
 
-// A vector's values from the `skip`-th on.
+// A vector's values from the `skip`-th on.  The few are stored one by one in a loop: unrolled, with a branch for each, a kernel's
+// code would be half as long again, and a short call is bound by reading its code.
 template <typename T, int V>
 __device__ __forceinline__ void put_from(T *to, int skip, const Words<T, V> &v) {
     if (skip == 0) return put_words(to, v);
+    Words<T, V> w = v;
+#pragma unroll 1
+    for (int e = 0; e < V; e++) {
+        if (e >= skip) to[e] = __builtin_bit_cast(Pack<T, 4 / sizeof(T)>, (uint32_t)w.w[0]).v[0];
 #pragma unroll
-    for (int e = 0; e < V; e++)
-        if (e >= skip) to[e] = round_to<T>(v[e]);
+        for (int i = 0; i < w.N; i++) {
+            const uint32_t next = i + 1 < w.N ? (uint32_t)w.w[i + 1] : 0;
+            w.w[i] = sizeof(T) == 4 ? next : (uint32_t)__builtin_amdgcn_alignbit(next, w.w[i], 16);
+        }
+    }
 }
 
 // A thread's eight columns.  The vector of a row's last thread ends with the row, so its first `skip` columns are those of the
@@ -430,16 +445,11 @@ struct Columns {
 #pragma unroll
             for (int e = 0; e < kCols; e++) keep[e] = 1.0f;
         }
-        if (skip) {  // the group's columns are the vector's last ones
-            float v[kCols];
+#pragma unroll 1
+        for (int i = 0; i < skip; i++) {  // the group's columns are the vector's last ones
 #pragma unroll
-            for (int e = 0; e < kCols; e++) {
-                v[e] = 0.0f;
-#pragma unroll
-                for (int f = 0; f < e; f++) v[e] = e - f == skip ? keep[f] : v[e];
-            }
-#pragma unroll
-            for (int e = 0; e < kCols; e++) keep[e] = v[e];
+            for (int e = kCols - 1; e > 0; e--) keep[e] = keep[e - 1];
+            keep[0] = 0.0f;
         }
     }
 };
@@ -492,7 +502,7 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
         if (a.h) h = mine.template get<T>(a.h, row, a.h_ld);
         mine.only_own(x), mine.only_own(h);
         if (row >= group_end) {
-            const int64_t group = row / a.gate_rows;
+            const int64_t group = group_of(a, row);
             way = Way<TPR, GENERAL>(a, mine, group);
             group_end = (group + 1) * a.gate_rows;
         }
@@ -546,8 +556,8 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
 // dx and dh of a chunk's rows, and the chunk's sums of the columns: a thread has eight columns of every row of its slot, whose
 // sums stay in its registers.  Chunks are those of columns_kernel.  Over a group of gate's rows
 //     A = sum drop(dt) hn,  B = sum drop(dt)   give   dw1 = s g A,  db1 = s g B,  dg = s (w1 A + b1 B).
-template <typename T, int TPR, bool GENERAL>
-__global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
+template <typename T, int TPR, bool GENERAL, bool PART>
+__global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL || sizeof(T) == 2 : !GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
     constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
     __shared__ float2 lds[2 * TPR / 16];
     extern __shared__ float room[];
@@ -559,7 +569,6 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
     const int slot = slot_of<TPR>();
     float sum_w2[V] = {}, sum_b2[V] = {}, sum_a[V] = {}, sum_b[V] = {}, bias[V];
     // A thread's own weights in LDS, read where they are used: in registers they would take sixteen.
-    float *const rest = room + 2 * NT * V;
     enum { kWay, kPre };
     auto store = [&](int which, const float (&v)[V]) __attribute__((always_inline)) {
 #pragma unroll
@@ -658,81 +667,71 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (!GENERAL && sizeof
         }
         mine.template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
     };
-    // some of a group's rows, or whole groups for each slot
+    // some of a group's rows (PART), or whole groups for each slot
     const int64_t chunk = blockIdx.x, group_rows = a.gate_rows;
-    const bool part = b.per_group != 0;
-    int64_t group = part ? chunk / b.per_group : chunk * SLOTS + slot;
-    const int64_t step = part ? b.per_group * SLOTS : 1, groups = part ? group + 1 : (a.rows + group_rows - 1) / group_rows;
-    float *const own_w1 = rest + threadIdx.x * V, *const own_b1 = own_w1 + NT * V;  // over the groups
-    if (!part) {
+    int64_t group = PART ? blockIdx.x / b.per_group : chunk * SLOTS + slot;
+    float gate_sum[V], w1_sum[V], b1_sum[V];
+    float *const own = room + (2 * NT + threadIdx.x) * V;  // sums over the groups: of b1 NT * V behind those of w1
+    if constexpr (!PART) {
 #pragma unroll
-        for (int e = 0; e < V; e++) own_w1[e] = own_b1[e] = 0.0f;
+        for (int e = 0; e < V; e++) own[e] = own[NT * V + e] = 0.0f;
     }
-    // sums of a group's rows to those of its vectors
-    auto close = [&](auto gate_sum, auto w1_sum, auto b1_sum) __attribute__((always_inline)) {
-        float g[V], w1[V], b1[V];
-        mine.parameters_of(a.gate ? a.gate + group * a.cols : nullptr, 1.0f, g);
-        mine.parameters_of(a.w1, 1.0f, w1);
-        mine.parameters_of(a.b1, 0.0f, b1);
-        const float factor = a.scale * a.drop.scale;
+    for (; group < (PART ? group + 1 : b.groups); group += (int64_t)gridDim.x * SLOTS) {
+        {
+            const Way<TPR, GENERAL> way(a, mine, group);
+            store(kWay, way.w);
+            if constexpr (GENERAL)
 #pragma unroll
-        for (int e = 0; e < V; e++) {
-            gate_sum(e, factor * (w1[e] * sum_a[e] + (GENERAL ? b1[e] * sum_b[e] : 0.0f)));
-            w1_sum(e, factor * g[e] * sum_a[e]), b1_sum(e, factor * g[e] * sum_b[e]);
+                for (int e = 0; e < V; e++) bias[e] = way.b[e];
         }
-    };
-    for (; group < groups; group += (int64_t)gridDim.x * SLOTS) {
-        const Way<TPR, GENERAL> way(a, mine, group);
-        store(kWay, way.w);
-        if constexpr (GENERAL)
-#pragma unroll
-            for (int e = 0; e < V; e++) bias[e] = way.b[e];
-        const int64_t end = std::min(a.rows, (group + 1) * group_rows);
-        int64_t row = group * group_rows + (part ? chunk % b.per_group * SLOTS + slot : 0);
+        const int64_t end = std::min(a.rows, (group + 1) * group_rows), step = PART ? (int64_t)b.per_group * SLOTS : 1;
+        int64_t row = group * group_rows + (PART ? blockIdx.x % b.per_group * SLOTS + slot : 0);
         if (row < end) {
             Loaded l = load(row);
             for (; row < end; row += step) work(l, row, row + step < end ? row + step : row);
         }
-        if (part) break;
-        close([&](int e, float v) { if (b.d_gate && e >= mine.skip) b.d_gate[group * a.cols + mine.first + e] = v; },
-              [&](int e, float v) { own_w1[e] += v; }, [&](int e, float v) { own_b1[e] += v; });
+        // the sums of a group's rows make those of its vectors
+        float g[V], w1[V], b1[V];
+        mine.parameters_of(a.gate ? a.gate + group * a.cols : nullptr, 1.0f, g);
+        mine.parameters_of(a.w1, 1.0f, w1);
+        if constexpr (GENERAL) mine.parameters_of(a.b1, 0.0f, b1);
+        const float factor = a.scale * a.drop.scale;
 #pragma unroll
-        for (int e = 0; e < V; e++) sum_a[e] = sum_b[e] = 0.0f;
-    }
-    // what the chunk has for each kind, joined over the slots
-    float gate_sum[V], w1_sum[V], b1_sum[V];
-    if (part) {
-        close([&](int e, float v) { gate_sum[e] = v; }, [&](int e, float v) { w1_sum[e] = v; }, [&](int e, float v) { b1_sum[e] = v; });
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; e++) w1_sum[e] = own_w1[e], b1_sum[e] = own_b1[e], gate_sum[e] = 0.0f;
-    }
-    int at = 0;
-#pragma unroll
-    for (int k = 0; k < kKinds; k++) {
-        if (!(b.kinds >> k & 1)) continue;
-        float *to = b.partials + (chunk * __builtin_popcount(b.kinds) + at) * a.cols;
-        at++;
-        if constexpr (SLOTS > 1) __syncthreads();
-#pragma unroll
-        for (int e = 0; e < V; e++)
-            if (e >= mine.skip) {
-                const float sum = k == kW2 ? sum_w2[e] : k == kB2 ? sum_b2[e] : k == kW1 ? w1_sum[e] : k == kB1 ? b1_sum[e] : gate_sum[e];
-                if constexpr (SLOTS > 1)
-                    rest[slot * (TPR * V) + mine.first + e] = sum;
-                else
-                    to[mine.first + e] = sum;
-            }
-        if constexpr (SLOTS > 1) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < (int)a.cols; i += NT) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int l = 0; l < SLOTS; l++) sum += rest[l * (TPR * V) + i];
-                to[i] = sum;
-            }
+        for (int e = 0; e < V; e++) {
+            gate_sum[e] = factor * (GENERAL ? fmaf(w1[e], sum_a[e], b1[e] * sum_b[e]) : w1[e] * sum_a[e]);
+            w1_sum[e] = factor * g[e] * sum_a[e], b1_sum[e] = factor * g[e] * sum_b[e];
         }
+        if constexpr (PART) break;
+        if (b.d_gate) mine.template put<float>(b.d_gate, group, a.cols, Words<float, V>::of([&](int e) { return gate_sum[e]; }));
+#pragma unroll
+        for (int e = 0; e < V; e++) own[e] += w1_sum[e], own[NT * V + e] += b1_sum[e], sum_a[e] = sum_b[e] = 0.0f;
     }
+    if constexpr (!PART) {
+#pragma unroll
+        for (int e = 0; e < V; e++) w1_sum[e] = own[e], b1_sum[e] = own[NT * V + e];
+    }
+    // What the chunk has for each kind, joined over the slots and written by neighbouring threads.  The weights' place is free.
+    int at = 0;
+    auto write = [&](int kind, const float (&v)[V]) __attribute__((always_inline)) {
+        if (!(b.kinds >> kind & 1)) return;
+        float *const to = b.partials + (chunk * __builtin_popcount(b.kinds) + at++) * a.cols;
+        __syncthreads();
+        const auto w = Words<float, V>::of([&](int e) { return v[e]; });
+        __builtin_memcpy(room + threadIdx.x * V, &w, sizeof(w));
+        __syncthreads();
+        for (int i = threadIdx.x; i < (int)a.cols; i += NT) {
+            const int first = i / V * V, place = first + i - std::min(first, (int)a.cols - V);
+            float sum = 0.0f;
+#pragma unroll
+            for (int l = 0; l < SLOTS; l++) sum += room[l * (TPR * V) + place];
+            to[i] = sum;
+        }
+    };
+    write(kW2, sum_w2);
+    if constexpr (GENERAL) write(kB2, sum_b2);
+    write(kW1, w1_sum);
+    if constexpr (GENERAL) write(kB1, b1_sum);
+    if constexpr (PART) write(kGate, gate_sum);
 }
 
 struct Outputs {
@@ -795,7 +794,7 @@ int with_threads(int64_t cols, F fn) {
     return fn(std::integral_constant<int, 1024>{});
 }
 
-// How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of four rows a slot at least, each
+// How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of two rows a slot at least, each
 // within a group of gate's rows, or of whole groups where these are short.
 struct Cut {
     int64_t per_group, groups, chunks;
@@ -804,7 +803,7 @@ struct Cut {
         if (in_registers(cols))
             with_threads(cols, [&](auto tpr) -> int {
                 constexpr int NT = block_of<tpr.value>();
-                blocks = kCus * 1024 / NT, least = 4 * (NT / tpr.value);
+                blocks = kCus * 1024 / NT, least = 2 * (NT / tpr.value);
                 return 0;
             });
         const int64_t want = std::max(least, (rows + blocks - 1) / blocks);
@@ -854,8 +853,13 @@ int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, h
     if (in_registers(a.cols) && (cut.per_group || a.cols <= kGroupsInLds)) {
         const int rc = with_threads(a.cols, [&](auto tpr) -> int {
             constexpr int TPR = tpr.value, NT = block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
-            const int bytes = 2 * each + (!cut.per_group ? 2 * each : NT > TPR ? each : 0);
-            (general ? &backward_rows_kernel<T, TPR, true> : &backward_rows_kernel<T, TPR, false>)<<<(unsigned)cut.chunks, NT, bytes, s>>>(a, b);
+            if (cut.per_group) {
+                (general ? &backward_rows_kernel<T, TPR, true, true> : &backward_rows_kernel<T, TPR, false, true>)
+                    <<<(unsigned)cut.chunks, NT, 2 * each, s>>>(a, b);
+            } else if constexpr (TPR <= 512) {
+                (general ? &backward_rows_kernel<T, TPR, true, false> : &backward_rows_kernel<T, TPR, false, false>)
+                    <<<(unsigned)cut.chunks, NT, 4 * each, s>>>(a, b);
+            }
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;
         });
@@ -972,7 +976,7 @@ extern "C" int byz_residual_norm_backward(const void *dout, int64_t dout_ld, con
     b.d_gate = cut.per_group ? nullptr : d_gate;
     for (int k = 0; k < kKinds; k++)
         if (out.of[k] && (k != kGate || cut.per_group)) b.kinds |= 1u << k;
-    b.chunks = cut.chunks, b.per_group = cut.per_group;
+    b.chunks = (uint32_t)cut.chunks, b.per_group = (uint32_t)cut.per_group, b.groups = cut.groups;
     return dtype == BYZ_F32 ? launch_backward<float>(a, b, cut, out, s)
            : dtype == BYZ_BF16 ? launch_backward<bf16>(a, b, cut, out, s) : launch_backward<f16>(a, b, cut, out, s);
 }
