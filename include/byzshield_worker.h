@@ -243,7 +243,8 @@ int byz_policy_loss_step(const float *dloss, const void *logits, int64_t rows, i
  * sum of logp over s, and ref[s] the same of a reference model (NULL: zeros),
  *     margin = beta ((sums - ref)[2 i] - (sums - ref)[2 i + 1]),  sigma(x) = 1 / (1 + exp(-x))
  *     loss[i] = -(1 - smoothing) log sigma(margin) - smoothing log sigma(-margin),  slope[i] = d loss / d margin
- * Rows of no sequence are in no loss, and their gradient is 0.  A pair whose bounds fall or leave 0 .. rows has a NaN loss and slope.
+ * Rows of no sequence are in no loss, and their gradient is 0.  A pair whose bounds fall or leave 0 .. rows has a NaN loss and
+ * slope, and what gradient its rows get is not specified.
  * sums (2 pairs) and slope (pairs, for the backward call) may be NULL.  0 <= smoothing <= 1; beta is finite.
  */
 int byz_preference_loss(const void *logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, const int32_t *label,
