@@ -334,7 +334,13 @@ struct RowJoiner {
     static constexpr int waves = TPR / 64;
     float2 *lds;  // 2 * waves
     int turn = 0;
-    __device__ explicit RowJoiner(float2 *l) : lds(l) {}
+    // starts with a barrier where a block has a row: it may have fewer waves than TPR has
+    __device__ explicit RowJoiner(float2 *l) : lds(l) {
+        if constexpr (waves > 1) {
+            if (threadIdx.x < 2 * waves) lds[threadIdx.x] = make_float2(0.0f, 0.0f);
+            __syncthreads();
+        }
+    }
     // over 2^LANES lanes that lie together; every one gets the same bits
     template <int LANES>
     static __device__ __forceinline__ float2 lanes(float2 v) {
@@ -374,6 +380,11 @@ constexpr int kCols = 8;  // columns of a thread: one call of the generator
 template <int TPR>
 constexpr int block_of() {
     return TPR <= 64 ? 256 : TPR;
+}
+// The threads a block is launched with: of TPR those whose waves a row needs (3674 x 5240 fp16, forward: 58 us with all 1024).
+template <int TPR>
+int threads_of(int64_t cols) {
+    return TPR <= 64 ? 256 : (int)((cols + 64 * kCols - 1) / (64 * kCols)) * 64;
 }
 
 // A vector's values from the `skip`-th on.  The few are stored one by one in a loop: unrolled, with a branch for each, a kernel's
@@ -719,7 +730,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
         const auto w = Words<float, V>::of([&](int e) { return v[e]; });
         __builtin_memcpy(room + threadIdx.x * V, &w, sizeof(w));
         __syncthreads();
-        for (int i = threadIdx.x; i < (int)a.cols; i += NT) {
+        for (int i = threadIdx.x; i < (int)a.cols; i += blockDim.x) {
             const int first = i / V * V, place = first + i - std::min(first, (int)a.cols - V);
             float sum = 0.0f;
 #pragma unroll
@@ -796,14 +807,15 @@ int with_threads(int64_t cols, F fn) {
 
 // How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of two rows a slot at least, each
 // within a group of gate's rows, or of whole groups where these are short.
+constexpr int64_t kLeast = 2;  // us at 2, 4, 8: backward of 333 x 1000 fp32 18, 23, 33, of 3950 x 604 bf16 30, 29, 36
 struct Cut {
     int64_t per_group, groups, chunks;
     Cut(int64_t rows, int64_t cols, int64_t gate_rows) {
         int64_t blocks = 512, least = 4;
         if (in_registers(cols))
             with_threads(cols, [&](auto tpr) -> int {
-                constexpr int NT = block_of<tpr.value>();
-                blocks = kCus * 1024 / NT, least = 2 * (NT / tpr.value);
+                constexpr int TPR = tpr.value;
+                blocks = kCus * (1024 / threads_of<TPR>(cols)), least = kLeast * (block_of<TPR>() / TPR);
                 return 0;
             });
         const int64_t want = std::max(least, (rows + blocks - 1) / blocks);
@@ -834,9 +846,10 @@ int launch_forward(const Args &a, hipStream_t s) {
     if (in_registers(a.cols)) {
         const bool general = a.b1 || a.b2 || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
         return with_threads(a.cols, [&](auto tpr) -> int {
-            constexpr int TPR = tpr.value, NT = block_of<TPR>(), slots = NT / TPR;
-            const int64_t blocks = std::min((a.rows + slots - 1) / slots, (int64_t)kCus * 2048 / NT);
-            (general ? &forward_rows_kernel<T, TPR, true> : &forward_rows_kernel<T, TPR, false>)<<<(unsigned)blocks, NT, 0, s>>>(a);
+            constexpr int TPR = tpr.value, slots = block_of<TPR>() / TPR;
+            const int threads = threads_of<TPR>(a.cols);
+            const int64_t blocks = std::min((a.rows + slots - 1) / slots, (int64_t)kCus * (2048 / threads));
+            (general ? &forward_rows_kernel<T, TPR, true> : &forward_rows_kernel<T, TPR, false>)<<<(unsigned)blocks, threads, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;
         });
@@ -855,10 +868,10 @@ int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, h
             constexpr int TPR = tpr.value, NT = block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
             if (cut.per_group) {
                 (general ? &backward_rows_kernel<T, TPR, true, true> : &backward_rows_kernel<T, TPR, false, true>)
-                    <<<(unsigned)cut.chunks, NT, 2 * each, s>>>(a, b);
+                    <<<(unsigned)cut.chunks, threads_of<TPR>(a.cols), 2 * each, s>>>(a, b);
             } else if constexpr (TPR <= 512) {
                 (general ? &backward_rows_kernel<T, TPR, true, false> : &backward_rows_kernel<T, TPR, false, false>)
-                    <<<(unsigned)cut.chunks, NT, 4 * each, s>>>(a, b);
+                    <<<(unsigned)cut.chunks, threads_of<TPR>(a.cols), 4 * each, s>>>(a, b);
             }
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;
