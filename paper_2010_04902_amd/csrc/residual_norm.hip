@@ -409,8 +409,8 @@ __device__ __forceinline__ void put_from(T *to, int skip, const Words<T, V> &v) 
 template <int TPR>
 struct Columns {
     int first, skip, number;  // number: of the generator's group
-    __device__ __forceinline__ explicit Columns(int64_t cols) {
-        const int own = threadIdx.x % TPR;
+    __device__ __forceinline__ explicit Columns(int64_t cols, int vector = 0) {  // the thread's vector of that number
+        const int own = vector * TPR + threadIdx.x % TPR;
         first = std::min(own * kCols, (int)cols - kCols);
         skip = std::min(own * kCols - first, kCols);
         number = std::min(own, ((int)cols - 1) / kCols);
@@ -494,68 +494,92 @@ struct Way {
     __device__ __forceinline__ float of(int e, float normal) const { return GENERAL ? fmaf(normal, w[e], b[e]) : normal * w[e]; }
 };
 
-// Eight columns of a row to each of TPR threads.  GENERAL: means and biases; without, there are none.
-template <typename T, int TPR, bool GENERAL>
+// R times eight columns of a row to each of TPR threads.  GENERAL: means and biases; without, there are none.
+template <typename T, int TPR, int R, bool GENERAL>
 __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a) {
     constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
     __shared__ float2 lds[2 * TPR / 16];
     RowJoiner<TPR> join(lds);
-    const Columns<TPR> mine(a.cols);
+    auto mine = [&](int r) __attribute__((always_inline)) { return Columns<TPR>(a.cols, r); };
     const uint64_t offset = drop_offset(a.drop);
     const float inv = 1.0f / (float)a.cols;
-    float w2[V], b2[V];
-    mine.parameters_of(a.w2, 1.0f, w2);
-    if constexpr (GENERAL) mine.parameters_of(a.b2, 0.0f, b2);
-    Way<TPR, GENERAL> way;
+    float w2[R][V], b2[R][V];
+    Way<TPR, GENERAL> way[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        mine(r).parameters_of(a.w2, 1.0f, w2[r]);
+        if constexpr (GENERAL) mine(r).parameters_of(a.b2, 0.0f, b2[r]);
+    }
     int64_t group_end = 0;
     for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
-        Words<T, V> x = mine.template get<T>(a.x, row, a.x_ld), h = {};
-        if (a.h) h = mine.template get<T>(a.h, row, a.h_ld);
-        mine.only_own(x), mine.only_own(h);
+        Words<T, V> x[R], h[R] = {};
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            x[r] = mine(r).template get<T>(a.x, row, a.x_ld);
+            if (a.h) h[r] = mine(r).template get<T>(a.h, row, a.h_ld);
+            mine(r).only_own(x[r]), mine(r).only_own(h[r]);
+        }
         if (row >= group_end) {
             const int64_t group = group_of(a, row);
-            way = Way<TPR, GENERAL>(a, mine, group);
+#pragma unroll
+            for (int r = 0; r < R; r++) way[r] = Way<TPR, GENERAL>(a, mine(r), group);
             group_end = (group + 1) * a.gate_rows;
         }
         Stats s;
-        float t[V];
+        float t[R][V];
         // the mean of rows of the layer norm first, then that of the squares about it
         auto moments = [&](int kind, float &mean, float &rstd, auto value) __attribute__((always_inline)) {
             float sum = 0.0f;
             if (GENERAL && kind == BYZ_NORM_LAYER) {
 #pragma unroll
-                for (int e = 0; e < V; e++) sum += value(e);
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum += value(r, e);
                 mean = join.sum(sum, 0.0f).x * inv;
                 sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const float d = value(e) - mean;
-                    sum += e >= mine.skip ? d * d : 0.0f;
-                }
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        const float d = value(r, e) - mean;
+                        sum += e >= mine(r).skip ? d * d : 0.0f;
+                    }
             } else {
 #pragma unroll
-                for (int e = 0; e < V; e++) sum = fmaf(value(e), value(e), sum);
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum = fmaf(value(r, e), value(r, e), sum);
             }
             rstd = 1.0f / sqrtf(join.sum(sum, 0.0f).x * inv + a.eps);
         };
         if (a.h) {
-            float keep[V];
-            mine.kept(a, offset, row, keep);
-            drop_first(a, h, keep);
-            if (a.post != BYZ_NORM_NONE) moments(a.post, s.mean1, s.rstd1, [&](int e) { return h[e]; });
+            float keep[R][V];
 #pragma unroll
-            for (int e = 0; e < V; e++)
-                t[e] = fmaf(way.of(e, GENERAL ? (h[e] - s.mean1) * s.rstd1 : h[e] * s.rstd1), keep[e], x[e]);
-            mine.template put<T>(a.out, row, a.out_ld, Words<T, V>::of([&](int e) { return t[e]; }));
+            for (int r = 0; r < R; r++) {
+                mine(r).kept(a, offset, row, keep[r]);
+                drop_first(a, h[r], keep[r]);
+            }
+            if (a.post != BYZ_NORM_NONE) moments(a.post, s.mean1, s.rstd1, [&](int r, int e) { return h[r][e]; });
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    t[r][e] = fmaf(way[r].of(e, GENERAL ? (h[r][e] - s.mean1) * s.rstd1 : h[r][e] * s.rstd1), keep[r][e], x[r][e]);
+                mine(r).template put<T>(a.out, row, a.out_ld, Words<T, V>::of([&](int e) { return t[r][e]; }));
+            }
         } else {
 #pragma unroll
-            for (int e = 0; e < V; e++) t[e] = x[e];
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int e = 0; e < V; e++) t[r][e] = x[r][e];
         }
         if (a.pre != BYZ_NORM_NONE) {
-            moments(a.pre, s.mean2, s.rstd2, [&](int e) { return t[e]; });
-            mine.template put<T>(a.y, row, a.y_ld, Words<T, V>::of([&](int e) {
-                                     return GENERAL ? fmaf((t[e] - s.mean2) * s.rstd2, w2[e], b2[e]) : t[e] * s.rstd2 * w2[e];
-                                 }));
+            moments(a.pre, s.mean2, s.rstd2, [&](int r, int e) { return t[r][e]; });
+#pragma unroll
+            for (int r = 0; r < R; r++)
+                mine(r).template put<T>(a.y, row, a.y_ld, Words<T, V>::of([&](int e) {
+                                            return GENERAL ? fmaf((t[r][e] - s.mean2) * s.rstd2, w2[r][e], b2[r][e]) : t[r][e] * s.rstd2 * w2[r][e];
+                                        }));
         }
         if (a.stats && threadIdx.x % TPR == 0) {
             float *at = a.stats + row * 4;
@@ -843,18 +867,27 @@ size_t workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
 
 template <typename T>
 int launch_forward(const Args &a, hipStream_t s) {
+    const bool general = a.b1 || a.b2 || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
+    if (a.cols > kRowsInRegisters && a.cols <= 2 * kRowsInRegisters) {
+        const unsigned blocks = (unsigned)std::min<int64_t>(a.rows, kCus * 2);
+        (general ? &forward_rows_kernel<T, 1024, 2, true> : &forward_rows_kernel<T, 1024, 2, false>)<<<blocks, 1024, 0, s>>>(a);
+        BYZ_HIP(hipGetLastError());
+        return BYZ_OK;
+    }
     if (in_registers(a.cols)) {
-        const bool general = a.b1 || a.b2 || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
         return with_threads(a.cols, [&](auto tpr) -> int {
             constexpr int TPR = tpr.value, slots = block_of<TPR>() / TPR;
             const int threads = threads_of<TPR>(a.cols);
             const int64_t blocks = std::min((a.rows + slots - 1) / slots, (int64_t)kCus * (2048 / threads));
-            (general ? &forward_rows_kernel<T, TPR, true> : &forward_rows_kernel<T, TPR, false>)<<<(unsigned)blocks, threads, 0, s>>>(a);
+            (general ? &forward_rows_kernel<T, TPR, 1, true> : &forward_rows_kernel<T, TPR, 1, false>)<<<(unsigned)blocks, threads, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;
         });
     }
-    forward_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
+    if (a.cols > kRowsInRegisters && a.rows < kCus)
+        forward_kernel<T, 1024><<<(unsigned)std::min(a.rows, kMaxGrid), 1024, 0, s>>>(a);
+    else
+        forward_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a);
     BYZ_HIP(hipGetLastError());
     return BYZ_OK;
 }
@@ -878,7 +911,10 @@ int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, h
         });
         if (rc != BYZ_OK) return rc;
     } else {
-        rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
+        if (a.cols > kGroupsInLds && a.rows < kCus)
+            rows_kernel<T, 1024><<<(unsigned)std::min(a.rows, kMaxGrid), 1024, 0, s>>>(a, b);
+        else
+            rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
         BYZ_HIP(hipGetLastError());
         if (!b.kinds && !b.d_gate) return BYZ_OK;
         columns_kernel<T><<<dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), (unsigned)cut.chunks), 256, 0, s>>>(a, b);
