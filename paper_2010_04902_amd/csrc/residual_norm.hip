@@ -328,16 +328,18 @@ __global__ __launch_bounds__(256) void columns_kernel(Args a, Back b) {
 
 // ------------------------------------------------------------------ rows in registers
 
-// Sums over the TPR threads of a row: part of a wave, a wave, or a block.
-template <int TPR>
+// Sums over the TPR threads of a row: part of a wave, a wave, or several, of which a block may have more than one such row.
+template <int TPR, int SLOTS>
 struct RowJoiner {
-    static constexpr int waves = TPR / 64;
-    float2 *lds;  // 2 * waves
+    static constexpr int waves = TPR / 64, places = waves > 8 ? 16 : waves > 4 ? 8 : waves > 2 ? 4 : 2;
+    static constexpr int size = waves > 1 ? 2 * places * SLOTS : 1;
+    float2 *lds;
     int turn = 0;
-    // starts with a barrier where a block has a row: it may have fewer waves than TPR has
+    // starts with a barrier where rows have several waves: they may have fewer than there are places
     __device__ explicit RowJoiner(float2 *l) : lds(l) {
         if constexpr (waves > 1) {
-            if (threadIdx.x < 2 * waves) lds[threadIdx.x] = make_float2(0.0f, 0.0f);
+            if (threadIdx.x < size) lds[threadIdx.x] = make_float2(0.0f, 0.0f);
+            lds += SLOTS > 1 ? (int)threadIdx.x / TPR * (2 * places) : 0;
             __syncthreads();
         }
     }
@@ -358,33 +360,41 @@ struct RowJoiner {
         constexpr int own = TPR >= 64 ? 6 : TPR == 32 ? 5 : 4;
         float2 v = lanes<own>(make_float2(a, b));
         if constexpr (waves > 1) {
-            float2 *at = lds + turn * waves;
+            float2 *at = lds + turn * places;
             turn ^= 1;
-            if (threadIdx.x % 64 == 0) at[threadIdx.x / 64] = v;
+            if (threadIdx.x % 64 == 0) at[threadIdx.x % TPR / 64] = v;
             __syncthreads();
-            v = lanes<waves == 16 ? 4 : waves == 8 ? 3 : waves == 4 ? 2 : 1>(at[threadIdx.x % waves]);
+            v = lanes<places == 16 ? 4 : places == 8 ? 3 : places == 4 ? 2 : 1>(at[threadIdx.x % places]);
         }
         return v;
     }
 };
 
-// Which of a block's rows a thread is at: a number that the compiler knows to be a wave's where it is.
-template <int TPR>
-__device__ __forceinline__ int slot_of() {
-    if constexpr (TPR > 64) return 0;
-    const int slot = threadIdx.x / TPR;
-    return TPR == 64 ? __builtin_amdgcn_readfirstlane(slot) : slot;
-}
-
 constexpr int kCols = 8;  // columns of a thread: one call of the generator
+
+// Threads of a block that has rows of TPR threads: forward, and backward, where a block's rows share what it writes of its sums
+// (3950 x 1024 bf16, layer norm, with one row a block: 31.7 us).
 template <int TPR>
 constexpr int block_of() {
     return TPR <= 64 ? 256 : TPR;
 }
-// The threads a block is launched with: of TPR those whose waves a row needs (3674 x 5240 fp16, forward: 58 us with all 1024).
 template <int TPR>
+constexpr int back_block_of() {
+    return TPR <= 64 ? 256 : TPR == 192 ? 384 : TPR <= 256 ? 512 : TPR;
+}
+// The threads it is launched with: where it has one row, the waves that this needs (3674 x 5240 fp16, forward, with all 1024: 58 us
+// for 33).
+template <int TPR, int NT>
 int threads_of(int64_t cols) {
-    return TPR <= 64 ? 256 : (int)((cols + 64 * kCols - 1) / (64 * kCols)) * 64;
+    return NT > TPR ? NT : (int)((cols + 64 * kCols - 1) / (64 * kCols)) * 64;
+}
+
+// Which of a block's rows a thread is at: a number that the compiler knows to be a wave's where it is.
+template <int TPR, int NT>
+__device__ __forceinline__ int slot_of() {
+    if constexpr (NT == TPR) return 0;
+    const int slot = threadIdx.x / TPR;
+    return TPR >= 64 ? __builtin_amdgcn_readfirstlane(slot) : slot;
 }
 
 // A vector's values from the `skip`-th on.  The few are stored one by one in a loop: unrolled, with a branch for each, a kernel's
@@ -498,8 +508,8 @@ struct Way {
 template <typename T, int TPR, int R, bool GENERAL>
 __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a) {
     constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
-    __shared__ float2 lds[2 * TPR / 16];
-    RowJoiner<TPR> join(lds);
+    __shared__ float2 lds[RowJoiner<TPR, SLOTS>::size];
+    RowJoiner<TPR, SLOTS> join(lds);
     auto mine = [&](int r) __attribute__((always_inline)) { return Columns<TPR>(a.cols, r); };
     const uint64_t offset = drop_offset(a.drop);
     const float inv = 1.0f / (float)a.cols;
@@ -511,7 +521,7 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
         if constexpr (GENERAL) mine(r).parameters_of(a.b2, 0.0f, b2[r]);
     }
     int64_t group_end = 0;
-    for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
+    for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR, NT>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
         Words<T, V> x[R], h[R] = {};
 #pragma unroll
         for (int r = 0; r < R; r++) {
@@ -592,16 +602,17 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
 // sums stay in its registers.  Chunks are those of columns_kernel.  Over a group of gate's rows
 //     A = sum drop(dt) hn,  B = sum drop(dt)   give   dw1 = s g A,  db1 = s g B,  dg = s (w1 A + b1 B).
 template <typename T, int TPR, bool GENERAL, bool PART>
-__global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL || sizeof(T) == 2 : !GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
-    constexpr int V = kCols, NT = block_of<TPR>(), SLOTS = NT / TPR;
-    __shared__ float2 lds[2 * TPR / 16];
+__global__ __launch_bounds__(back_block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL || sizeof(T) == 2 : !GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
+    constexpr int V = kCols, NT = back_block_of<TPR>(), SLOTS = NT / TPR;
+    constexpr bool PACE = SLOTS > 1 && TPR > 64;  // barriers, at which all slots of the block meet
+    __shared__ float2 lds[RowJoiner<TPR, SLOTS>::size];
     extern __shared__ float room[];
-    RowJoiner<TPR> join(lds);
+    RowJoiner<TPR, SLOTS> join(lds);
     const Columns<TPR> mine(a.cols);
     const uint64_t offset = drop_offset(a.drop);
     const float inv = 1.0f / (float)a.cols;
     const float inv_a = a.pre == BYZ_NORM_LAYER ? inv : 0.0f, inv_b = a.post == BYZ_NORM_LAYER ? inv : 0.0f;
-    const int slot = slot_of<TPR>();
+    const int slot = slot_of<TPR, NT>();
     float sum_w2[V] = {}, sum_b2[V] = {}, sum_a[V] = {}, sum_b[V] = {}, bias[V];
     // A thread's own weights in LDS, read where they are used: in registers they would take sixteen.
     enum { kWay, kPre };
@@ -638,8 +649,9 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
         l.dout = mine.template get<T>(dout_at, row, dout_ld);
         return l;
     };
-    // The row that l has; the next one is loaded meanwhile.
-    auto work = [&](Loaded &l, int64_t row, int64_t next) __attribute__((always_inline)) {
+    // The row that l has; the next one is loaded meanwhile.  Of a row that is not the slot's (its waves only keep pace with those of
+    // others) nothing is in a sum or written.
+    auto work = [&](Loaded &l, int64_t row, int64_t next, bool active) __attribute__((always_inline)) {
         const Words<T, V> x = l.x;
         Words<T, V> h = l.h, dout = l.dout, dy = l.dy;
         const Stats s = l.s;
@@ -647,10 +659,13 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
         float keep[V], tn[V], w2[V], way[V];
         fetch(kWay, way), fetch(kPre, w2);
         mine.kept(a, offset, row, keep);
-        if (!b.dy) dy = {};
+        if (!b.dy || (PACE && !active)) dy = {};
         if (!b.dout) dout = {};
         if (!a.h) h = {};
         mine.only_own(dy);
+        if (PACE && !active)
+#pragma unroll
+            for (int e = 0; e < V; e++) keep[e] = 0.0f;
         drop_first(a, h, keep);
         auto hn = [&](int e) { return GENERAL ? (h[e] - s.mean1) * s.rstd1 : h[e] * s.rstd1; };
         float p1 = 0.0f, p2 = 0.0f;
@@ -681,7 +696,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
             sum_w2[e] = fmaf(dy[e], tn[e], sum_w2[e]);
             if constexpr (GENERAL) sum_b2[e] += dy[e];
         }
-        mine.template put<T>(b.dx, row, b.dx_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
+        if (!PACE || active) mine.template put<T>(b.dx, row, b.dx_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
         fetch(kWay, way);
 #pragma unroll
         for (int e = 0; e < V; e++) {
@@ -700,7 +715,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
 #pragma unroll
             for (int e = 0; e < V; e++) dt[e] = fmaf(hn(e), mean_bhn, GENERAL ? fmaf(s.rstd1, dt[e], mean_b) : s.rstd1 * dt[e]);
         }
-        mine.template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
+        if (!PACE || active) mine.template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[e]; }));
     };
     // some of a group's rows (PART), or whole groups for each slot
     const int64_t chunk = blockIdx.x, group_rows = a.gate_rows;
@@ -711,7 +726,14 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
 #pragma unroll
         for (int e = 0; e < V; e++) own[e] = own[NT * V + e] = 0.0f;
     }
-    for (; group < (PART ? group + 1 : b.groups); group += (int64_t)gridDim.x * SLOTS) {
+    // with PACE every slot of a block goes through as many rows
+    for (int64_t base = PART ? group : chunk * SLOTS; base < (PART ? base + 1 : b.groups); base += (int64_t)gridDim.x * SLOTS) {
+        if constexpr (!PART) group = base + slot;
+        const bool there = group < b.groups;
+        if (!there) {
+            if constexpr (!PACE) break;
+            group = b.groups - 1;
+        }
         {
             const Way<TPR, GENERAL> way(a, mine, group);
             store(kWay, way.w);
@@ -720,10 +742,13 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
                 for (int e = 0; e < V; e++) bias[e] = way.b[e];
         }
         const int64_t end = std::min(a.rows, (group + 1) * group_rows), step = PART ? (int64_t)b.per_group * SLOTS : 1;
-        int64_t row = group * group_rows + (PART ? blockIdx.x % b.per_group * SLOTS + slot : 0);
-        if (row < end) {
-            Loaded l = load(row);
-            for (; row < end; row += step) work(l, row, row + step < end ? row + step : row);
+        const int64_t start = group * group_rows + (PART ? blockIdx.x % b.per_group * SLOTS : 0);
+        const int64_t most = PART ? end : start + group_rows;  // where the slot with most rows ends
+        int64_t row = start + (PART ? slot : 0);
+        if (PACE ? start < most : row < end) {
+            Loaded l = load(std::min(row, end - 1));
+            for (int64_t at = PACE ? start : row; at < (PACE ? most : end); at += step, row += step)
+                work(l, PACE ? std::min(row, end - 1) : row, std::min(row + step, end - 1), !PACE || (there && row < end));
         }
         // the sums of a group's rows make those of its vectors
         float g[V], w1[V], b1[V];
@@ -737,7 +762,7 @@ __global__ __launch_bounds__(block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL ||
             w1_sum[e] = factor * g[e] * sum_a[e], b1_sum[e] = factor * g[e] * sum_b[e];
         }
         if constexpr (PART) break;
-        if (b.d_gate) mine.template put<float>(b.d_gate, group, a.cols, Words<float, V>::of([&](int e) { return gate_sum[e]; }));
+        if (b.d_gate && there) mine.template put<float>(b.d_gate, group, a.cols, Words<float, V>::of([&](int e) { return gate_sum[e]; }));
 #pragma unroll
         for (int e = 0; e < V; e++) own[e] += w1_sum[e], own[NT * V + e] += b1_sum[e], sum_a[e] = sum_b[e] = 0.0f;
     }
@@ -824,6 +849,7 @@ int with_threads(int64_t cols, F fn) {
     if (threads <= 32) return fn(std::integral_constant<int, 32>{});
     if (threads <= 64) return fn(std::integral_constant<int, 64>{});
     if (threads <= 128) return fn(std::integral_constant<int, 128>{});
+    if (threads <= 192) return fn(std::integral_constant<int, 192>{});
     if (threads <= 256) return fn(std::integral_constant<int, 256>{});
     if (threads <= 512) return fn(std::integral_constant<int, 512>{});
     return fn(std::integral_constant<int, 1024>{});
@@ -838,8 +864,8 @@ struct Cut {
         int64_t blocks = 512, least = 4;
         if (in_registers(cols))
             with_threads(cols, [&](auto tpr) -> int {
-                constexpr int TPR = tpr.value;
-                blocks = kCus * (1024 / threads_of<TPR>(cols)), least = kLeast * (block_of<TPR>() / TPR);
+                constexpr int TPR = tpr.value, NT = back_block_of<TPR>();
+                blocks = kCus * (1024 / threads_of<TPR, NT>(cols)), least = kLeast * (NT / TPR);
                 return 0;
             });
         const int64_t want = std::max(least, (rows + blocks - 1) / blocks);
@@ -876,8 +902,8 @@ int launch_forward(const Args &a, hipStream_t s) {
     }
     if (in_registers(a.cols)) {
         return with_threads(a.cols, [&](auto tpr) -> int {
-            constexpr int TPR = tpr.value, slots = block_of<TPR>() / TPR;
-            const int threads = threads_of<TPR>(a.cols);
+            constexpr int TPR = tpr.value, NT = block_of<TPR>(), slots = NT / TPR;
+            const int threads = threads_of<TPR, NT>(a.cols);
             const int64_t blocks = std::min((a.rows + slots - 1) / slots, (int64_t)kCus * (2048 / threads));
             (general ? &forward_rows_kernel<T, TPR, 1, true> : &forward_rows_kernel<T, TPR, 1, false>)<<<(unsigned)blocks, threads, 0, s>>>(a);
             BYZ_HIP(hipGetLastError());
@@ -898,13 +924,13 @@ int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, h
     const bool general = a.b1 || (b.kinds & (1u << kB1 | 1u << kB2)) || a.post == BYZ_NORM_LAYER || a.pre == BYZ_NORM_LAYER;
     if (in_registers(a.cols) && (cut.per_group || a.cols <= kGroupsInLds)) {
         const int rc = with_threads(a.cols, [&](auto tpr) -> int {
-            constexpr int TPR = tpr.value, NT = block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
+            constexpr int TPR = tpr.value, NT = back_block_of<TPR>(), each = NT * kCols * (int)sizeof(float);
             if (cut.per_group) {
                 (general ? &backward_rows_kernel<T, TPR, true, true> : &backward_rows_kernel<T, TPR, false, true>)
-                    <<<(unsigned)cut.chunks, threads_of<TPR>(a.cols), 2 * each, s>>>(a, b);
+                    <<<(unsigned)cut.chunks, threads_of<TPR, NT>(a.cols), 2 * each, s>>>(a, b);
             } else if constexpr (TPR <= 512) {
                 (general ? &backward_rows_kernel<T, TPR, true, false> : &backward_rows_kernel<T, TPR, false, false>)
-                    <<<(unsigned)cut.chunks, threads_of<TPR>(a.cols), 4 * each, s>>>(a, b);
+                    <<<(unsigned)cut.chunks, threads_of<TPR, NT>(a.cols), 4 * each, s>>>(a, b);
             }
             BYZ_HIP(hipGetLastError());
             return BYZ_OK;

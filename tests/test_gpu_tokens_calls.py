@@ -240,3 +240,44 @@ def test_preference_of_a_padded_batch():
     for s, (a, b) in enumerate(zip(edges, edges[1:])):
         assert _same_bits(grad[a:b], grad2[s * long:s * long + b - a])
         assert bool((grad2[s * long + b - a:(s + 1) * long] == 0).all())
+
+
+@pytest.mark.parametrize("rows, gate_rows", [(13, 5), (7, 7), (7, 100), (900, 7), (3001, 1000), (40, 39)])
+@pytest.mark.parametrize("cols", [5, 40, 700, 1500, 4000, 8000, 9000])
+def test_groups_of_gates_rows_that_end_early(cols, rows, gate_rows):
+    """The C call takes groups that do not divide the rows: the last one is shorter."""
+    L = worker_tokens._load()
+    groups = -(-rows // gate_rows)
+    c = _residual_case(rows, cols, BF16, "rms", "layer", 1, 0.1, seed=cols)
+    gate = 1 + _randn(_gen(cols), groups, cols, scale=0.3)
+    wide = gate.repeat_interleave(gate_rows, dim=0)[:rows].contiguous()
+
+    def run(g, n):
+        out, y, dx, dh = (torch.empty_like(c["x"]) for _ in range(4))
+        stats, grads = torch.empty(rows, 4, device=DEV), [torch.full((cols,), math.nan, device=DEV) for _ in range(3)]
+        d_gate = torch.full_like(g, math.nan)
+        p = lambda t: t.data_ptr()  # noqa: E731
+        assert L.byz_residual_norm(p(c["x"]), cols, p(c["h"]), cols, rows, cols, 1, c["form"], p(c["w1"]), None, p(g), n, p(c["w2"]),
+                                   p(c["b2"]), p(out), cols, p(y), cols, p(stats), None) == 0
+        need = L.byz_residual_norm_backward_workspace_bytes(rows, cols, 1, n)
+        ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+        assert L.byz_residual_norm_backward(p(c["dout"]), cols, p(c["dy"]), cols, p(c["x"]), cols, p(c["h"]), cols, p(stats), rows, cols, 1,
+                                            c["form"], p(c["w1"]), None, p(g), n, p(c["w2"]), p(dx), cols, p(dh), cols, p(grads[0]), None,
+                                            p(d_gate), p(grads[1]), p(grads[2]), p(ws), need, None) == 0
+        torch.cuda.synchronize()
+        return out, y, stats, dx, dh, grads, d_gate
+
+    got, want = run(gate, gate_rows), run(wide, 1)
+    for a, b in zip(got[:3], want[:3]):
+        assert _same_bits(a, b)
+    # gate_rows is one of a call's sizes, which other kernels may take: both results are within half a step of bf16 (2^-8) of values
+    # that some dozens of fp32 roundings of a row's largest ones, 64 at most, are apart
+    for a, b in zip(got[3:5], want[3:5]):
+        assert bool(((a.double() - b.double()).abs() <= 2 * 2.0 ** -8 * b.double().abs() + 64 * 2.0 ** -24 * 64).all())
+    # sums over the rows in another order: some dozens of roundings of what they are made of, of which dx, dh and y are the scale
+    for a, b in zip(got[5], want[5]):
+        assert float((a - b).abs().max()) <= 64 * 2.0 ** -24 * rows * 16
+    each = want[6].double()
+    for g in range(groups):
+        part = each[g * gate_rows:(g + 1) * gate_rows]
+        assert bool(((got[6][g].double() - part.sum(0)).abs() <= 64 * 2.0 ** -24 * part.abs().sum(0) + 1e-30).all())
