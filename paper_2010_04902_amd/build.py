@@ -56,7 +56,7 @@ def _build_module(target, source, verbose):
 
 
 def build(verbose=False):
-    """Always compiles (about six and a half minutes on 8 cores); raises where the library does not build."""
+    """Always compiles (about seven minutes on 8 cores); raises where the library does not build."""
     sys.path.insert(0, CSRC)
     try:
         import gen_selnet

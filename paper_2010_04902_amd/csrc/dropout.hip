@@ -1,8 +1,11 @@
 // Dropout whose mask is made where it is used (gfx950): y = x scale where a value stays, else 0.  Its gradient is the same call.
 //
-// Bound by memory: a value in, a value out.  The generator's ten rounds for eight values take about half of the
-// instruction slots that reading and writing eight bf16 values leave.  A thread does groups of eight columns, numbered over
-// rows and groups alike, so rows shorter than a wave leave no lanes idle.
+// Bound by memory: a value in, a value out; with 16-bit types the generator's ten rounds for eight values keep the vector units 0.69 of
+// the time busy.  Groups of eight columns are numbered over rows and groups alike, so rows shorter than a wave leave no lanes idle; a
+// thread does two.  Results go through the caches: stored past them 8192 x 16384 bf16 took 76 us alone, but 190 with an operation
+// behind it that reads the result, for 90 and 179.
+//
+// 8192 x 16384 bf16 90 us (5.9 TB/s), fp32 191 to 237; 70000 x 1517 bf16, rows at odd addresses, 97 (4.4 TB/s); 30 x 512 3.1.
 #include <algorithm>
 
 #include "drop.h"

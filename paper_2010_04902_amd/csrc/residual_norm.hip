@@ -7,6 +7,16 @@
 //     dt = dout + rstd2 (a - mean a - tn mean(a tn)),  du = s g drop(dt),  dx = dt
 //     dh = rstd1 (b - mean b - hn mean(b hn)),  b = du w1
 //     dw2 = sum dy tn,  db2 = sum dy,  dw1 = sum du hn,  db1 = sum du,  dg = sum s drop(u) dt
+//
+// Bound by memory where rows are many: four tensors forward, six backward, each once.  Rows of 8 to 8192 columns (16384 forward) are held
+// in registers, eight columns a thread, which is one call of the generator: a row is part of a wave, a wave, or up to 1024 threads.
+// Backward a thread also sums its columns over the rows of its block; the blocks' sums are joined by finish_kernel.  Narrower and wider
+// rows, and gates of a few rows each on more than 4096 columns, take kernels that read a row up to three times and the
+// columns' sums by a second reading.  Short calls are bound by one row's chain (2 us, two reductions) and by reading the code: with
+// partial vectors unrolled a backward kernel of 15 KB took 13 us for one row; of half that length it takes 11 for two.
+//
+// 8192 x 4096 bf16, both norms RMS, gate and dropout: forward 48 us (5.6 TB/s, vector units busy 0.61), backward 91 (4.7 TB/s with the blocks'
+// sums, busy 0.57) and 6 for the join; with layer norms and biases 67 and 106 together.  1920 x 512 4.8, 10 and 5.
 #include <algorithm>
 
 #include "drop.h"
@@ -598,11 +608,18 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
     }
 }
 
+// Waves of a SIMD that the registers of backward_rows_kernel are to leave room for: four where that costs few spills or none.  us at
+// four and at two: 8192 x 4096 bf16 with layer norms 106 and 127.
+template <typename T>
+constexpr int back_waves(int tpr, bool general, bool part) {
+    return tpr == 1024 || (sizeof(T) == 2 && (part || !general)) || (part && !general) ? 4 : 2;
+}
+
 // dx and dh of a chunk's rows, and the chunk's sums of the columns: a thread has eight columns of every row of its slot, whose
 // sums stay in its registers.  Chunks are those of columns_kernel.  Over a group of gate's rows
 //     A = sum drop(dt) hn,  B = sum drop(dt)   give   dw1 = s g A,  db1 = s g B,  dg = s (w1 A + b1 B).
 template <typename T, int TPR, bool GENERAL, bool PART>
-__global__ __launch_bounds__(back_block_of<TPR>(), TPR == 1024 || (PART ? !GENERAL || sizeof(T) == 2 : !GENERAL && sizeof(T) == 2) ? 4 : 2) void backward_rows_kernel(Args a, Back b) {
+__global__ __launch_bounds__(back_block_of<TPR>(), back_waves<T>(TPR, GENERAL, PART)) void backward_rows_kernel(Args a, Back b) {
     constexpr int V = kCols, NT = back_block_of<TPR>(), SLOTS = NT / TPR;
     constexpr bool PACE = SLOTS > 1 && TPR > 64;  // barriers, at which all slots of the block meet
     __shared__ float2 lds[RowJoiner<TPR, SLOTS>::size];
