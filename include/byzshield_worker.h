@@ -6,7 +6,7 @@
  * the same values give the same bits, wherever their tensors lie and whatever their pitches are (no
  * atomics, every sum in a fixed order, launch shapes chosen by sizes and type alone).  A file within a
  * call of more rows or samples is a call of other sizes: copies have to be computed by calls alike.
- * None mixes the samples of a file, and all of them enqueue work and nothing else.
+ * None mixes the samples of a file (the preference loss those of a pair alone), and all of them enqueue work and nothing else.
  *
  * Conventions (beyond those of byzshield.h)
  *   - Device pointers of the current device; `stream` is a hipStream_t passed as void*.  No

@@ -367,8 +367,13 @@ struct RowJoiner {
         return v;
     }
     __device__ __forceinline__ float2 sum(float a, float b) {
-        constexpr int own = TPR >= 64 ? 6 : TPR == 32 ? 5 : 4;
-        float2 v = lanes<own>(make_float2(a, b));
+        constexpr int own = TPR >= 64 ? 6 : TPR == 32 ? 5 : TPR == 16 ? 4 : 2;
+        float2 v = make_float2(a, b);
+        if constexpr (TPR == 8) {  // the eight lanes' mirror image; their halves then have the same four sums
+            v.x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v.x), 0x141, 0xf, 0xf, true));
+            v.y += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v.y), 0x141, 0xf, 0xf, true));
+        }
+        v = lanes<own>(v);
         if constexpr (waves > 1) {
             float2 *at = lds + turn * places;
             turn ^= 1;
@@ -862,6 +867,7 @@ bool in_registers(int64_t cols) { return cols >= kCols && cols <= kRowsInRegiste
 template <typename F>
 int with_threads(int64_t cols, F fn) {
     const int64_t threads = (cols + kCols - 1) / kCols;
+    if (threads <= 8) return fn(std::integral_constant<int, 8>{});
     if (threads <= 16) return fn(std::integral_constant<int, 16>{});
     if (threads <= 32) return fn(std::integral_constant<int, 32>{});
     if (threads <= 64) return fn(std::integral_constant<int, 64>{});
