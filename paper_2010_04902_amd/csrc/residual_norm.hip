@@ -816,6 +816,103 @@ __global__ __launch_bounds__(back_block_of<TPR>(), back_waves<T>(TPR, GENERAL, P
     if constexpr (PART) write(kGate, gate_sum);
 }
 
+// dx, dh and the means of rows of 8193 to 16384 columns of 16 bits, root mean squares only and without additions: sixteen columns a
+// thread, in registers from the one read that rows_kernel does three times.  Their sums would not fit beside them and are
+// columns_kernel's.  Of the other norms and of fp32 the registers spill: rows_kernel's.  us on 2048 x 16384 bf16: 110 against rows_kernel's
+// 170; with layer norms 344 against 306 (both with the sums, 3000 x 9001 fp16), fp32 173 against 160 (1024 x 16384).
+template <typename T>
+__global__ __launch_bounds__(1024, 4) void wide_rows_kernel(Args a, Back b) {
+    constexpr int V = kCols, R = 2, TPR = 1024;
+    __shared__ float2 lds[RowJoiner<TPR, 1>::size];
+    RowJoiner<TPR, 1> join(lds);
+    auto mine = [&](int r) __attribute__((always_inline)) { return Columns<TPR>(a.cols, r); };
+    const uint64_t offset = drop_offset(a.drop);
+    const float inv = 1.0f / (float)a.cols;
+    float w2[R][V];
+    Way<TPR, false> way[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) mine(r).parameters_of(a.w2, 1.0f, w2[r]);
+    int64_t group_end = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        Words<T, V> x[R], h[R] = {}, dout[R] = {}, dy[R] = {};
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            x[r] = mine(r).template get<T>(a.x, row, a.x_ld);
+            if (a.h) h[r] = mine(r).template get<T>(a.h, row, a.h_ld);
+            if (b.dy) dy[r] = mine(r).template get<T>(b.dy, row, b.dy_ld);
+            if (b.dout) dout[r] = mine(r).template get<T>(b.dout, row, b.dout_ld);
+        }
+        const Stats s = stats_of(b.stats, row);
+        if (row >= group_end) {
+            const int64_t group = group_of(a, row);
+#pragma unroll
+            for (int r = 0; r < R; r++) way[r] = Way<TPR, false>(a, mine(r), group);
+            group_end = (group + 1) * a.gate_rows;
+        }
+        uint32_t mask[R];
+        auto hn = [&](int r, int e) { return h[r][e] * s.rstd1; };
+        auto kept = [&](int r, int e) { return mask[r] >> e & 1 ? 1.0f : 0.0f; };
+        auto tn = [&](int r, int e) {
+            const float t = a.h ? fmaf(way[r].of(e, hn(r, e)), kept(r, e), x[r][e]) : x[r][e];
+            return t * s.rstd2;
+        };
+        auto unpack_again = [&](int r) __attribute__((always_inline)) { x[r].keep(), h[r].keep(), dout[r].keep(), dy[r].keep(); };
+        float p2 = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            float keep[V];
+            mine(r).kept(a, offset, row, keep);
+            mine(r).only_own(dy[r]);
+            drop_first(a, h[r], keep);
+            mask[r] = 0;
+#pragma unroll
+            for (int e = 0; e < V; e++) mask[r] |= keep[e] != 0.0f ? 1u << e : 0u;
+#pragma unroll
+            for (int e = 0; e < V; e++) p2 = fmaf(dy[r][e] * w2[r][e], tn(r, e), p2);
+            unpack_again(r);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        float mean_atn = 0.0f;
+        if (b.dy) mean_atn = join.sum(0.0f, p2).y * inv;
+        float dt[R][V], p4 = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                dt[r][e] = dout[r][e];
+                if (b.dy) {
+                    dt[r][e] = fmaf(s.rstd2, dy[r][e] * w2[r][e], dt[r][e]);
+                    dt[r][e] = fmaf(tn(r, e), -s.rstd2 * mean_atn, dt[r][e]);
+                }
+            }
+            mine(r).template put<T>(b.dx, row, b.dx_ld, Words<T, V>::of([&](int e) { return dt[r][e]; }));
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                dt[r][e] *= kept(r, e) * way[r].w[e];
+                p4 = fmaf(dt[r][e], hn(r, e), p4);
+            }
+            h[r].keep();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        float mean_bhn = 0.0f;
+        if (a.h) {
+            if (a.post != BYZ_NORM_NONE) mean_bhn = join.sum(0.0f, p4).y * inv;
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+                if (a.post != BYZ_NORM_NONE) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) dt[r][e] = fmaf(hn(r, e), -s.rstd1 * mean_bhn, s.rstd1 * dt[r][e]);
+                }
+                mine(r).template put<T>(b.dh, row, b.dh_ld, Words<T, V>::of([&](int e) { return dt[r][e]; }));
+            }
+        }
+        if (threadIdx.x == 0) {
+            float *at = b.rest + row * 4;
+            at[0] = 0.0f, at[1] = mean_atn, at[2] = 0.0f, at[3] = mean_bhn;
+        }
+    }
+}
+
 struct Outputs {
     float *of[kKinds];
 };
@@ -884,7 +981,7 @@ constexpr int64_t kLeast = 2;  // us at 2, 4, 8: backward of 333 x 1000 fp32 18,
 struct Cut {
     int64_t per_group, groups, chunks;
     Cut(int64_t rows, int64_t cols, int64_t gate_rows) {
-        int64_t blocks = 512, least = 4;
+        int64_t blocks = std::max<int64_t>(8, 8 * kCus / ((cols + 511) / 512)), least = 4;  // columns_kernel's, times its 512 columns
         if (in_registers(cols))
             with_threads(cols, [&](auto tpr) -> int {
                 constexpr int TPR = tpr.value, NT = back_block_of<TPR>();
@@ -960,10 +1057,14 @@ int launch_backward(const Args &a, Back b, const Cut &cut, const Outputs &out, h
         });
         if (rc != BYZ_OK) return rc;
     } else {
-        if (a.cols > kGroupsInLds && a.rows < kCus)
+        const bool wide = sizeof(T) == 2 && !general && a.cols > kRowsInRegisters && a.cols <= 2 * kRowsInRegisters;
+        if (wide) {
+            if constexpr (sizeof(T) == 2) wide_rows_kernel<T><<<(unsigned)std::min<int64_t>(a.rows, kCus * 2), 1024, 0, s>>>(a, b);
+        } else if (a.cols > kGroupsInLds && a.rows < kCus) {
             rows_kernel<T, 1024><<<(unsigned)std::min(a.rows, kMaxGrid), 1024, 0, s>>>(a, b);
-        else
+        } else {
             rows_kernel<T, 256><<<(unsigned)std::min(a.rows, kMaxGrid), 256, 0, s>>>(a, b);
+        }
         BYZ_HIP(hipGetLastError());
         if (!b.kinds && !b.d_gate) return BYZ_OK;
         columns_kernel<T><<<dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), (unsigned)cut.chunks), 256, 0, s>>>(a, b);

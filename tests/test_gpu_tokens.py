@@ -229,6 +229,33 @@ def test_norm_alone(rows, cols, dtype):
         _residual_check(got, want, dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, cols, gate", [(3, 8193, 1), (42, 9001, 7), (600, 8200, 150), (9, 12288, 9), (2, 16384, 1), (700, 16383, 1),
+                                              (3, 16385, 1)])
+def test_residual_wide_rows_of_root_mean_squares(rows, cols, gate, dtype):
+    for post, pre, dout, dy in (("rms", "rms", True, True), ("none", "rms", True, True), ("rms", "none", True, False),
+                                ("rms", "rms", False, True), ("rms", "rms", True, False)):
+        c = _residual_case(rows, cols, dtype, post, pre, gate, 0.2, bias=False, seed=rows)
+        _residual_check(_residual_run(c, dout=dout, dy=dy), _residual_want(c, post, pre, 0.2, dout, dy), dtype)
+        if rows > 9:
+            break
+    c = _residual_case(rows, cols, dtype, "none", "rms", 0, 0.0, bias=False)
+    c["h"] = c["w1"] = c["b1"] = None
+    got = _residual_run(c)
+    got.pop("out")
+    _residual_check(got, _residual_want(c, "none", "rms", 0.0), dtype)
+
+
+def test_residual_wide_rows_anywhere_and_twice():
+    c = _residual_case(600, 9001, BF16, "rms", "rms", 200, 0.1, bias=False)
+    dense = _residual_run(c)
+    moved = dict(c)
+    for name in ("x", "h", "dout", "dy"):
+        moved[name] = torch.full((600, 9006), math.nan, dtype=BF16, device=DEV)[:, 3:9004].copy_(c[name])
+    for got in (_residual_run(moved), _residual_run(c)):
+        assert all(_same_bits(got[name], dense[name]) for name in dense)
+
+
 def test_residual_one_gradient_alone():
     for dout, dy in ((True, False), (False, True)):
         for rows, cols in ((20, 300), (2, 9000)):
