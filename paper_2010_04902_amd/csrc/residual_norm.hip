@@ -530,10 +530,14 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
     const float inv = 1.0f / (float)a.cols;
     float w2[R][V], b2[R][V];
     Way<TPR, GENERAL> way[R];
-#pragma unroll
-    for (int r = 0; r < R; r++) {
+    constexpr bool HELD = R == 1 || !GENERAL;  // the second norm's parameters fit into the registers too
+    auto second = [&](int r) __attribute__((always_inline)) {
         mine(r).parameters_of(a.w2, 1.0f, w2[r]);
         if constexpr (GENERAL) mine(r).parameters_of(a.b2, 0.0f, b2[r]);
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int r = 0; r < R; r++) second(r);
     }
     int64_t group_end = 0;
     for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot_of<TPR, NT>(); row < a.rows; row += (int64_t)gridDim.x * SLOTS) {
@@ -601,10 +605,12 @@ __global__ __launch_bounds__(block_of<TPR>(), 4) void forward_rows_kernel(Args a
         if (a.pre != BYZ_NORM_NONE) {
             moments(a.pre, s.mean2, s.rstd2, [&](int r, int e) { return t[r][e]; });
 #pragma unroll
-            for (int r = 0; r < R; r++)
+            for (int r = 0; r < R; r++) {
+                if constexpr (!HELD) second(r);
                 mine(r).template put<T>(a.y, row, a.y_ld, Words<T, V>::of([&](int e) {
                                             return GENERAL ? fmaf((t[r][e] - s.mean2) * s.rstd2, w2[r][e], b2[r][e]) : t[r][e] * s.rstd2 * w2[r][e];
                                         }));
+            }
         }
         if (a.stats && threadIdx.x % TPR == 0) {
             float *at = a.stats + row * 4;
