@@ -11,8 +11,8 @@
 // Bound by memory where rows are many: four tensors forward, six backward, each once.  Rows of 8 to 8192 columns (16384 forward) are held
 // in registers, eight columns a thread, which is one call of the generator: a row is part of a wave, a wave, or up to 1024 threads.
 // Backward a thread also sums its columns over the rows of its block; the blocks' sums are joined by finish_kernel.  Narrower and wider
-// rows, and gates of a few rows each on more than 4096 columns, take kernels that read a row up to three times and the
-// columns' sums by a second reading.  Short calls are bound by one row's chain (2 us, two reductions) and by reading the code: with
+// rows, and gates of a few rows each on more than 4096 columns, take kernels that read a row up to three times (once up to 16384 columns of
+// 16 bits, root mean squares) and the columns' sums by a second reading.  Short calls are bound by one row's chain (2 us, two reductions) and by reading the code: with
 // partial vectors unrolled a backward kernel of 15 KB took 13 us for one row; of half that length it takes 11 for two.
 //
 // 8192 x 4096 bf16, both norms RMS, gate and dropout: forward 48 us (5.6 TB/s, vector units busy 0.61), backward 91 (4.7 TB/s with the blocks'
@@ -824,8 +824,8 @@ __global__ __launch_bounds__(back_block_of<TPR>(), back_waves<T>(TPR, GENERAL, P
 
 // dx, dh and the means of rows of 8193 to 16384 columns of 16 bits, root mean squares only and without additions: sixteen columns a
 // thread, in registers from the one read that rows_kernel does three times.  Their sums would not fit beside them and are
-// columns_kernel's.  Of the other norms and of fp32 the registers spill: rows_kernel's.  us on 2048 x 16384 bf16: 110 against rows_kernel's
-// 170; with layer norms 344 against 306 (both with the sums, 3000 x 9001 fp16), fp32 173 against 160 (1024 x 16384).
+// columns_kernel's.  Of the other norms and of fp32 the registers spill: rows_kernel's.  us of a whole backward pass, so and with
+// rows_kernel: 2048 x 16384 bf16 200 and 260; with layer norms 284 and 255, 3000 x 9001 of them 344 and 257, 1024 x 16384 fp32 240 and 215.
 template <typename T>
 __global__ __launch_bounds__(1024, 4) void wide_rows_kernel(Args a, Back b) {
     constexpr int V = kCols, R = 2, TPR = 1024;
@@ -982,12 +982,13 @@ int with_threads(int64_t cols, F fn) {
 }
 
 // How the rows are cut for the sums of columns: chunks for sixteen waves a compute unit, but of two rows a slot at least, each
-// within a group of gate's rows, or of whole groups where these are short.
+// within a group of gate's rows, or of whole groups where these are short.  columns_kernel's blocks, of 512 columns of 16 bits each, are some
+// eight a compute unit: with 512 chunks whatever the width, backward of 2048 x 16384 bf16 took 68 us more, 1024 x 40000 78 more.
 constexpr int64_t kLeast = 2;  // us at 2, 4, 8: backward of 333 x 1000 fp32 18, 23, 33, of 3950 x 604 bf16 30, 29, 36
 struct Cut {
     int64_t per_group, groups, chunks;
     Cut(int64_t rows, int64_t cols, int64_t gate_rows) {
-        int64_t blocks = std::max<int64_t>(8, 8 * kCus / ((cols + 511) / 512)), least = 4;  // columns_kernel's, times its 512 columns
+        int64_t blocks = std::max<int64_t>(8, 8 * kCus / ((cols + 511) / 512)), least = 4;
         if (in_registers(cols))
             with_threads(cols, [&](auto tpr) -> int {
                 constexpr int TPR = tpr.value, NT = back_block_of<TPR>();
