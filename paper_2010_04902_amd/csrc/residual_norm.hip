@@ -122,7 +122,8 @@ struct Piece {
         kept = a.drop.threshold ? DropV<V>(a.drop, offset, (uint32_t)row, (uint32_t)col).mask : ~0u;
 #pragma unroll
         for (int e = 0; e < V; e++) {
-            hn[e] = (h[e] - s.mean1) * s.rstd1;
+            // without a norm, whose sums it would be in, what is dropped may be no number: it is in no product below
+            hn[e] = a.post == BYZ_NORM_NONE && !(kept >> e & 1) ? 0.0f : (h[e] - s.mean1) * s.rstd1;
             v[e] = kept >> e & 1 ? fmaf(hn[e], w1[e], b1[e]) * a.drop.scale : 0.0f;
             sg[e] *= a.scale;
             t[e] = e < n ? fmaf(sg[e], v[e], x[e]) : 0.0f;
