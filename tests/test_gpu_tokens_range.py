@@ -1,11 +1,13 @@
-"""The token operators at the ends of their values' range."""
+"""The token operators at the ends of their values' range: dropped values that are no numbers, and the statistics of rows whose largest
+values lie anywhere."""
 import math
 
 import pytest
 import torch
 
-from test_gpu_tokens import DEV, TYPES, _residual_case, _residual_run, _same_bits
-from token_forms import kept
+import paper_2010_04902_amd as B
+from test_gpu_tokens import DEV, TYPES, _gen, _near, _randn, _residual_case, _residual_run, _same_bits, _u
+from token_forms import E, kept, logp_terms
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +29,110 @@ def test_dropped_values_reach_no_gradient(rows, cols, gate, dtype):
                 assert got.keys() == want.keys() and "d_post_weight" in got
                 for name in want:
                     assert _same_bits(got[name], want[name]), (pre, bias, value, name)
+
+
+# ------------------------------------------------------------------ rows of losses
+
+# one vocabulary at least for each way of holding a row of each type, and those beside it
+HELD = [(1, 1), (3, 5), (5, 100), (6, 900), (9, 2047), (7, 4100), (5, 8192), (3, 9001), (6, 20011), (40, 32000), (4, 50021), (130, 33000),
+        (130, 66001), (3, 140001)]
+
+
+def _sum_tol(vocab, dtype):
+    """A sum of exponentials, relative: a thread has vocab / (256 V) vectors of V values at most, each of whose sums is rounded once
+    beside the thread's; 7 roundings within a vector, 3 at each of 10 joins of threads, 3 of a power, 8 of the logarithm."""
+    return (vocab / (256 * 128 / torch.finfo(dtype).bits) + 48) * E
+
+
+def _stats_check(stats, z, label, temperature):
+    """The row's largest logit is one of its values, so exactly that."""
+    d = z.double()
+    top = d.amax(1)
+    total = ((d - top[:, None]) / temperature).exp().sum(1).log()
+    none = label < 0
+    _near(stats[:, 0], torch.where(none, 0.0, top), torch.zeros_like(top), "largest logit")
+    _near(stats[:, 1], torch.where(none, 0.0, total), _sum_tol(z.shape[1], z.dtype) + 2 * E * total, "log-sum")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", HELD)
+def test_statistics_are_those_of_the_row(rows, vocab, dtype):
+    z = _randn(_gen(vocab), rows, vocab, dtype=dtype, scale=3.0)
+    label = torch.arange(rows, dtype=torch.int32, device=DEV) * 7 % vocab
+    if rows > 2:
+        label[1] = -1
+    zeros = torch.zeros(rows, device=DEV)
+    bounds = torch.tensor([0, rows // 2, rows], dtype=torch.int32, device=DEV)
+    for temperature in (1.0, 0.7):
+        _stats_check(B.byz_token_logp(z, label, temperature)[1], z, label, temperature)
+        _stats_check(B.byz_policy_loss(z, label, zeros, zeros, temperature=temperature)[2], z, label, temperature)
+        _stats_check(B.byz_preference_loss(z, label, bounds, temperature=temperature)[3], z, label, temperature)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", HELD)
+def test_a_large_value_anywhere(rows, vocab, dtype):
+    """A label far above the rest, wherever it lies: at 40 and more the rest does not reach the sum's last bit, so the sum is
+    exactly 1, logp is off by one rounding of the sum at most, and the gradient by that and its exponents' rounding."""
+    gen = _gen(vocab)
+    rest = _randn(gen, rows, vocab, scale=0.5)
+    places = torch.tensor([vocab - 1, vocab // 2, 0, vocab - 9, 3 * vocab // 4, vocab - 2, vocab // 3], device=DEV).clamp_min(0)
+    at = places[torch.arange(rows, device=DEV) % len(places)]
+    label = at.to(torch.int32)
+    every = torch.arange(rows, device=DEV)
+    d = _randn(gen, rows)
+    for peak in (44.0, 60.0, 84.0, 120.0):
+        z = rest.clone()
+        z[every, at] = peak
+        z = z.to(dtype)
+        want, q, hot = logp_terms(z, label, 1.0)
+        logp, stats = B.byz_token_logp(z, label)
+        assert torch.equal(stats[:, 0], z[every, at].float())
+        tol = torch.full_like(want, E)
+        _near(logp, want, tol, "logp")
+        w = d.double()
+        full = w[:, None] * (hot - q)
+        q_log = torch.where(q > 0, -q.clamp_min(1e-300).log(), 0.0)
+        # of the rest: exponents of up to q_log log2(e), rounded three times, and the power's own error
+        near = _u(dtype) * full.abs() + E * w.abs()[:, None] * torch.where(hot > 0, 4.0, q * (16 + 4 * q_log))
+        near += torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+        _near(B.byz_token_logp_backward(d, z, label, stats), full, near, "dlogits")
+        # the step at advantage -1 and old 0: its ratio is exp(logp), so 1
+        zeros = torch.zeros(rows, device=DEV)
+        loss, logp2, grad = B.byz_policy_loss_step(z, label, zeros, zeros - 1, d, clip_low=1.0)
+        _near(logp2, want, tol, "logp of the step")
+        _near(loss, want.exp(), 4 * tol, "loss of the step")
+        _near(grad, full, near + 4 * E * full.abs(), "dlogits of the step")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(12, 40), (12, 700), (12, 3001), (12, 8192), (12, 20011), (12, 30000), (140, 33000), (140, 66001)])
+def test_rows_with_what_is_no_number(rows, vocab, dtype):
+    """NaN or +inf anywhere makes a row's log-probability and gradient NaN; banned entries anywhere weigh nothing; others stay."""
+    gen = _gen(rows + vocab)
+    z, label = _randn(gen, rows, vocab, dtype=dtype), torch.full((rows,), 17, dtype=torch.int32, device=DEV)
+    clean = z.clone()
+    for row, (place, value) in enumerate(((0, math.nan), (vocab - 1, math.nan), (vocab // 2, math.nan), (5, math.inf), (vocab - 3, math.inf))):
+        z[row, place] = value
+    z[5, :16] = z[5, 19:] = -math.inf
+    z[6, 24:] = -math.inf  # whole threads and waves have nothing
+    z[7, :17] = -math.inf
+    z[8] = -math.inf
+    z[9] = -math.nan
+    ones, old = torch.ones(rows, device=DEV), torch.full((rows,), -9.0, device=DEV)
+    logp, stats = B.byz_token_logp(z, label)
+    loss, logp2, grad = B.byz_policy_loss_step(z, label, old, -ones, ones, clip_low=1.0)
+    alone = B.byz_policy_loss_backward(ones, z, label, old, -ones, stats, clip_low=1.0)
+    bad = [0, 1, 2, 3, 4, 9]
+    for t in (logp, logp2, loss):
+        assert bool(t[bad].isnan().all()) and not bool(t[[5, 6, 7, 8, 10, 11]].isnan().any())
+    for t in (grad, alone):
+        assert bool(t[bad].isnan().all()) and not bool(t[[5, 6, 7, 10, 11]].isnan().any())
+        assert bool((t[8] == 0).all())  # a ratio of 0
+        assert bool((t[5, :16] == 0).all() and (t[6, 24:] == 0).all() and (t[7, :17] == 0).all())
+    assert logp[8] == -math.inf and logp2[8] == -math.inf
+    want, _, _ = logp_terms(z[[5, 6, 7]], label[:3], 1.0)
+    _near(logp[[5, 6, 7]], want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "logp")
+    _near(logp2[[5, 6, 7]], want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "logp of the step")
+    same, _ = B.byz_token_logp(clean, label)
+    assert _same_bits(logp[10:], same[10:])
