@@ -37,6 +37,7 @@ struct Args {
     int64_t rows, vocab, ld;
     const int32_t *label;
     float temperature;
+    double per_temperature;  // its inverse: with divisions in fp64 by every thread for its row's weight a step of 8192 x 66000 bf16 took 522 us for 500
     Kind kind;
     // policy
     const float *old, *advantage, *ref;
@@ -101,7 +102,7 @@ __device__ __forceinline__ Terms finish(const Args &a, int64_t row, int32_t labe
     const bool empty = label < 0;
     if (empty || m == -INFINITY) m = 0.0f;  // no token, or nothing but banned logits (or NaN, which is in the sum)
     const double log_sum = empty ? 0.0 : log_of(sum);
-    double logp = empty ? 0.0 : label >= a.vocab ? NAN : ((double)z - (double)m) / (double)a.temperature - log_sum;
+    double logp = empty ? 0.0 : label >= a.vocab ? NAN : ((double)z - (double)m) * a.per_temperature - log_sum;
     Terms t{m, (float)log_sum, 0.0f, label};
     if (a.stats) a.stats[row * 2] = m, a.stats[row * 2 + 1] = (float)log_sum;
     if (a.logp) a.logp[row] = (float)logp;
@@ -109,7 +110,7 @@ __device__ __forceinline__ Terms finish(const Args &a, int64_t row, int32_t labe
         double loss = 0.0, slope = 0.0;
         if (!empty) policy(a, row, logp, loss, slope);
         if (a.loss) a.loss[row] = (float)loss;
-        if (a.dloss && !empty) t.w = (float)((double)a.dloss[row] * slope / (double)a.temperature);
+        if (a.dloss && !empty) t.w = (float)((double)a.dloss[row] * slope * a.per_temperature);
     }
     if (a.kind == kPreference) a.logp64[row] = logp;
     if (a.terms) a.terms[row] = t;
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(256) void terms_kernel(Args a) {
         } else if (a.kind == kPolicy) {
             const double z = (float)((const T *)a.logits)[row * a.ld + label];
             double loss;
-            policy(a, row, (z - (double)t.m) / (double)a.temperature - (double)t.log_sum, loss, slope);
+            policy(a, row, (z - (double)t.m) * a.per_temperature - (double)t.log_sum, loss, slope);
             slope *= (double)a.dloss[row];
         } else {
             // the last sequence that starts at this row or before; the search ends whatever the bounds are
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(256) void terms_kernel(Args a) {
             if (low < 2 * a.pairs && a.bounds[low] <= row)
                 slope = (low % 2 ? -1.0 : 1.0) * (double)a.beta * (double)a.given_slope[low / 2] * (double)a.dloss[low / 2];
         }
-        t.w = (float)(slope / (double)a.temperature);
+        t.w = (float)(slope * a.per_temperature);
     }
     a.terms[row] = t;
 }
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(256) void pairs_kernel(Args a) {
             if (a.slope) a.slope[pair] = (float)slope;
         }
         if (a.dloss && good) {
-            const double w = (double)a.beta * slope * (double)a.dloss[pair] / (double)a.temperature;
+            const double w = (double)a.beta * slope * (double)a.dloss[pair] * a.per_temperature;
             for (int64_t i = b0 + (int64_t)threadIdx.x; i < b2; i += 256)
                 if (a.terms[i].label >= 0) a.terms[i].w = (float)(i < b1 ? w : -w);
         }
@@ -325,18 +326,6 @@ __global__ __launch_bounds__(256) void gradient_kernel(Args a, int64_t parts, in
             out[edge] = round_to<T>(edge == t.label ? q.less(x, 1.0f) : q.weighted(x));
         }
     }
-}
-
-// The same weight in fp32 from a row's sum, for results of 16 bits: good to some 2^-20 of the terms it is made of, where a
-// result has 2^-9 or 2^-12, and a tenth of the instructions.
-__device__ __forceinline__ float policy_slope(const Args &a, int64_t row, float m, float sum, float z) {
-    const float advantage = a.advantage[row], log2e = 1.44269504f;
-    const float logp = (z - m) / a.temperature - __builtin_amdgcn_logf(sum) * 0.69314718f;
-    const float r = __builtin_amdgcn_exp2f((logp - a.old[row]) * log2e);
-    const bool above = advantage >= 0.0f && r > a.high, below = !(advantage >= 0.0f) && r < a.low;
-    float slope = above || below ? 0.0f * advantage : -advantage * r;
-    if (a.kl != 0.0f) slope -= a.kl * (__builtin_amdgcn_exp2f((a.ref[row] - logp) * log2e) - 1.0f);
-    return slope;
 }
 
 // The largest of G vectors in registers from the `from`-th on, from their bits, so that those of 16 bits need not be unpacked: as signed
@@ -466,14 +455,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args 
             if (tid == 0) a.terms[row] = Terms{s.m, s.s, z, label};
             if (label >= 0) {
                 if (s.m == -INFINITY) s.m = 0.0f;
-                if constexpr (sizeof(T) == 2) {
-                    const float sum = s.s == 0.0f ? 1.0f : s.s;  // of a row without anything
-                    w = label >= a.vocab ? NAN : a.dloss[row] * policy_slope(a, row, s.m, sum, z) / a.temperature;
-                } else {
-                    double loss, slope;
-                    policy(a, row, ((double)z - (double)s.m) / (double)a.temperature - log_of(s.s), loss, slope);
-                    w = label >= a.vocab ? NAN : (float)((double)a.dloss[row] * slope / (double)a.temperature);
-                }
+                double loss, slope;  // in the same steps as losses_kernel, so that loss and gradient are clipped alike
+                policy(a, row, ((double)z - (double)s.m) * a.per_temperature - log_of(s.s), loss, slope);
+                w = label >= a.vocab ? NAN : (float)((double)a.dloss[row] * slope * a.per_temperature);
             }
         } else if constexpr (NT == 64) {
             if (tid == 0) w = finish(a, row, label, s.m, s.s, z).w;
@@ -678,6 +662,7 @@ bool floats_ok(const float *p) { return aligned(p, 4); }
 Args args_of(const void *logits, int64_t rows, int64_t vocab, int64_t ld, const int32_t *label, float temperature, Kind kind) {
     Args a{};
     a.logits = logits, a.rows = rows, a.vocab = vocab, a.ld = ld, a.label = label, a.temperature = temperature, a.kind = kind;
+    a.per_temperature = 1.0 / (double)temperature;
     return a;
 }
 

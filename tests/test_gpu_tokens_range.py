@@ -1,12 +1,12 @@
-"""The token operators at the ends of their values' range: dropped values that are no numbers, and the statistics of rows whose largest
-values lie anywhere."""
+"""The token operators at the ends of their values' range: dropped values that are no numbers, the statistics of rows whose largest
+values lie anywhere, ratios next to the clipping's ends."""
 import math
 
 import pytest
 import torch
 
 import paper_2010_04902_amd as B
-from test_gpu_tokens import DEV, TYPES, _gen, _near, _randn, _residual_case, _residual_run, _same_bits, _u
+from test_gpu_tokens import DEV, F16, TYPES, _gen, _near, _randn, _residual_case, _residual_run, _same_bits, _u
 from token_forms import E, kept, logp_terms
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +136,66 @@ def test_rows_with_what_is_no_number(rows, vocab, dtype):
     _near(logp2[[5, 6, 7]], want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "logp of the step")
     same, _ = B.byz_token_logp(clean, label)
     assert _same_bits(logp[10:], same[10:])
+
+
+# ------------------------------------------------------------------ the policy loss at its ends
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(140, 500), (140, 20011), (140, 50001), (140, 66001), (140, 140000)])
+def test_ratios_next_to_the_clippings_ends(rows, vocab, dtype):
+    """The step's gradient is clipped where the ratio is past the bound, also if it is so by 2e-5 and the log-probability some
+    thousand: the sum's error of some 2^-20 at most is what may decide otherwise."""
+    gen = _gen(vocab)
+    z = _randn(gen, rows, vocab)
+    label = torch.randint(0, vocab, (rows,), generator=gen, device=DEV).to(torch.int32)
+    z[torch.arange(rows, device=DEV), label.long()] = -3008.0  # a number of every type
+    z = z.to(dtype)
+    logp, _, _ = logp_terms(z, label, 1.0)
+    ones = torch.ones(rows, device=DEV)
+    for sign, clip_low, clip_high in ((1.0, 0.2, 0.28), (-1.0, 0.2, 0.28)):
+        low, high = (float(torch.tensor(1.0) + s * torch.tensor(c)) for s, c in ((-1, clip_low), (1, clip_high)))
+        bound = high if sign > 0 else low
+        old = (logp - math.log(bound)).float()
+        away = ((logp - old.double()).exp() - bound) * sign  # more than 0: clipped
+        clear = away.abs() > 2e-5
+        assert int(clear.sum()) > rows // 2 and bool((away[clear] > 0).any()) and bool((away[clear] < 0).any())
+        _, _, grad = B.byz_policy_loss_step(z, label, old, sign * ones, ones, clip_low=clip_low, clip_high=clip_high)
+        clipped = (grad == 0).all(dim=1)
+        assert torch.equal(clipped[clear], (away > 0)[clear])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(140, 30), (140, 9001), (140, 50001), (140, 66001), (130, 140001)])
+def test_policy_loss_at_its_ends_of_long_rows(rows, vocab, dtype):
+    """Ratios of exactly 0 and infinity, advantages of 0, banned labels, labels that are none, in every kernel."""
+    z = torch.zeros(rows, vocab, dtype=dtype, device=DEV)
+    label = torch.arange(rows, dtype=torch.int32, device=DEV) % 16
+    z[3, 3] = -math.inf  # its token is banned
+    z[4] = -math.inf  # nothing is left
+    z[5] = math.nan
+    label[5] = -1
+    label[6] = vocab
+    old = torch.full((rows,), -math.log(vocab), device=DEV)
+    old[0] = math.inf  # ratio 0
+    old[1] = -math.inf  # ratio infinite
+    advantage = torch.ones(rows, device=DEV)
+    advantage[2], advantage[7] = 0.0, -1.0
+    dloss = torch.ones(rows, device=DEV)
+    loss, logp, stats = B.byz_policy_loss(z, label, old, advantage)
+    loss2, logp2, step = B.byz_policy_loss_step(z, label, old, advantage, dloss)
+    alone = B.byz_policy_loss_backward(dloss, z, label, old, advantage, stats)
+    want = torch.full((rows,), -1.0, dtype=torch.float64)
+    want[:8] = torch.tensor([0.0, -1.2, 0.0, 0.0, 0.0, 0.0, math.nan, 1.0], dtype=torch.float64)
+    # a sum of equal terms, its logarithm and old's rounding
+    for got in (loss, loss2):
+        _near(got, want, torch.full_like(want, (64 + 4 * math.log(vocab)) * E), "loss")
+    for got in (logp, logp2):
+        assert got[3] == -math.inf and got[4] == -math.inf and got[5] == 0 and bool(got[6].isnan())
+    for grad in (step, alone):
+        assert bool((grad[:6] == 0).all()) and bool(grad[6].isnan().all())
+        each = grad[8:].double().cpu()
+        hot = torch.zeros_like(each)
+        hot[torch.arange(rows - 8), label[8:].long().cpu()] = 1
+        full = 1 / vocab - hot
+        _near(each, full, _u(dtype) * full.abs() + (256 + 8 * math.log(vocab)) * E * (hot + 1 / vocab) + 2.0 ** -24 * (dtype == F16), "dlogits")
