@@ -74,14 +74,18 @@ __device__ __forceinline__ double exp_of(double d) {
     return ldexp((double)__builtin_amdgcn_exp2f((float)(y - k)), (int)k);
 }
 
-// exp(g) - 1 - g: near 0 its series
-__device__ __forceinline__ double exp_rest(double g) {
-    if (!(fabs(g) < 0.5)) return exp_of(g) - 1.0 - g;
+// exp(g) - 1, and less g: near 0 by the series of the latter.  At infinity, a token banned by the policy, both are infinite, and at
+// minus infinity, one banned by the reference, -1 and infinite.
+__device__ __forceinline__ void exp_less(double g, double &one, double &both) {
+    if (!(fabs(g) < 0.5)) {
+        one = exp_of(g) - 1.0, both = one == INFINITY ? one : one - g;
+        return;
+    }
     double s = 1.0 / 479001600;  // 1 / 12!, and down to 1 / 2!
     double f = 479001600;
 #pragma unroll
     for (int n = 12; n > 2; n--) f /= n, s = s * g + 1.0 / f;
-    return s * g * g;
+    both = s * g * g, one = both + g;
 }
 
 // The policy loss of a row and its derivative by logp.
@@ -91,9 +95,10 @@ __device__ __forceinline__ void policy(const Args &a, int64_t row, double logp, 
     loss = -advantage * (above ? (double)a.high : below ? (double)a.low : r);
     slope = above || below ? 0.0 * advantage : -advantage * r;
     if (a.kl != 0.0f) {
-        const double g = (double)a.ref[row] - logp, rest = exp_rest(g);
-        loss += (double)a.kl * rest;
-        slope -= (double)a.kl * (rest + g);
+        double one, both;
+        exp_less((double)a.ref[row] - logp, one, both);
+        loss += (double)a.kl * both;
+        slope -= (double)a.kl * one;
     }
 }
 

@@ -1,5 +1,5 @@
 """The token operators at the ends of their values' range: dropped values that are no numbers, the statistics of rows whose largest
-values lie anywhere, ratios next to the clipping's ends."""
+values lie anywhere, ratios next to the clipping's ends, banned tokens."""
 import math
 
 import pytest
@@ -199,3 +199,27 @@ def test_policy_loss_at_its_ends_of_long_rows(rows, vocab, dtype):
         hot[torch.arange(rows - 8), label[8:].long().cpu()] = 1
         full = 1 / vocab - hot
         _near(each, full, _u(dtype) * full.abs() + (256 + 8 * math.log(vocab)) * E * (hot + 1 / vocab) + 2.0 ** -24 * (dtype == F16), "dlogits")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(140, 30), (140, 9001), (140, 50001), (140, 66001), (130, 140001)])
+def test_a_token_that_the_reference_bans(rows, vocab, dtype):
+    """ref = -inf: an infinite loss whose gradient is kl (onehot - q), -kl (exp(g) - 1) being kl; and a banned token's loss is infinite."""
+    gen = _gen(vocab)
+    z = _randn(gen, rows, vocab, dtype=dtype)
+    label = torch.randint(0, vocab, (rows,), generator=gen, device=DEV).to(torch.int32)
+    z[0, label[0].long()] = -math.inf
+    _, q, hot = logp_terms(z, label, 1.0)
+    ref = torch.full((rows,), -math.inf, device=DEV)
+    ref[0] = -1.0
+    zeros, ones = torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    terms = {"ref": ref, "kl": 0.25}
+    loss, _, stats = B.byz_policy_loss(z, label, zeros, zeros, **terms)
+    loss2, _, step = B.byz_policy_loss_step(z, label, zeros, zeros, ones, **terms)
+    assert bool((loss == math.inf).all()) and bool((loss2 == math.inf).all())
+    alone = B.byz_policy_loss_backward(ones, z, label, zeros, zeros, stats, **terms)
+    full = 0.25 * (hot - q)[1:]
+    q_log = -q[1:].clamp_min(1e-300).log()
+    tol = _u(dtype) * full.abs() + E * (128 * q[1:] + 4 * q[1:] * q_log + 8 * hot[1:]) + 2.0 ** -24 * (dtype == F16)
+    for grad in (step, alone):
+        _near(grad[1:], full, tol, "dlogits")
