@@ -353,7 +353,7 @@ __device__ __forceinline__ float largest_of(const Words<T, V> (&x)[R], int from)
     over([&](uint32_t w) { most = __builtin_elementwise_max(most, __builtin_bit_cast(Ints, w)); });
     Int a = most[0];
     if constexpr (N == 2) a = std::max(a, most[1]);
-    if (a < 0) {
+    if (__builtin_expect(a < 0, false)) {
         Uints least = std::numeric_limits<Uint>::max();
         over([&](uint32_t w) { least = __builtin_elementwise_min(least, __builtin_bit_cast(Uints, w)); });
         Uint b = least[0];
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args 
                     for (int v = 0; v < R; v++) x[v] = shifted(x[v], next_word[v]);
             // A thread's sum of exp2((x - m) c), G vectors at a time, so that exponentials overlap with the loads behind them and of short
             // rows some are left out.  Its m is the largest value: with one far below that the exponents' rounding would be in the
-            // sum.  us of steps with all vectors at once and so: 750 x 32000 fp16 20.5 and 19.5, 8192 x 66000 bf16 517 and 487.
+            // sum.  us of a step of 8192 x 66000 bf16 with all vectors at once 517, so 487.
             s.m = std::numeric_limits<float>::lowest();
             auto raise_to = [&](float top) __attribute__((always_inline)) {
                 top = fmaxf(s.m, top);
@@ -433,17 +433,17 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args 
 #pragma unroll
             for (int from = 0; from < R; from += G) {
                 if (from > 0 && from * NT >= vectors) break;
-                if ((from + G) * NT > vectors) {  // not for all threads
+                if (__builtin_expect((from + G) * NT > vectors, false)) {  // not for all threads
 #pragma unroll
                     for (int v = from; v < from + G; v++)
-                        if (own + v * NT >= vectors) x[v] = banned<T, V>();
+                        if ((v + 1) * NT > vectors && own + v * NT >= vectors) x[v] = banned<T, V>();
                 }
                 raise_to(largest_of<G>(x, from));
 #pragma unroll
                 for (int v = from; v < from + G; v++) {
-                    float sum = __builtin_amdgcn_exp2f((x[v][0] - s.m) * c);
+                    float sum = __builtin_amdgcn_exp2f(less<T>(x[v][0], s.m) * c);
 #pragma unroll
-                    for (int e = 1; e < V; e++) sum += __builtin_amdgcn_exp2f((x[v][e] - s.m) * c);
+                    for (int e = 1; e < V; e++) sum += __builtin_amdgcn_exp2f(less<T>(x[v][e], s.m) * c);
                     s.s += sum;
                     x[v].keep();
                     __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time

@@ -120,6 +120,19 @@ struct Row {
     __device__ int64_t edge(int t) const { return vectors * V + t; }  // the t-th single element
 };
 
+// x - m for an x of type T that has just been unpacked: of fp16 as x 1 - m, with a 1 that the compiler does not know, because a fused
+// product takes a half from where it lies.  The same number, and an instruction less a value: policy step of 750 x 32000 17.8 us for 18.7.
+template <typename T>
+__device__ __forceinline__ float less(float x, float m) {
+    if constexpr (std::is_same_v<T, f16>) {
+        float one = 1.0f;
+        asm("" : "+s"(one));
+        return fmaf(x, one, -m);
+    } else {
+        return x - m;
+    }
+}
+
 // q_v times a weight, from a logit.  The exponent is (x - m) c - l, with c = log2(e) / T in two parts where the result is fp32.
 // The instruction's exp2 gives 0 below 2^-126, where a product with the weight still has a value: there the
 // exponent is raised by 32 and the product lowered by it.
@@ -139,7 +152,7 @@ struct Softmax {
     __device__ __forceinline__ float weighted(float x) const { return less(x, 0.0f); }
     // w (q - p)
     __device__ __forceinline__ float less(float x, float p) const {
-        const float d = x - m;
+        const float d = byz_worker::less<T>(x, m);
         if constexpr (sizeof(T) == 4) {
             // c_low can be 0 or less: the small term of a banned entry, d = -inf, is that of a finite d, or the sum would be NaN
             const float e = fmaf(d, c, fmaf(fmaxf(d, -0x1p64f), c_low, -l));
