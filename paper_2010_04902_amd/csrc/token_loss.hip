@@ -441,9 +441,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args 
                 raise_to(largest_of<G>(x, from));
 #pragma unroll
                 for (int v = from; v < from + G; v++) {
-                    float sum = __builtin_amdgcn_exp2f(less<T>(x[v][0], s.m) * c);
+                    float sum = __builtin_amdgcn_exp2f(less<T, true>(x[v][0], s.m) * c);
 #pragma unroll
-                    for (int e = 1; e < V; e++) sum += __builtin_amdgcn_exp2f(less<T>(x[v][e], s.m) * c);
+                    for (int e = 1; e < V; e++) sum += __builtin_amdgcn_exp2f(less<T, true>(x[v][e], s.m) * c);
                     s.s += sum;
                     x[v].keep();
                     __builtin_amdgcn_sched_barrier(0);  // one vector's values in registers at a time
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT, 4) void held_rows_kernel(Args 
         }
         if constexpr (!STEP) continue;
         T *out = (T *)a.dlogits + row * a.dlogits_ld;
-        const Softmax<T> q(s.m, s.s == 0.0f ? 1.0f : s.s, a.temperature, -w, c);
+        const Softmax<T, true> q(s.m, s.s == 0.0f ? 1.0f : s.s, a.temperature, -w, c);
         const int64_t ahead = row + gridDim.x;
         const bool more = kAlone && ahead < a.rows && a.label[ahead] >= 0;
         const Row<T> next(a.logits, more ? ahead : row, a.ld, a.vocab);

@@ -7,9 +7,10 @@
 
 namespace byz_worker {
 
-// A sum of positive terms in fp32: a thread adds some hundred of them at most, and the threads' sums are joined pairwise, so it
-// is good to some 2^-23 of itself, of which the loss has the logarithm.  In fp64 it would be ten times nearer, for a conversion
-// and an fp64 addition a value.
+// A sum of positive terms in fp32.  A vector's terms are added among themselves first, so that small ones are not lost one by one
+// beside a large sum; the threads' sums are joined pairwise.  A thread's is off by 2^-24 of itself for each of its vectors at most, which
+// are 98 for 200003 logits of 16 bits over 256 threads.  The loss has the logarithm.  In fp64 it would cost a conversion and an
+// fp64 addition a value.
 struct RunningSum {
     float m = -INFINITY, s = 0.0f;  // maximum of the raw logits, sum of exp2((x - m) c)
     template <int N>
@@ -22,10 +23,10 @@ struct RunningSum {
             for (int i = 0; i < N; i++) s += x[i] == -INFINITY ? 0.0f : x[i];
             return;
         }
-        float sum = s * __builtin_amdgcn_exp2f((m - top) * c);
+        float sum = __builtin_amdgcn_exp2f((x[0] - top) * c);
 #pragma unroll
-        for (int i = 0; i < N; i++) sum += __builtin_amdgcn_exp2f((x[i] - top) * c);
-        s = sum, m = top;
+        for (int i = 1; i < N; i++) sum += __builtin_amdgcn_exp2f((x[i] - top) * c);
+        s = fmaf(s, __builtin_amdgcn_exp2f((m - top) * c), sum), m = top;
     }
     // The power is taken in halves: a sum of the resident kernel can be 2^117 of its m and weigh something where the power itself is
     // less than fp32 has.
@@ -120,11 +121,12 @@ struct Row {
     __device__ int64_t edge(int t) const { return vectors * V + t; }  // the t-th single element
 };
 
-// x - m for an x of type T that has just been unpacked: of fp16 as x 1 - m, with a 1 that the compiler does not know, because a fused
-// product takes a half from where it lies.  The same number, and an instruction less a value: policy step of 750 x 32000 17.8 us for 18.7.
-template <typename T>
+// x - m for an x that was just unpacked.  FUSED: of fp16 as x 1 - m with a 1 that the compiler does not know, because a fused product takes
+// a half from where it lies; the same number for an instruction less a value.  Where rows are held in registers that counts (policy
+// step of 750 x 32000 17.8 us for 18.7), where they stream past it does not (distillation step of 8192 x 20000 173 us for 171).
+template <typename T, bool FUSED>
 __device__ __forceinline__ float less(float x, float m) {
-    if constexpr (std::is_same_v<T, f16>) {
+    if constexpr (FUSED && std::is_same_v<T, f16>) {
         float one = 1.0f;
         asm("" : "+s"(one));
         return fmaf(x, one, -m);
@@ -136,7 +138,7 @@ __device__ __forceinline__ float less(float x, float m) {
 // q_v times a weight, from a logit.  The exponent is (x - m) c - l, with c = log2(e) / T in two parts where the result is fp32.
 // The instruction's exp2 gives 0 below 2^-126, where a product with the weight still has a value: there the
 // exponent is raised by 32 and the product lowered by it.
-template <typename T>
+template <typename T, bool FUSED = false>
 struct Softmax {
     float m, c, c_low, l, w;
     __device__ Softmax(double m_, double log_sum, double temperature, float weight) {
@@ -152,7 +154,7 @@ struct Softmax {
     __device__ __forceinline__ float weighted(float x) const { return less(x, 0.0f); }
     // w (q - p)
     __device__ __forceinline__ float less(float x, float p) const {
-        const float d = byz_worker::less<T>(x, m);
+        const float d = byz_worker::less<T, FUSED>(x, m);
         if constexpr (sizeof(T) == 4) {
             // c_low can be 0 or less: the small term of a banned entry, d = -inf, is that of a finite d, or the sum would be NaN
             const float e = fmaf(d, c, fmaf(fmaxf(d, -0x1p64f), c_low, -l));

@@ -1,5 +1,5 @@
 """The token operators at the ends of their values' range: dropped values that are no numbers, the statistics of rows whose largest
-values lie anywhere, ratios next to the clipping's ends, banned tokens."""
+values lie anywhere, many small terms beside a large one, ratios next to the clipping's ends, banned tokens."""
 import math
 
 import pytest
@@ -223,3 +223,18 @@ def test_a_token_that_the_reference_bans(rows, vocab, dtype):
     tol = _u(dtype) * full.abs() + E * (128 * q[1:] + 4 * q[1:] * q_log + 8 * hot[1:]) + 2.0 ** -24 * (dtype == F16)
     for grad in (step, alone):
         _near(grad[1:], full, tol, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(130, 200003), (2, 200003), (130, 20011)])
+def test_many_small_terms_next_to_a_large_one(rows, vocab, dtype):
+    """256 vectors of 16 bytes start with a 1, all else terms that are each just under half of its last bit: they count."""
+    V = 128 // torch.finfo(dtype).bits
+    z = torch.full((rows, vocab), -16.75, dtype=dtype, device=DEV)
+    z[:, :256 * V:V] = 0.0
+    label = torch.arange(rows, dtype=torch.int32, device=DEV)
+    want, _, _ = logp_terms(z, label, 1.0)
+    _near(B.byz_token_logp(z, label)[0], want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "logp")
+    _, lse = B.byz_distill_loss(z, torch.zeros(rows, 1, device=DEV), label[:, None].contiguous())
+    want = z.double().logsumexp(1)
+    _near(lse, want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "log-sum of distillation")
