@@ -203,7 +203,7 @@ int byz_residual_norm_backward(const void *dout, int64_t dout_ld, const void *dy
  *     logp[i] = z_label / temperature - log sum_v exp(z_v / temperature),  q = softmax of z / temperature
  * A logit of -inf is a banned one: q = 0 there, logp = -inf if it is the label's.  A label of vocab or more makes the row NaN, and
  * its gradient.  stats: rows * 2, the row's largest logit m and log sum_v exp((z_v - m) / temperature), for the backward calls
- * (0 and 0 where all are banned or there is no token); where it is an output it may be NULL.  temperature > 0; vocab < 2^31.
+ * (0 and 0 where all are banned or there is no token); where it is an output it may be NULL.  temperature >= 2^-64; vocab < 2^31.
  * All calls of this section take a workspace of byz_token_loss_workspace_bytes.  dlogits (pitch dlogits_ld, type dtype)
  * may be the logits themselves with the same pitch.
  */

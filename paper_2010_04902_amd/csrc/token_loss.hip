@@ -673,7 +673,8 @@ Args args_of(const void *logits, int64_t rows, int64_t vocab, int64_t ld, const 
 
 // The checks that all calls share, and the workspace's parts.
 int check(Args &a, int dtype, bool gradient, void *workspace, size_t bytes) {
-    if (!sizes_ok(a.rows, a.vocab, dtype) || !(a.temperature > 0.0f) || !real(a.temperature)) return BYZ_EINVAL;
+    // colder by some 2^-24, log2(e) / T in two parts times a banned logit's difference passes fp32's range
+    if (!sizes_ok(a.rows, a.vocab, dtype) || !(a.temperature >= 0x1p-64f) || !real(a.temperature)) return BYZ_EINVAL;
     if (a.rows == 0) return BYZ_OK;
     if (!a.logits || !a.label || !aligned(a.logits, dtype_size(dtype)) || !aligned(a.label, 4) || a.ld < a.vocab ||
         !extent_ok(a.rows, a.ld, a.vocab) || !floats_ok(a.stats) || !floats_ok(a.given_stats))

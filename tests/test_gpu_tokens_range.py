@@ -238,3 +238,33 @@ def test_many_small_terms_next_to_a_large_one(rows, vocab, dtype):
     _, lse = B.byz_distill_loss(z, torch.zeros(rows, 1, device=DEV), label[:, None].contiguous())
     want = z.double().logsumexp(1)
     _near(lse, want, _sum_tol(vocab, dtype) + 2 * E * want.abs(), "log-sum of distillation")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, vocab", [(6, 300), (5, 9001), (4, 50021), (130, 66001)])
+def test_extreme_temperatures(rows, vocab, dtype):
+    """The coldest leaves the largest logit alone, the hottest makes all alike that are not banned."""
+    gen = _gen(vocab)
+    z = _randn(gen, rows, vocab)
+    z = z.masked_fill(torch.rand(rows, vocab, generator=gen, device=DEV) < 0.2, -math.inf)
+    label = torch.randint(0, vocab, (rows,), generator=gen, device=DEV).to(torch.int32)
+    z[torch.arange(rows, device=DEV), label.long()] = 20.0
+    z = z.to(dtype)
+    d = torch.rand(rows, generator=gen, device=DEV) + 0.5
+    for temperature in (2.0 ** -64, 2.0 ** 64):
+        want, q, hot = logp_terms(z, label, temperature)
+        old = want.float()
+        logp, stats = B.byz_token_logp(z, label, temperature)
+        _, logp2, step = B.byz_policy_loss_step(z, label, old, -torch.ones(rows, device=DEV), d, clip_low=1.0, temperature=temperature)
+        alone = B.byz_token_logp_backward(d, z, label, stats, temperature)
+        for got in (logp, logp2):
+            _near(got, want, (0.0 if temperature < 1 else _sum_tol(vocab, dtype)) + 2 * E * want.abs(), "logp")
+        if temperature < 1:
+            assert bool((alone == 0).all()) and bool((step == 0).all())
+            continue
+        w = d.double()[:, None] / temperature
+        full = w * (hot - q)
+        # q's exponents have some 20 units, of which 2^-20 is rounding; the step's ratio has that of logp and old
+        tol = _u(dtype) * full.abs() + w * (q + hot) * 2.0 ** -17 + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+        _near(alone, full, tol, "dlogits")
+        _near(step, full, tol, "dlogits of the step")

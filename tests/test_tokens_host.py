@@ -179,6 +179,12 @@ def test_loss_refusals(name):
 
 
 @pytest.mark.parametrize("name", CALLS)
+def test_losses_refuse_temperatures_next_to_0(name):
+    for value in (2.0 ** -65, 1e-30, 2.0 ** -149):
+        assert getattr(W._load(), name)(*{**CALLS[name], "temperature": value}.values(), None) == EINVAL
+
+
+@pytest.mark.parametrize("name", CALLS)
 def test_loss_without_rows(name):
     none = dict(rows=0, logits=None, label=None, ws=None, nbytes=0)
     if "preference" in name:
