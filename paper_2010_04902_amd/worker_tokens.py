@@ -32,6 +32,9 @@ class byz_residual_form(ctypes.Structure):
         super().__init__(post, pre, eps, scale, p, seed & _WORD, offset & _WORD, None, first_row)
         self.offset_at = offset_at
 
+    def __setattr__(self, name, value):
+        super().__setattr__(name, _row(value) if name == "first_row" else value)
+
     @property
     def offset_at(self):
         return self._counter
@@ -84,6 +87,13 @@ def _load():
 # 10.8 / 5.4, policy loss 13.7 / 6.2, its step 14.4 / 6.5, preference step 19.3 / 11.3.
 
 
+def _row(n):
+    """n, if the library can be given it whole; which rows there are it says itself."""
+    if not -2 ** 63 <= n < 2 ** 63:
+        raise ValueError("first_row is %d, the last row there can be is 2^32 - 1" % n)
+    return n
+
+
 def _counter(t):
     """Address of an int64 of one element on the GPU."""
     if _lib is None:
@@ -124,6 +134,7 @@ def byz_dropout(x, p, seed, offset=0, offset_at=None, first_row=0, out=None, str
         done = _calls.dropout(x, p, seed, offset, first_row)
         if done is not None:
             return _w._done(done, "byz_dropout")
+    first_row = _row(first_row)
     _w._outside_the_graph(x)
     rows, cols, ld = _w._matrix(x, "x")
     index, dtype = _w._device(x, "x"), _w._dtype(x, "x")

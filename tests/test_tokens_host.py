@@ -220,3 +220,15 @@ def test_binding_refuses_other_layouts():
     for x in (torch.zeros(10), torch.zeros(2, 3, 4), torch.zeros(10, 4).t(), torch.zeros(4, 1).expand(4, 10)):
         with pytest.raises(ValueError):
             B.byz_dropout(x, 0.1, 1)
+
+
+def test_binding_refuses_rows_that_would_wrap():
+    for first_row in (2 ** 63, 2 ** 64, 2 ** 64 + 5, -2 ** 63 - 1):
+        with pytest.raises(ValueError, match="first_row"):
+            B.byz_residual_form(first_row=first_row)
+        form = B.byz_residual_form(first_row=7)
+        with pytest.raises(ValueError, match="first_row"):
+            form.first_row = first_row
+        assert form.first_row == 7
+        with pytest.raises(ValueError, match="first_row"):
+            B.byz_dropout(torch.zeros(4, 10), 0.1, 1, first_row=first_row)
