@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2010_04902_amd as B
-from test_gpu_tokens import DEV, F16, TYPES, _gen, _near, _randn, _residual_case, _residual_run, _same_bits, _u
+from test_gpu_tokens import DEV, F16, TYPES, _gen, _near, _randn, _residual_case, _residual_check, _residual_run, _residual_want, _same_bits, _u
 from token_forms import E, kept, logp_terms
 
 pytestmark = pytest.mark.gpu
@@ -268,3 +268,12 @@ def test_extreme_temperatures(rows, vocab, dtype):
         tol = _u(dtype) * full.abs() + w * (q + hot) * 2.0 ** -17 + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
         _near(alone, full, tol, "dlogits")
         _near(step, full, tol, "dlogits of the step")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, cols, gate", [(1100, 8200, 550), (1030, 9001, 1)])
+def test_wide_rows_in_turn_with_layer_norms(rows, cols, gate, dtype):
+    """More rows than there are blocks, so that a block takes a second and a third one."""
+    c = _residual_case(rows, cols, dtype, "layer", "layer", gate, 0.1, bias=True, seed=rows)
+    want = _residual_want(c, "layer", "layer", 0.1)
+    _residual_check(_residual_run(c), want, dtype)
