@@ -184,7 +184,8 @@ int byz_residual_norm(const void *x, int64_t x_ld, const void *h, int64_t h_ld, 
 
 /*
  * Its gradients for dout and dy (either may be NULL: zeros), from the call's x, h and stats: dx and dh (no dh without h), and those of
- * the vectors, fp32 sums over the rows, each of which may be NULL; d_gate has gate's shape.
+ * the vectors, fp32 sums over the rows, each of which may be NULL; d_gate has gate's shape.  The workspace is that of the call's gate_rows, and
+ * of gate_rows = rows without a gate.
  */
 size_t byz_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype, int64_t gate_rows);
 int byz_residual_norm_backward(const void *dout, int64_t dout_ld, const void *dy, int64_t dy_ld, const void *x, int64_t x_ld,

@@ -5,7 +5,7 @@
 // thread does two.  Results go through the caches: stored past them 8192 x 16384 bf16 took 76 us alone, but 190 with an operation
 // behind it that reads the result, for 90 and 179.
 //
-// 8192 x 16384 bf16 90 us (5.9 TB/s), fp32 191 to 237; 70000 x 1517 bf16, rows at odd addresses, 97 (4.4 TB/s); 30 x 512 3.1.
+// 8192 x 16384 bf16 90 to 96 us (5.9 TB/s), fp32 191 to 237; 70000 x 1517 bf16, rows at odd addresses, 97 (4.4 TB/s); 30 x 512 3.1.
 #include <algorithm>
 
 #include "drop.h"

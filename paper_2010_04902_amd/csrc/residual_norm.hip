@@ -12,10 +12,10 @@
 // in registers, eight columns a thread, which is one call of the generator: a row is part of a wave, a wave, or up to 1024 threads.
 // Backward a thread also sums its columns over the rows of its block; the blocks' sums are joined by finish_kernel.  Narrower and wider
 // rows, and gates of a few rows each on more than 4096 columns, take kernels that read a row up to three times (once up to 16384 columns of
-// 16 bits, root mean squares) and the columns' sums by a second reading.  Short calls are bound by one row's chain (2 us, two reductions) and by reading the code: with
-// partial vectors unrolled a backward kernel of 15 KB took 13 us for one row; of half that length it takes 11 for two.
+// 16 bits, root mean squares) and the columns' sums by a second reading.  Short calls are bound by one row's chain (2 us, two reductions); code
+// counts there: with partial vectors unrolled a backward kernel of 15 KB took 13 us for one row; of half that length it takes 11 for two.
 //
-// 8192 x 4096 bf16, both norms RMS, gate and dropout: forward 48 us (5.6 TB/s, vector units busy 0.61), backward 91 (4.7 TB/s with the blocks'
+// 8192 x 4096 bf16, both norms RMS, gate and dropout: forward 48 to 53 us (5.6 TB/s, vector units busy 0.61), backward 91 (4.7 TB/s with the blocks'
 // sums, busy 0.57) and 6 for the join; with layer norms and biases 67 and 106 together.  1920 x 512 4.8, 10 and 5.
 #include <algorithm>
 
@@ -825,7 +825,7 @@ __global__ __launch_bounds__(back_block_of<TPR>(), back_waves<T>(TPR, GENERAL, P
 
 // dx, dh and the means of rows of 8193 to 16384 columns of 16 bits, root mean squares only and without additions: sixteen columns a
 // thread, in registers from the one read that rows_kernel does three times.  Their sums would not fit beside them and are
-// columns_kernel's.  Of the other norms and of fp32 the registers spill: rows_kernel's.  us of a whole backward pass, so and with
+// columns_kernel's.  Of the other norms and of fp32 the four tensors in registers spill: rows_kernel's.  us of a whole backward pass, so and with
 // rows_kernel: 2048 x 16384 bf16 200 and 260; with layer norms 284 and 255, 3000 x 9001 of them 344 and 257, 1024 x 16384 fp32 240 and 215.
 template <typename T>
 __global__ __launch_bounds__(1024, 4) void wide_rows_kernel(Args a, Back b) {

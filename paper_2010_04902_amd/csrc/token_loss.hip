@@ -9,7 +9,7 @@
 // Bound by memory.  The policy step holds rows of up to 256 KB in registers, so that they are read once; the preference step cannot: a
 // row's weight depends on all rows of its pair, so its logits are read twice, the last rows first the second time.
 //
-// 8192 x 131072 bf16 policy step 777 to 820 us (4.2 GB at 5.3 TB/s, vector units busy 0.63); 750 x 32000 fp16 18.9.  6144 x 50021 bf16 preference
+// 8192 x 131072 bf16 policy step 772 to 826 us (4.3 GB at 5.2 to 5.6 TB/s, vector units busy 0.66); 750 x 32000 fp16 17.8 to 18.5.  6144 x 50021 bf16 preference
 // step, a quarter of the rows prompts: sums 96, pairs 6, gradient 182 (5.9 TB/s).  7 x 50021 fp32 loss 7.3, one launch of 1024
 // threads a row.
 #include <algorithm>
